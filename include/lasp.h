@@ -402,6 +402,109 @@ int lasp_bidir_seq_bwd(const lasp_shape *shapes, int32_t T, const void *const *q
                        void *const *dq, void *const *dk, void *const *dv, void *scratch, size_t scratch_bytes,
                        void *hip_stream);
 
+/*
+ * ---- Gated linear recurrence ----------------------------------------------------
+ * The elementwise member of the family of App. A.4 (m_t = o_t m_{t-1} + e_t i_t^T with a vector state and a
+ * gate per channel; the HGRN and LRN rows of Table 6). For every sequence and channel, tokens s = 1..len:
+ *     a_s = exp(log_a_s),   b_s = 1, or 1 - a_s when `coupled`,
+ *     h_s = a_s h_{s-1} + b_s x_s,   h_0 = h_in,   out_s = h_s,   h_out = h_len.
+ * Backward, gradients of sum(out * dout) + sum(h_out * dh_out), with e_s the gradient w.r.t. h_s:
+ *     e_s = dout_s + a_{s+1} e_{s+1}  (e_len = dout_len + dh_out),   dx_s = b_s e_s,
+ *     dlog_a_s = a_s e_s (h_{s-1} - [coupled] x_s),   dh_in = a_1 e_1.
+ *
+ *   x, log_a, dx, dlog_a  [B][N] rows of D elements of `dtype`, `ld` elements from row to row (0 = D): the value and the
+ *           gate may lie side by side in the output of one projection, their gradients in that of its gradient.
+ *   out, dout  [B][N][D] of `dtype`.      h_in, h_out, dh_out, dh_in  [B][D] float.
+ *   log_a   any value up to 0 (above, the state grows). -inf: a = 0, the state starts anew at that token (documents
+ *           packed into one sequence); the gradient there is 0.
+ *   len     NULL, or DEVICE int32 [B]: tokens of every sequence, 0 <= len <= N (other values count as the nearest of
+ *           these). What the inputs hold past it is not looked at; out, dx and dlog_a are 0 there.
+ *   h_in    NULL = zeros. h_out may be h_in and dh_in may be dh_out (the same pointer): updated in place.
+ *   h_out, dh_in  may be NULL.     dh_out  NULL = zeros.
+ *   x       (backward) read only when coupled, may be NULL otherwise. out: as the forward call wrote it; h_{s-1} is taken
+ *           from there, so for bfloat16 data dlog_a carries that rounding (2^-9 of h).
+ *   scratch lasp_rec_scratch_bytes() bytes, for either call.
+ * The state is carried in float; float data: a is held in two floats, so that 1 - a keeps its bits near a = 1.
+ * Sequences continue as with lasp_fwd: h_out of one call is h_in of the next, dh_in the dh_out of the call before.
+ * Results are bit-reproducible. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, N < 1; D no
+ * positive multiple of 8; ld neither 0 nor a multiple of 8 from D up; more than 2^31 - 1 in B N or B D.
+ */
+typedef struct {
+    int32_t B, N, D;
+    int32_t dtype;    /* lasp_dtype */
+    int32_t coupled;  /* 0: b = 1, otherwise b = 1 - a */
+    int32_t ld;       /* 0 = D */
+} lasp_rec_shape;
+int lasp_check_rec(const lasp_rec_shape *shape);
+/* 0 on an invalid shape. */
+size_t lasp_rec_scratch_bytes(const lasp_rec_shape *shape);
+int lasp_rec_fwd(const lasp_rec_shape *shape, const void *x, const void *log_a, const float *h_in, const int32_t *len,
+                 void *out, float *h_out, void *scratch, size_t scratch_bytes, void *hip_stream);
+int lasp_rec_bwd(const lasp_rec_shape *shape, const void *x, const void *log_a, const void *out, const float *h_in,
+                 const int32_t *len, const void *dout, const float *dh_out, void *dx, void *dlog_a, float *dh_in,
+                 void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/*
+ * ---- Before a block: residual add and norm --------------------------------------
+ *     r_out = r + scale * x,     y = weight * r_out * rstd,     rstd = (mean_c r_out^2 + eps)^(-1/2)
+ * for every row (token) of C elements; y is taken from r_out before it is rounded to `dtype`. Backward, from r_out as
+ * stored (as rounded), with dr_out the gradient that reaches r_out past the norm:
+ *     dr = dr_out + rstd (weight * dy - r_out rstd^2 mean_c(weight * dy * r_out)),     dx = scale * dr,
+ *     dweight = sum over rows of dy * r_out * rstd,     dscale = sum over rows of x * dr.
+ *
+ *   r, x, r_out, y, dy, dr_out, dr, dx  [rows][C] of `dtype`.    scale, weight, dscale, dweight  [C] float.
+ *   x       forward: NULL = nothing is added (r_out and scale must then be NULL). backward: read for dscale only.
+ *   scale, weight  NULL = ones.      dr_out  NULL = zeros.      eps  >= 0, finite (LASP_ERR_SHAPE otherwise).
+ *   r_out   may be r, and dr may be dr_out (the same pointer): updated in place.
+ *   dx      NULL = not wanted (without a scale it equals dr).     dweight, dscale  NULL = not wanted.
+ *   scratch lasp_addnorm_scratch_bytes() bytes; not looked at when neither dweight nor dscale is wanted.
+ * Squares and sums are taken in float, dweight and dscale in a fixed order (bit-reproducible). Statuses and asynchrony as for
+ * lasp_fwd. Refused (LASP_ERR_SHAPE): rows < 1; C not a multiple of 8 in 8..16384.
+ */
+typedef struct {
+    int32_t rows, C;
+    int32_t dtype;    /* lasp_dtype */
+} lasp_rows;
+int lasp_check_rows(const lasp_rows *shape);
+size_t lasp_addnorm_scratch_bytes(const lasp_rows *shape);
+int lasp_addnorm_fwd(const lasp_rows *shape, const void *r, const void *x, const float *scale, const float *weight, float eps,
+                     void *r_out, void *y, void *hip_stream);
+int lasp_addnorm_bwd(const lasp_rows *shape, const void *r_out, const void *x, const float *scale, const float *weight, float eps,
+                     const void *dy, const void *dr_out, void *dr, void *dx, float *dweight, float *dscale, void *scratch,
+                     size_t scratch_bytes, void *hip_stream);
+
+/*
+ * ---- Behind a block: norm and gate ----------------------------------------------
+ *     n = o * rstd,     y = weight * n * act(u)
+ * from a mixer's output o, heads first (what lasp_fwd writes; a recurrence's out with H = 1), to y, tokens first (what the
+ * output projection reads). rstd as above, over the D features of a head or over the H D features of a token. act(u): u,
+ * sigmoid(u) or u sigmoid(u), or 1 with no gate. Backward, with t = dy * act(u):
+ *     du = dy * weight * n * act'(u),   do = rstd (weight * t - n mean(weight * t * n)),   dweight = sum over tokens of t * n.
+ *
+ *   o, do   [B][H][N][D] of `dtype`.     y, dy  [B][N][H D] of `dtype`.     weight, dweight  [H D] float.
+ *   u, du   [B][N] rows of H D elements of `dtype`, `ld` elements from row to row (0 = H D); not looked at with LASP_GATE_NONE.
+ *   weight  NULL = ones.      dweight  NULL = not wanted.      eps  >= 0, finite (LASP_ERR_SHAPE otherwise).
+ *   scratch lasp_gatenorm_scratch_bytes() bytes; not looked at when dweight is not wanted.
+ * Sums as for the norm before a block. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, H, N < 1; D no
+ * positive multiple of 8; more than 16384 elements in H D; more than 2^31 - 1 in B N H; an unknown gate or
+ * `over`; ld neither 0 nor a multiple of 8 from H D up.
+ */
+typedef enum { LASP_GATE_NONE = 0, LASP_GATE_IDENTITY = 1, LASP_GATE_SIGMOID = 2, LASP_GATE_SILU = 3 } lasp_gate;
+typedef enum { LASP_OVER_HEAD = 0, LASP_OVER_TOKEN = 1 } lasp_over;
+typedef struct {
+    int32_t B, H, N, D;
+    int32_t dtype;    /* lasp_dtype */
+    int32_t gate;     /* lasp_gate */
+    int32_t over;     /* lasp_over */
+    int32_t ld;       /* 0 = H D */
+} lasp_gate_shape;
+int lasp_check_gate(const lasp_gate_shape *shape);
+size_t lasp_gatenorm_scratch_bytes(const lasp_gate_shape *shape);
+int lasp_gatenorm_fwd(const lasp_gate_shape *shape, const void *o, const void *u, const float *weight, float eps, void *y,
+                      void *hip_stream);
+int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u, const float *weight, float eps, const void *dy,
+                      void *d_o, void *du, float *dweight, void *scratch, size_t scratch_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

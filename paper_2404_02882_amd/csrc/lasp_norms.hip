@@ -1,0 +1,581 @@
+// HIP kernels (gfx950 / CDNA4) for what stands before and behind a mixer in its block:
+//   k_addnorm_fwd / k_addnorm_bwd : residual add with a scale per channel, root-mean-square norm with a weight
+//   k_gate_fwd / k_gate_bwd       : norm of a mixer's output (heads first), times weight and gate, tokens first
+// All of them stream: a row is read once, kept in registers while its sums are formed, and written once. `LANES` threads
+// take a row, `PIECES` pieces of 16 bytes each; a workgroup takes several rows where one does not need it whole, and goes
+// on to further rows, so that weights are loaded once and the gradients of weights are summed in registers.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "lasp_block.h"
+
+namespace lasp {
+
+// Threads of a workgroup, and the rows it takes at a time.
+template <int LANES>
+struct Group {
+    static constexpr int NT = LANES > 256 ? LANES : 256, ROWS = NT / LANES, WAVES = LANES / 64;
+};
+
+// Sums over the threads of a row, in every one of them, in a fixed order.
+template <int LANES, int K>
+DEVI void row_sums(float (&v)[K], float *lds) {
+#pragma unroll
+    for (int d = LANES < 64 ? LANES / 2 : 32; d > 0; d >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
+    if constexpr (LANES > 64) {   // a row has the workgroup to itself
+        constexpr int WAVES = LANES / 64;
+        __syncthreads();          // the sums of the row before have been read
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) lds[k * WAVES + (threadIdx.x >> 6)] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v[k] += lds[k * WAVES + w];
+        }
+    }
+}
+DEVI float rstd_of(float squares, int C, float eps) { return 1.0f / __builtin_sqrtf(squares / (float)C + eps); }
+
+// The pieces of a row a thread takes: piece k is number lane + k LANES of C / W.
+template <typename T, int LANES, int PIECES>
+struct Mine {
+    static constexpr int W = Piece<T>::W;
+    int lane, n;
+    DEVI explicit Mine(int C) : lane(threadIdx.x % LANES), n(C / W) {}
+    DEVI bool has(int k) const { return lane + k * LANES < n; }
+    DEVI int at(int k) const { return min(lane + k * LANES, n - 1) * W; }   // (one that exists, whatever k)
+};
+template <int PIECES>
+struct Places {
+    int t[PIECES];
+};
+template <typename T, int LANES, int PIECES>
+DEVI Places<PIECES> places(const Mine<T, LANES, PIECES> &my) {
+    Places<PIECES> p;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) p.t[k] = my.at(k);
+    return p;
+}
+template <int W>
+DEVI void load_weight(const float *w, int at, float (&f)[W]) {
+    if (w) {
+        load_floats<W>(w + at, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) f[i] = 1.0f;
+    }
+}
+
+// The weights of a thread's pieces: in registers for all rows it takes, or (rows of a 1024-thread workgroup, whose threads have
+// 128 registers) loaded for every row.
+template <typename T, int LANES, int PIECES>
+struct Weights {
+    static constexpr int W = Piece<T>::W;
+    static constexpr bool KEEP = LANES <= 256;
+    const float *p;
+    float f[KEEP ? PIECES : 1][W];
+    DEVI Weights(const float *vec, const int (&at)[PIECES]) : p(vec) {
+        if constexpr (KEEP)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) load_weight<W>(p, at[k], f[k]);
+    }
+    DEVI void get(int k, int at, float (&w)[W]) const {
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = f[k][i];
+        } else {
+            load_weight<W>(p, at, w);
+        }
+    }
+};
+
+// A workgroup's sums for a vector of C floats, one partial row: its row groups are added one after the other in LDS.
+template <typename T, int LANES, int PIECES>
+DEVI void write_partial(const Mine<T, LANES, PIECES> &my, const float (&acc)[PIECES][Piece<T>::W], float *dst, float *lds) {
+    constexpr int W = Piece<T>::W, ROWS = Group<LANES>::ROWS;
+    const int row = threadIdx.x / LANES;
+    if constexpr (ROWS > 1) {
+        for (int r = 0; r < ROWS; ++r) {
+            __syncthreads();
+            if (row == r)
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k)
+                    if (my.has(k)) {
+                        float *p = lds + my.at(k);
+                        float f[W];
+#pragma unroll
+                        for (int i = 0; i < W; ++i) f[i] = acc[k][i];
+                        if (r > 0) {
+                            float g[W];
+                            load_floats<W>(p, g);
+#pragma unroll
+                            for (int i = 0; i < W; ++i) f[i] += g[i];
+                        }
+                        if (r == ROWS - 1) store_floats<W>(dst + my.at(k), f);
+                        else store_floats<W>(p, f);
+                    }
+        }
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+            if (my.has(k)) store_floats<W>(dst + my.at(k), acc[k]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Before a block.
+// ---------------------------------------------------------------------------
+template <typename T, int LANES, int PIECES>
+__global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_fwd(const T *r, const T *__restrict__ x, const float *__restrict__ scale,
+                                                                  const float *__restrict__ weight, float eps, T *r_out,
+                                                                  T *__restrict__ y, int rows, int C) {
+    using P = Piece<T>;
+    constexpr int W = P::W, ROWS = Group<LANES>::ROWS;
+    __shared__ float lds[Group<LANES>::NT / 64];
+    const Mine<T, LANES, PIECES> my(C);
+    const Weights<T, LANES, PIECES> ws(weight, places(my).t), scs(scale, places(my).t);
+    for (long long row0 = (long long)blockIdx.x * ROWS; row0 < rows; row0 += (long long)gridDim.x * ROWS) {
+        const long long row = row0 + threadIdx.x / LANES;
+        const bool there = row < rows;
+        const size_t base = (size_t)(there ? row : row0) * C;
+        u32x4 vr[PIECES], vx[PIECES];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            vr[k] = *(const u32x4 *)(r + base + my.at(k));
+            if (x) vx[k] = *(const u32x4 *)(x + base + my.at(k));
+        }
+        float f[PIECES][W], sums[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            P::unpack(vr[k], f[k]);
+            if (x) {
+                float g[W], sc[W];
+                P::unpack(vx[k], g);
+                scs.get(k, my.at(k), sc);
+#pragma unroll
+                for (int i = 0; i < W; ++i) f[k][i] = __builtin_fmaf(sc[i], g[i], f[k][i]);
+            }
+            if (my.has(k))
+#pragma unroll
+                for (int i = 0; i < W; ++i) sums[0] = __builtin_fmaf(f[k][i], f[k][i], sums[0]);
+        }
+        row_sums<LANES>(sums, lds);
+        const float rstd = rstd_of(sums[0], C, eps);
+        if (there)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                if (my.has(k)) {
+                    if (r_out) *(u32x4 *)(r_out + base + my.at(k)) = P::pack(f[k]);
+                    float o[W], w[W];
+                    ws.get(k, my.at(k), w);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) o[i] = f[k][i] * rstd * w[i];
+                    *(u32x4 *)(y + base + my.at(k)) = P::pack(o);
+                }
+    }
+}
+
+template <typename T, int LANES, int PIECES>
+__global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_bwd(const T *__restrict__ r, const T *__restrict__ x,
+                                                                  const float *__restrict__ scale, const float *__restrict__ weight,
+                                                                  float eps, const T *__restrict__ dy, const T *dr_out, T *dr,
+                                                                  T *__restrict__ dx, float *__restrict__ pw, float *__restrict__ ps,
+                                                                  int rows, int C) {
+    using P = Piece<T>;
+    constexpr int W = P::W, ROWS = Group<LANES>::ROWS;
+    __shared__ float lds[2 * Group<LANES>::NT / 64];
+    __shared__ __attribute__((aligned(16))) float part[ROWS > 1 ? LANES * PIECES * W : 4];
+    const Mine<T, LANES, PIECES> my(C);
+    const Weights<T, LANES, PIECES> ws(weight, places(my).t), scs(scale, places(my).t);
+    float aw[PIECES][W] = {}, as[PIECES][W] = {};
+    for (long long row0 = (long long)blockIdx.x * ROWS; row0 < rows; row0 += (long long)gridDim.x * ROWS) {
+        const long long row = row0 + threadIdx.x / LANES;
+        const bool there = row < rows;
+        const size_t base = (size_t)(there ? row : row0) * C;
+        u32x4 vr[PIECES], vy[PIECES], vx[PIECES], vd[PIECES];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            const size_t at = base + my.at(k);
+            vr[k] = *(const u32x4 *)(r + at);
+            vy[k] = *(const u32x4 *)(dy + at);
+            if (ps) vx[k] = *(const u32x4 *)(x + at);
+            if (dr_out) vd[k] = *(const u32x4 *)(dr_out + at);
+        }
+        float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+            if (my.has(k)) {
+                float f[W], g[W], w[W];
+                P::unpack(vr[k], f);
+                P::unpack(vy[k], g);
+                ws.get(k, my.at(k), w);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    sums[0] = __builtin_fmaf(f[i], f[i], sums[0]);
+                    sums[1] = __builtin_fmaf(w[i] * g[i], f[i], sums[1]);
+                }
+            }
+        row_sums<LANES>(sums, lds);
+        const float rstd = rstd_of(sums[0], C, eps), c = sums[1] / (float)C * rstd * rstd;
+        if (there)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                if (my.has(k)) {
+                    float f[W], g[W], d[W], o[W], w[W], sc[W];
+                    P::unpack(vr[k], f);
+                    P::unpack(vy[k], g);
+                    ws.get(k, my.at(k), w);
+                    scs.get(k, my.at(k), sc);
+                    if (dr_out) P::unpack(vd[k], d);
+                    else
+#pragma unroll
+                        for (int i = 0; i < W; ++i) d[i] = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        d[i] = __builtin_fmaf(rstd, w[i] * g[i] - f[i] * c, d[i]);
+                        aw[k][i] = __builtin_fmaf(g[i] * f[i], rstd, aw[k][i]);
+                        o[i] = sc[i] * d[i];
+                    }
+                    *(u32x4 *)(dr + base + my.at(k)) = P::pack(d);
+                    if (dx) *(u32x4 *)(dx + base + my.at(k)) = P::pack(o);
+                    if (ps) {
+                        P::unpack(vx[k], f);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) as[k][i] = __builtin_fmaf(f[i], d[i], as[k][i]);
+                    }
+                }
+    }
+    if (pw) write_partial<T, LANES, PIECES>(my, aw, pw + (size_t)blockIdx.x * C, part);
+    if (ps) write_partial<T, LANES, PIECES>(my, as, ps + (size_t)blockIdx.x * C, part);
+}
+
+// ---------------------------------------------------------------------------
+// Behind a block. A row is a head of a token (its C = D features) or a whole token (C = H D); `per` rows make a token, and
+// a thread stays with the same head of every token it comes to, so that its weights and their gradients stay in registers.
+// ---------------------------------------------------------------------------
+// act(u) and its derivative.
+DEVI void activate(int gate, float u, float &act, float &slope) {
+    if (gate == 1) {
+        act = u;
+        slope = 1.0f;
+    } else {
+        // 1 / (1 + 2^-u log2 e): 0 and 1 at the ends, where the power is infinite or 0
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.44269504f));
+        act = gate == 2 ? s : u * s;
+        slope = gate == 2 ? s * (1.0f - s) : s * __builtin_fmaf(u, 1.0f - s, 1.0f);
+    }
+}
+
+// Where a thread's pieces lie: o(k) in a token's part of o, t(k) in its row of u, y.
+template <typename T, int LANES, int PIECES>
+struct GatePlace {
+    Mine<T, LANES, PIECES> my;
+    long long slot, token0, step;   // this thread's row group, its first token, tokens from one turn to the next
+    size_t o[PIECES];
+    int t[PIECES];
+    DEVI GatePlace(int C, int per, int H, int N, int D) : my(C) {
+        constexpr int ROWS = Group<LANES>::ROWS;
+        slot = (long long)blockIdx.x * ROWS + threadIdx.x / LANES;
+        step = (long long)gridDim.x * ROWS / per;
+        token0 = slot / per;
+        const int head = (int)(slot - token0 * per);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            t[k] = head * C + my.at(k);
+            const int h = t[k] / D;
+            o[k] = (size_t)h * N * D + (t[k] - h * D);
+        }
+    }
+};
+
+template <typename T, int LANES, int PIECES>
+__global__ __launch_bounds__(Group<LANES>::NT) void k_gate_fwd(const T *__restrict__ O, const T *__restrict__ U,
+                                                               const float *__restrict__ weight, float eps, T *__restrict__ Y, int gate,
+                                                               int tokens, int per, int C, int H, int N, int D, long long ld) {
+    using P = Piece<T>;
+    constexpr int W = P::W;
+    __shared__ float lds[Group<LANES>::NT / 64];
+    const GatePlace<T, LANES, PIECES> at(C, per, H, N, D);
+    const auto &my = at.my;
+    const size_t wide = (size_t)H * D;
+    const Weights<T, LANES, PIECES> ws(weight, at.t);
+    // (every thread takes as many turns as the first of its workgroup: the sums may need all of them)
+    const long long first = (long long)blockIdx.x * Group<LANES>::ROWS / per;
+    for (long long turn = 0; first + turn * at.step < tokens; ++turn) {
+        const long long want = at.token0 + turn * at.step;
+        const bool there = want < tokens && at.token0 < at.step;
+        const size_t tok = there ? want : 0, seq = tok / N;
+        const T *o = O + (tok + seq * (H - 1) * N) * D;
+        u32x4 vo[PIECES], vu[PIECES];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            vo[k] = *(const u32x4 *)(o + at.o[k]);
+            if (gate) vu[k] = *(const u32x4 *)(U + tok * ld + at.t[k]);
+        }
+        float f[PIECES][W], sums[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            P::unpack(vo[k], f[k]);
+            if (my.has(k))
+#pragma unroll
+                for (int i = 0; i < W; ++i) sums[0] = __builtin_fmaf(f[k][i], f[k][i], sums[0]);
+        }
+        row_sums<LANES>(sums, lds);
+        const float rstd = rstd_of(sums[0], C, eps);
+        if (there)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                if (my.has(k)) {
+                    float u[W], w[W];
+                    if (gate) P::unpack(vu[k], u);
+                    ws.get(k, at.t[k], w);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        f[k][i] *= rstd * w[i];
+                        if (gate) {
+                            float act, slope;
+                            activate(gate, u[i], act, slope);
+                            f[k][i] *= act;
+                        }
+                    }
+                    *(u32x4 *)(Y + tok * wide + at.t[k]) = P::pack(f[k]);
+                }
+    }
+}
+
+template <typename T, int LANES, int PIECES>
+__global__ __launch_bounds__(Group<LANES>::NT) void k_gate_bwd(const T *__restrict__ O, const T *__restrict__ U,
+                                                               const float *__restrict__ weight, float eps, const T *__restrict__ dY,
+                                                               T *__restrict__ dO, T *__restrict__ dU, float *__restrict__ pw, int gate,
+                                                               int tokens, int per, int C, int H, int N, int D, long long ld) {
+    using P = Piece<T>;
+    constexpr int W = P::W, ROWS = Group<LANES>::ROWS;
+    __shared__ float lds[2 * Group<LANES>::NT / 64];
+    __shared__ __attribute__((aligned(16))) float part[ROWS > 1 ? LANES * PIECES * W : 4];
+    const GatePlace<T, LANES, PIECES> at(C, per, H, N, D);
+    const auto &my = at.my;
+    const size_t wide = (size_t)H * D;
+    const Weights<T, LANES, PIECES> ws(weight, at.t);
+    float aw[PIECES][W] = {};
+    const long long first = (long long)blockIdx.x * ROWS / per;
+    for (long long turn = 0; first + turn * at.step < tokens; ++turn) {
+        const long long want = at.token0 + turn * at.step;
+        const bool there = want < tokens && at.token0 < at.step;
+        const size_t tok = there ? want : 0, seq = tok / N, head0 = (tok + seq * (H - 1) * N) * D;
+        u32x4 vo[PIECES], vu[PIECES], vy[PIECES];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            vo[k] = *(const u32x4 *)(O + head0 + at.o[k]);
+            vy[k] = *(const u32x4 *)(dY + tok * wide + at.t[k]);
+            if (gate) vu[k] = *(const u32x4 *)(U + tok * ld + at.t[k]);
+        }
+        float sums[2] = {0.0f, 0.0f};
+        float g[PIECES][W], du[PIECES][W];   // dy act(u), dy weight act'(u)
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            float f[W], u[W], w[W];
+            P::unpack(vo[k], f);
+            P::unpack(vy[k], g[k]);
+            ws.get(k, at.t[k], w);
+            if (gate) {
+                P::unpack(vu[k], u);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    float act, slope;
+                    activate(gate, u[i], act, slope);
+                    du[k][i] = g[k][i] * w[i] * slope;
+                    g[k][i] *= act;
+                }
+            }
+            if (my.has(k))
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    sums[0] = __builtin_fmaf(f[i], f[i], sums[0]);
+                    sums[1] = __builtin_fmaf(w[i] * g[k][i], f[i], sums[1]);
+                }
+        }
+        row_sums<LANES>(sums, lds);
+        const float rstd = rstd_of(sums[0], C, eps), c = sums[1] / (float)C * rstd * rstd;
+        if (there)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                if (my.has(k)) {
+                    float f[W], d[W], w[W];
+                    P::unpack(vo[k], f);
+                    ws.get(k, at.t[k], w);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        d[i] = rstd * (w[i] * g[k][i] - f[i] * c);
+                        aw[k][i] = __builtin_fmaf(g[k][i] * f[i], rstd, aw[k][i]);
+                    }
+                    *(u32x4 *)(dO + head0 + at.o[k]) = P::pack(d);
+                    if (gate) {
+#pragma unroll
+                        for (int i = 0; i < W; ++i) d[i] = du[k][i] * f[i] * rstd;
+                        *(u32x4 *)(dU + tok * ld + at.t[k]) = P::pack(d);
+                    }
+                }
+    }
+    if (!pw) return;
+    if (per == 1) {
+        write_partial<T, LANES, PIECES>(my, aw, pw + (size_t)blockIdx.x * C, part);
+    } else if (at.token0 < at.step) {   // a partial row per token of a turn; every head's part from its own threads
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+            if (my.has(k)) store_floats<W>(pw + at.token0 * wide + at.t[k], aw[k]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// k_column_sums: out[c] = part[0][c] + part[1][c] + ..., blockIdx.y one of two such sums. A workgroup takes 64 columns, 64
+// threads by 16 groups of rows; fixed order.
+// ---------------------------------------------------------------------------
+constexpr int kSumColumns = 64, kSumGroups = 16;
+__global__ __launch_bounds__(kSumColumns * kSumGroups / 4) void k_column_sums(const float *__restrict__ part0, float *__restrict__ out0,
+                                                                              const float *__restrict__ part1, float *__restrict__ out1,
+                                                                              int n, int C) {
+    __shared__ f32x4 lds[kSumGroups][kSumColumns / 4];
+    const float *part = blockIdx.y ? part1 : part0;
+    float *out = blockIdx.y ? out1 : out0;
+    const int c4 = threadIdx.x % (kSumColumns / 4), g = threadIdx.x / (kSumColumns / 4);
+    const int c = blockIdx.x * kSumColumns + 4 * c4;
+    f32x4 sum{0, 0, 0, 0};
+    if (c < C)
+#pragma unroll 4
+        for (int r = g; r < n; r += kSumGroups) sum += *(const f32x4 *)(part + (size_t)r * C + c);
+    lds[g][c4] = sum;
+    __syncthreads();
+    if (g != 0 || c >= C) return;
+    for (int i = 1; i < kSumGroups; ++i) sum += lds[i][c4];
+    *(f32x4 *)(out + c) = sum;
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+RowPlan row_plan(int tokens, int heads, int C, int dtype) {
+    RowPlan p{tokens, heads, C, dtype, 64, 1};
+    const int n = C / (dtype == 0 ? 4 : 8);
+    if (n <= 8) p.lanes = 8;
+    else if (n <= 16) p.lanes = 16;
+    else if (n <= 32) p.lanes = 32;
+    else if (n > 1024) p.lanes = 1024;
+    else if (n > 256) p.lanes = 256;
+    p.pieces = n <= p.lanes ? 1 : n <= 2 * p.lanes ? 2 : 4;
+    return p;
+}
+namespace {
+constexpr int kWorkgroups = 512;
+int rows_at_a_time(const RowPlan &p) { return std::max(p.lanes, 256) / p.lanes; }
+// Workgroups: no more than there are rows for, and (rows that are heads) at least one row group for every head of a token.
+int workgroups(const RowPlan &p, int most) {
+    const long long rows = (long long)p.tokens * p.heads, at = rows_at_a_time(p);
+    return (int)std::max<long long>(std::min<long long>((rows + at - 1) / at, most), (p.heads + at - 1) / at);
+}
+int partial_rows(const RowPlan &p) {   // of a backward pass
+    const int n = workgroups(p, kWorkgroups);
+    return p.heads == 1 ? n : (int)((long long)n * rows_at_a_time(p) / p.heads);
+}
+hipError_t column_sums(const float *p0, float *o0, const float *p1, float *o1, int n, int C, hipStream_t s) {
+    if (!o0) {
+        p0 = p1;
+        o0 = o1;
+        o1 = nullptr;
+    }
+    if (o0) k_column_sums<<<dim3((C + kSumColumns - 1) / kSumColumns, o1 ? 2 : 1), dim3(kSumColumns * kSumGroups / 4), 0, s>>>(p0, o0, p1, o1, n, C);
+    return hipGetLastError();
+}
+// f.template operator()<T, LANES, PIECES>() for the plan's.
+template <typename T, typename F>
+void by_lanes(const RowPlan &p, F f) {
+    switch (p.lanes) {
+        case 8: return f.template operator()<T, 8, 1>();
+        case 16: return f.template operator()<T, 16, 1>();
+        case 32: return f.template operator()<T, 32, 1>();
+        case 64: return p.pieces == 1 ? f.template operator()<T, 64, 1>() : p.pieces == 2 ? f.template operator()<T, 64, 2>() : f.template operator()<T, 64, 4>();
+        case 256: return p.pieces == 2 ? f.template operator()<T, 256, 2>() : f.template operator()<T, 256, 4>();
+        default:
+            if constexpr (sizeof(T) == 4)
+                if (p.pieces == 4) return f.template operator()<T, 1024, 4>();
+            return f.template operator()<T, 1024, 2>();
+    }
+}
+template <typename F>
+void by_plan(const RowPlan &p, F f) {
+    if (p.dtype == 0) by_lanes<float>(p, f);
+    else by_lanes<bf16_t>(p, f);
+}
+struct AddNormFwd {
+    const RowPlan &p;
+    const AddNormArgs &a;
+    hipStream_t s;
+    template <typename T, int LANES, int PIECES>
+    void operator()() const {
+        k_addnorm_fwd<T, LANES, PIECES><<<dim3(workgroups(p, 2 * kWorkgroups)), dim3(Group<LANES>::NT), 0, s>>>(
+            (const T *)a.r, (const T *)a.x, a.scale, a.weight, a.eps, (T *)a.r_out, (T *)a.y, p.tokens, p.C);
+    }
+};
+struct AddNormBwd {
+    const RowPlan &p;
+    const AddNormArgs &a;
+    hipStream_t s;
+    template <typename T, int LANES, int PIECES>
+    void operator()() const {
+        const int n = workgroups(p, kWorkgroups);
+        k_addnorm_bwd<T, LANES, PIECES><<<dim3(n), dim3(Group<LANES>::NT), 0, s>>>(
+            (const T *)a.r, (const T *)a.x, a.scale, a.weight, a.eps, (const T *)a.dy, (const T *)a.dr_out, (T *)a.dr, (T *)a.dx,
+            a.dweight ? a.scratch : nullptr, a.dscale ? a.scratch + (size_t)n * p.C : nullptr, p.tokens, p.C);
+    }
+};
+struct GateFwd {
+    const RowPlan &p;
+    const GateArgs &a;
+    hipStream_t s;
+    template <typename T, int LANES, int PIECES>
+    void operator()() const {
+        k_gate_fwd<T, LANES, PIECES><<<dim3(workgroups(p, 2 * kWorkgroups)), dim3(Group<LANES>::NT), 0, s>>>(
+            (const T *)a.o, (const T *)a.u, a.weight, a.eps, (T *)a.y, a.gate, p.tokens, p.heads, p.C, a.H, a.N, a.D, a.ld);
+    }
+};
+struct GateBwd {
+    const RowPlan &p;
+    const GateArgs &a;
+    hipStream_t s;
+    template <typename T, int LANES, int PIECES>
+    void operator()() const {
+        k_gate_bwd<T, LANES, PIECES><<<dim3(workgroups(p, kWorkgroups)), dim3(Group<LANES>::NT), 0, s>>>(
+            (const T *)a.o, (const T *)a.u, a.weight, a.eps, (const T *)a.dy, (T *)a.d_o, (T *)a.du, a.dweight ? a.scratch : nullptr,
+            a.gate, p.tokens, p.heads, p.C, a.H, a.N, a.D, a.ld);
+    }
+};
+}  // namespace
+
+size_t addnorm_scratch(const RowPlan &p) { return 2 * (size_t)partial_rows(p) * p.C * sizeof(float); }
+size_t gatenorm_scratch(const RowPlan &p) { return (size_t)partial_rows(p) * p.heads * p.C * sizeof(float); }
+
+hipError_t launch_addnorm_fwd(const RowPlan &p, const AddNormArgs &a, hipStream_t s) {
+    by_plan(p, AddNormFwd{p, a, s});
+    return hipGetLastError();
+}
+hipError_t launch_addnorm_bwd(const RowPlan &p, const AddNormArgs &a, hipStream_t s) {
+    by_plan(p, AddNormBwd{p, a, s});
+    const int n = partial_rows(p);
+    return column_sums(a.scratch, a.dweight, a.scratch + (size_t)n * p.C, a.dscale, n, p.C, s);
+}
+hipError_t launch_gatenorm_fwd(const RowPlan &p, const GateArgs &a, hipStream_t s) {
+    by_plan(p, GateFwd{p, a, s});
+    return hipGetLastError();
+}
+hipError_t launch_gatenorm_bwd(const RowPlan &p, const GateArgs &a, hipStream_t s) {
+    by_plan(p, GateBwd{p, a, s});
+    return column_sums(a.scratch, a.dweight, nullptr, nullptr, partial_rows(p), p.heads * p.C, s);
+}
+
+}  // namespace lasp

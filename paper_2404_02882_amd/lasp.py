@@ -26,6 +26,20 @@ class Shape(ctypes.Structure):
                 ("kv_heads", ctypes.c_int32), ("Dv", ctypes.c_int32)]
 
 
+class RecShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("coupled", ctypes.c_int32), ("ld", ctypes.c_int32)]
+
+
+class RowsShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class GateShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("over", ctypes.c_int32), ("ld", ctypes.c_int32)]
+
+
 class LaspError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -115,7 +129,23 @@ def _bind_bidir_sequence(handle):
     return handle
 
 
-lib = _bind_bidir_sequence(_bind(ctypes.CDLL(LIB_PATH)))
+def _bind_blocks(handle):
+    """The same for the gated recurrence and the norms around a mixer."""
+    rec, rows, gate, f = ctypes.POINTER(RecShape), ctypes.POINTER(RowsShape), ctypes.POINTER(GateShape), ctypes.c_float
+    for name, shape in (("rec", rec), ("addnorm", rows), ("gatenorm", gate)):
+        size = getattr(handle, f"lasp_{name}_scratch_bytes")
+        size.argtypes, size.restype = [shape], _sz
+    handle.lasp_check_rec.argtypes, handle.lasp_check_rows.argtypes, handle.lasp_check_gate.argtypes = [rec], [rows], [gate]
+    handle.lasp_rec_fwd.argtypes = [rec] + [_vp] * 7 + [_sz, _vp]
+    handle.lasp_rec_bwd.argtypes = [rec] + [_vp] * 11 + [_sz, _vp]
+    handle.lasp_addnorm_fwd.argtypes = [rows] + [_vp] * 4 + [f] + [_vp] * 3
+    handle.lasp_addnorm_bwd.argtypes = [rows] + [_vp] * 4 + [f] + [_vp] * 7 + [_sz, _vp]
+    handle.lasp_gatenorm_fwd.argtypes = [gate] + [_vp] * 3 + [f] + [_vp] * 2
+    handle.lasp_gatenorm_bwd.argtypes = [gate] + [_vp] * 3 + [f] + [_vp] * 5 + [_sz, _vp]
+    return handle
+
+
+lib = _bind_blocks(_bind_bidir_sequence(_bind(ctypes.CDLL(LIB_PATH))))
 
 
 def profile_begin(max_calls: int) -> None:
@@ -407,6 +437,179 @@ def lasp_bidir_seq_bwd(shapes, T, q, k, v, dout, kv, dkv, dq, dk, dv, scratch, s
                                 scratch.numel() * scratch.element_size(), _stream(stream))
     if rc != 0:
         raise LaspError(rc, "lasp_bidir_seq_bwd")
+
+
+# ---- The gated recurrence and the norms around a mixer --------------------------
+GATES = {"none": 0, "identity": 1, "sigmoid": 2, "silu": 3}
+OVER = {"head": 0, "token": 1}
+_TORCH = {LASP_F32: torch.float32, LASP_BF16: torch.bfloat16}
+
+
+def _dtype_code(dtype):
+    if isinstance(dtype, torch.dtype):
+        return {torch.float32: LASP_F32, torch.bfloat16: LASP_BF16}.get(dtype, -1)
+    return {"f32": LASP_F32, "bf16": LASP_BF16}.get(dtype, -1) if isinstance(dtype, str) else int(dtype)
+
+
+def make_rec_shape(B, N, D, dtype, coupled=False, ld=0) -> RecShape:
+    return RecShape(int(B), int(N), int(D), _dtype_code(dtype), int(bool(coupled)), int(ld))
+
+
+def make_rows(rows, C, dtype) -> RowsShape:
+    return RowsShape(int(rows), int(C), _dtype_code(dtype))
+
+
+def make_gate_shape(B, H, N, D, dtype, gate="silu", over="head", ld=0) -> GateShape:
+    """gate: one of GATES, over: one of OVER (unknown names are refused by the calls)."""
+    return GateShape(int(B), int(H), int(N), int(D), _dtype_code(dtype), GATES.get(gate, -1), OVER.get(over, -1), int(ld))
+
+
+def check_rec(shape: RecShape) -> int:
+    return int(lib.lasp_check_rec(ctypes.byref(shape)))
+
+
+def check_rows(shape: RowsShape) -> int:
+    return int(lib.lasp_check_rows(ctypes.byref(shape)))
+
+
+def check_gate(shape: GateShape) -> int:
+    return int(lib.lasp_check_gate(ctypes.byref(shape)))
+
+
+def rec_scratch_bytes(shape: RecShape) -> int:
+    return int(lib.lasp_rec_scratch_bytes(ctypes.byref(shape)))
+
+
+def addnorm_scratch_bytes(shape: RowsShape) -> int:
+    return int(lib.lasp_addnorm_scratch_bytes(ctypes.byref(shape)))
+
+
+def gatenorm_scratch_bytes(shape: GateShape) -> int:
+    return int(lib.lasp_gatenorm_scratch_bytes(ctypes.byref(shape)))
+
+
+class _Args:
+    """Addresses of a call's tensors, each checked for type, size, layout and device (these calls take no shape but the
+    plan's, so that a tensor of another one would be read past its end)."""
+
+    __slots__ = ("device", "dtype")
+
+    def __init__(self, dtype):
+        self.device, self.dtype = None, _TORCH.get(dtype)
+
+    def _placed(self, t, name):
+        if not t.is_cuda:
+            raise ValueError(f"{name}: must be on a GPU")
+        at = t.get_device()
+        if self.device is None:
+            self.device = at
+        elif at != self.device:
+            raise ValueError(f"{name}: on device {at}, other tensors of the call on {self.device}")
+        return t.data_ptr()
+
+    def of(self, t, name, numel, dtype=None):
+        """A contiguous tensor of `numel` elements (None passes)."""
+        if t is None:
+            return None
+        dtype = dtype or self.dtype
+        if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous, {numel} elements of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+        return self._placed(t, name)
+
+    def rows(self, t, name, B, N, width, ld):
+        """[B][N] rows of `width` elements, `ld` from row to row (0 = width)."""
+        if t is None:
+            return None
+        ld = ld or width
+        if t.dtype is not self.dtype or t.shape != (B, N, width) or (width > 1 and t.stride(2) != 1) or \
+                (N > 1 and t.stride(1) != ld) or (B > 1 and t.stride(0) != N * ld):
+            raise ValueError(f"{name}: must be [{B}][{N}][{width}] of {self.dtype}, rows {ld} apart, not {tuple(t.shape)} with "
+                             f"strides {t.stride()} of {t.dtype}")
+        return self._placed(t, name)
+
+    def scratch(self, t, name="scratch"):
+        if t is None:
+            return None, 0
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
+        return self._placed(t, name), t.numel() * t.element_size()
+
+    def call(self, fn, where, args, stream):
+        """On `stream`, or the current one of the tensors' device."""
+        at = self.device
+        if at is None:                     # a required tensor is missing: the library says which status that is
+            rc = fn(*args, None)
+        elif at == torch.cuda.current_device():
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+        else:
+            with torch.cuda.device(at):
+                rc = fn(*args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+        if rc != 0:
+            raise LaspError(rc, where)
+
+
+def lasp_rec_fwd(shape: RecShape, x, log_a, h_in, lens, out, h_out, scratch, stream=None) -> None:
+    """h_s = exp(log_a_s) h_{s-1} + b_s x_s per channel: x, log_a [B,N,D] (rows shape.ld apart), out [B,N,D], h_in, h_out float32
+    [B,D] or None, lens int32 [B] or None; raises LaspError on a non-zero status."""
+    a, s = _Args(shape.dtype), shape
+    f, n = torch.float32, s.B * s.D
+    args = (ctypes.byref(s), a.rows(x, "x", s.B, s.N, s.D, s.ld), a.rows(log_a, "log_a", s.B, s.N, s.D, s.ld), a.of(h_in, "h_in", n, f),
+            a.of(lens, "lens", s.B, torch.int32), a.of(out, "out", s.N * n), a.of(h_out, "h_out", n, f), *a.scratch(scratch))
+    a.call(lib.lasp_rec_fwd, "lasp_rec_fwd", args, stream)
+
+
+def lasp_rec_bwd(shape: RecShape, x, log_a, out, h_in, lens, dout, dh_out, dx, dlog_a, dh_in, scratch, stream=None) -> None:
+    """Gradients dx, dlog_a (as x, log_a), dh_in of lasp_rec_fwd, from its `out` (x: needed when coupled); raises LaspError on a
+    non-zero status."""
+    a, s = _Args(shape.dtype), shape
+    f, n = torch.float32, s.B * s.D
+    args = (ctypes.byref(s), a.rows(x, "x", s.B, s.N, s.D, s.ld), a.rows(log_a, "log_a", s.B, s.N, s.D, s.ld), a.of(out, "out", s.N * n),
+            a.of(h_in, "h_in", n, f), a.of(lens, "lens", s.B, torch.int32), a.of(dout, "dout", s.N * n), a.of(dh_out, "dh_out", n, f),
+            a.rows(dx, "dx", s.B, s.N, s.D, s.ld), a.rows(dlog_a, "dlog_a", s.B, s.N, s.D, s.ld), a.of(dh_in, "dh_in", n, f),
+            *a.scratch(scratch))
+    a.call(lib.lasp_rec_bwd, "lasp_rec_bwd", args, stream)
+
+
+def lasp_addnorm_fwd(shape: RowsShape, r, x, scale, weight, eps, r_out, y, stream=None) -> None:
+    """r_out = r + scale * x, y = weight * r_out / rms(r_out), rows of C (scale, weight float32 [C] or None; x, r_out None: the norm
+    of r alone); raises LaspError on a non-zero status."""
+    a, s, f = _Args(shape.dtype), shape, torch.float32
+    n = s.rows * s.C
+    args = (ctypes.byref(s), a.of(r, "r", n), a.of(x, "x", n), a.of(scale, "scale", s.C, f), a.of(weight, "weight", s.C, f), float(eps),
+            a.of(r_out, "r_out", n), a.of(y, "y", n))
+    a.call(lib.lasp_addnorm_fwd, "lasp_addnorm_fwd", args, stream)
+
+
+def lasp_addnorm_bwd(shape: RowsShape, r_out, x, scale, weight, eps, dy, dr_out, dr, dx, dweight, dscale, scratch, stream=None) -> None:
+    """Gradients of lasp_addnorm_fwd from its r_out (dr_out: what reaches r_out past the norm, or None; dx, dweight, dscale may be
+    None, scratch then too); raises LaspError on a non-zero status."""
+    a, s, f = _Args(shape.dtype), shape, torch.float32
+    n = s.rows * s.C
+    args = (ctypes.byref(s), a.of(r_out, "r_out", n), a.of(x, "x", n), a.of(scale, "scale", s.C, f), a.of(weight, "weight", s.C, f),
+            float(eps), a.of(dy, "dy", n), a.of(dr_out, "dr_out", n), a.of(dr, "dr", n), a.of(dx, "dx", n),
+            a.of(dweight, "dweight", s.C, f), a.of(dscale, "dscale", s.C, f), *a.scratch(scratch))
+    a.call(lib.lasp_addnorm_bwd, "lasp_addnorm_bwd", args, stream)
+
+
+def lasp_gatenorm_fwd(shape: GateShape, o, u, weight, eps, y, stream=None) -> None:
+    """y = weight * o / rms(o) * act(u): o [B,H,N,D], u [B,N,H*D] (rows shape.ld apart), y [B,N,H*D], weight float32 [H*D] or None;
+    raises LaspError on a non-zero status."""
+    a, s = _Args(shape.dtype), shape
+    wide, n = s.H * s.D, s.B * s.N * s.H * s.D
+    args = (ctypes.byref(s), a.of(o, "o", n), a.rows(u, "u", s.B, s.N, wide, s.ld), a.of(weight, "weight", wide, torch.float32), float(eps),
+            a.of(y, "y", n))
+    a.call(lib.lasp_gatenorm_fwd, "lasp_gatenorm_fwd", args, stream)
+
+
+def lasp_gatenorm_bwd(shape: GateShape, o, u, weight, eps, dy, do, du, dweight, scratch, stream=None) -> None:
+    """Gradients of lasp_gatenorm_fwd: do as o, du as u, dweight (may be None, scratch then too); raises LaspError on a non-zero
+    status."""
+    a, s = _Args(shape.dtype), shape
+    wide, n = s.H * s.D, s.B * s.N * s.H * s.D
+    args = (ctypes.byref(s), a.of(o, "o", n), a.rows(u, "u", s.B, s.N, wide, s.ld), a.of(weight, "weight", wide, torch.float32), float(eps),
+            a.of(dy, "dy", n), a.of(do, "do", n), a.rows(du, "du", s.B, s.N, wide, s.ld), a.of(dweight, "dweight", wide, torch.float32),
+            *a.scratch(scratch))
+    a.call(lib.lasp_gatenorm_bwd, "lasp_gatenorm_bwd", args, stream)
 
 
 class Workspace:
