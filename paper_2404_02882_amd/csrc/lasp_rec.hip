@@ -2,52 +2,66 @@
 // over channels: the vector-state member of the recurrences of LASP (arxiv 2404.02882) App. A.4, Table 6.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "lasp_block.h"
 
+#ifndef RWF
+#define RWF 4
+#define RRF 8
+#define EUF 3
+#endif
+#ifndef RWB
+#define RWB 4
+#define RRB 8
+#define EUB 2
+#endif
+#ifndef BACKN
+#define BACKN 8
+#endif
 namespace lasp {
 
-// The gate of one element. A step of the recurrence is y -> a y + u.
+// The gate of one token, or the product of several (log_a summed): a step of the recurrence is y -> a y + u.
 template <typename T>
 struct Gate;
-// bfloat16 data: a in one float. Its rounding, 2^-25 of a, is a relative 2^-25 / (1 - a) of what the state converges to;
+// bfloat16 data: a as a float. Its rounding, 2^-25 of a, is a relative 2^-25 / (1 - a) of what the state converges to;
 // log_a itself comes rounded to 2^-9, which weighs more for any a that a memory of fewer than 2^16 tokens has.
 template <>
 struct Gate<bf16_t> {
-    float a;
-    DEVI explicit Gate(float log_a) : a(__builtin_amdgcn_exp2f(log_a * 1.44269504f)) {}
-    DEVI float step(float y, float u) const { return __builtin_fmaf(a, y, u); }
-    DEVI float times(float y) const { return a * y; }
-    DEVI float b() const { return 1.0f - a; }
+    float w;
+    DEVI explicit Gate(float log_a) : w(__builtin_amdgcn_exp2f(log_a * 1.44269504f)) {}
+    static DEVI Gate of_word(float w) { return Gate(w, 0); }
+    DEVI float step(float y, float u) const { return __builtin_fmaf(w, y, u); }
+    DEVI float times(float y) const { return w * y; }
+    DEVI float b() const { return 1.0f - w; }
+
+private:
+    DEVI Gate(float word, int) : w(word) {}
 };
-// Float data: a = hi + lo. For |log_a| < 1/2 from m = a - 1 by its power series (log_a^9 / 9! < 2^-26 of log_a is left
-// out), so that 1 - a has 24 bits however near to 1 a is; beyond, lo = 0.
+// Float data: for -1/4 < log_a < 0 the distance a - 1 from 1, by its power series (what is left out, log_a^6 / 7! < 2^-24 of it,
+// rounds away), so that 1 - a has 24 bits however near to 1 a is: with a itself 20000 tokens of a = 1 - 1e-6 are 1.4e-4 off, as
+// every rounding of a goes the same way. The sign bit tells the two apart. Elsewhere the power: the exponent's rounding,
+// |log_a| 2^-24 of a, is at most 2^-25 of 1.
 template <>
 struct Gate<float> {
-    float hi, lo, m;
+    float w;
     DEVI explicit Gate(float l) {
-        if (__builtin_fabsf(l) < 0.5f) {
-            float q = 1.0f / 40320;
-            q = __builtin_fmaf(q, l, 1.0f / 5040);
-            q = __builtin_fmaf(q, l, 1.0f / 720);
-            q = __builtin_fmaf(q, l, 1.0f / 120);
-            q = __builtin_fmaf(q, l, 1.0f / 24);
-            q = __builtin_fmaf(q, l, 1.0f / 6);
-            q = __builtin_fmaf(q, l, 0.5f);
-            m = __builtin_fmaf(l * l, q, l);
-            hi = 1.0f + m;
-            lo = m - (hi - 1.0f);
-        } else {
-            // log_a log2(e) in two floats: the product's rounding would be |log_a| 2^-24 of a
-            const float t = l * 1.44269504f, rest = __builtin_fmaf(l, 1.44269504f, -t) + l * 1.92596303e-8f;
-            const float e = __builtin_amdgcn_exp2f(t);
-            hi = e > 0.0f ? __builtin_fmaf(e, rest * 0.693147181f, e) : e;   // (log_a = -inf: rest is NaN)
-            lo = 0.0f;
-            m = hi - 1.0f;
-        }
+        float q = 1.0f / 720;
+        q = __builtin_fmaf(q, l, 1.0f / 120);
+        q = __builtin_fmaf(q, l, 1.0f / 24);
+        q = __builtin_fmaf(q, l, 1.0f / 6);
+        q = __builtin_fmaf(q, l, 0.5f);
+        const float m = __builtin_fmaf(l * l, q, l), a = __builtin_amdgcn_exp2f(l * 1.44269504f);
+        w = l > -0.25f && l < 0.0f ? m : a;
     }
-    DEVI float step(float y, float u) const { return __builtin_fmaf(hi, y, __builtin_fmaf(lo, y, u)); }
-    DEVI float times(float y) const { return __builtin_fmaf(hi, y, lo * y); }
-    DEVI float b() const { return -m; }
+    static DEVI Gate of_word(float w) { return Gate(w, 0); }
+    DEVI bool near() const { return __builtin_bit_cast(int, w) < 0; }
+    DEVI float step(float y, float u) const { return __builtin_fmaf(w, y, u) + (near() ? y : 0.0f); }
+    DEVI float times(float y) const { return __builtin_fmaf(w, y, near() ? y : 0.0f); }
+    DEVI float b() const { return near() ? -w : 1.0f - w; }
+
+private:
+    DEVI Gate(float word, int) : w(word) {}
 };
 
 // Where a column lies: its sequence, first channel, tokens that exist.
@@ -166,32 +180,317 @@ __global__ __launch_bounds__(kStepThreads) void k_rec_step_bwd(const T *__restri
 }
 
 // ---------------------------------------------------------------------------
+// k_rec_tiles: the sequence in tiles, one workgroup each. A thread takes ROWS consecutive rows of a column (in the order of the
+// scan: from the first token on, backward from the last one), which it keeps in registers as they were loaded:
+//   1. its rows as one step y -> A y + X, joined over the rows of the wave and the waves of the workgroup,
+//   2. the tile's step is published, and the state that enters the tile found: the nearest tile in front whose end state
+//      is published, and the steps of those between, applied in order,
+//   3. its rows again, from the state that enters them, to the outputs.
+// So every input is read once and every output written once. States are applied one tile after the other whatever is
+// published when: the same results on every run.
+// Workgroups take their tiles from a counter, in the order of the scan: a tile waits only for tiles whose workgroups have
+// started, and those for none behind them, so every wait ends. Values carry their own flag: a word that is kEmpty has not
+// been published (NaN are published as another one), so no fence is needed.
+// ---------------------------------------------------------------------------
+constexpr unsigned kEmpty = 0xffffffffu;
+DEVI unsigned published(float f) { return f != f ? 0x7fc00000u : __builtin_bit_cast(unsigned, f); }
+
+struct RecLook {                 // in the scratch
+    unsigned *ticket;
+    unsigned long long *steps;   // [tile][column block][channel]: the gate's word, X
+    unsigned *ends;              // [tile][column block][channel]: the state behind the tile
+};
+template <typename V>
+DEVI V look(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V>
+DEVI void show(V *p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// The state behind tile `tile` - 1 for one channel, whose slots in consecutive tiles are `stride` apart, `slot` that of `tile`.
+template <typename T, int BACK>
+DEVI float entering(const RecLook &lk, int tile, size_t slot, size_t stride) {
+    auto at = [&](int k) { return slot - (size_t)min(k + 1, tile) * stride; };
+    unsigned long long step[BACK];
+#pragma unroll
+    for (int k = 0; k < BACK; ++k) step[k] = look(lk.steps + at(k));
+    for (;;) {
+        unsigned end[BACK];
+#pragma unroll
+        for (int k = 0; k < BACK; ++k) end[k] = look(lk.ends + at(k));
+        int found = -1, missing = BACK;   // nearest end; nearest tile without a step
+#pragma unroll
+        for (int k = BACK - 1; k >= 0; --k) {
+            if (end[k] != kEmpty) found = k;
+            if ((unsigned)step[k] == kEmpty) missing = k;
+        }
+        if (found >= 0 && found <= missing) {
+            float y = 0.0f;
+#pragma unroll
+            for (int k = BACK - 1; k >= 0; --k) {
+                if (k == found) y = __builtin_bit_cast(float, end[k]);
+                else if (k < found) y = Gate<T>::of_word(__builtin_bit_cast(float, (unsigned)step[k])).step(y, __builtin_bit_cast(float, (unsigned)(step[k] >> 32)));
+            }
+            return y;
+        }
+        // (a published step stays: asked for again only where one is missing)
+        if (missing < BACK) {
+#pragma unroll
+            for (int k = 0; k < BACK; ++k)
+                if ((unsigned)step[k] == kEmpty) step[k] = look(lk.steps + at(k));
+        }
+        __builtin_amdgcn_s_sleep(1);
+    }
+}
+
+// LANES threads side by side along the columns; the others of a wave are further rows.
+template <typename T, bool COUPLED, bool BWD, int LANES, int WAVES, int ROWS>
+__global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const T *__restrict__ X, const T *__restrict__ L, const T *__restrict__ out_in,
+                                                         const T *__restrict__ dout, const float *h_in, const float *enter,
+                                                         const int *__restrict__ len, T *__restrict__ out, T *__restrict__ dx,
+                                                         T *__restrict__ dl, float *leave, RecLook lk, int cols, int N, int D,
+                                                         long long ld, int ntiles, int nblocks) {
+    using P = Piece<T>;
+    constexpr int W = P::W, NT = 64 * WAVES, PARTS = 64 / LANES, NCH = LANES * W;
+    constexpr bool kKeepGates = sizeof(T) == 4;   // the rows' gates, once computed, in the place of their log_a
+    __shared__ float sL[WAVES][NCH], sX[WAVES][NCH];
+    __shared__ unsigned sTicket;
+    unsigned ticket = blockIdx.x;
+    if (ntiles > 1) {
+        if (threadIdx.x == 0) sTicket = __hip_atomic_fetch_add(lk.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        ticket = sTicket;
+    }
+    const int tile = __builtin_amdgcn_readfirstlane(ticket / nblocks), block = __builtin_amdgcn_readfirstlane(ticket % nblocks);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, part = lane / LANES, cl = lane % LANES;
+    const int col = block * LANES + cl;
+    const bool mine = col < cols;
+    const Column<T> c(min(col, cols - 1), N, D, len);
+    const size_t row0 = (size_t)c.seq * N;
+    const size_t pbase = row0 * ld + c.ch, tbase = row0 * D + c.ch;
+    // row r of the thread is token at(r)
+    const long long p0 = ((long long)tile * WAVES * PARTS + w * PARTS + part) * ROWS, first = BWD ? N - 1 - p0 : p0;
+    constexpr int dir = BWD ? -1 : 1;
+    auto at = [&](int r) { return first + dir * r; };
+    auto there = [&](int r) { return at(r) >= 0 && at(r) < c.n; };
+    const bool whole = __all(there(0) && there(ROWS - 1));
+
+    u32x4 vu[ROWS], vl[ROWS];   // x, or the gradient of out
+    [[maybe_unused]] u32x4 vo[BWD ? ROWS : 1], vx[BWD && COUPLED ? ROWS : 1];
+    auto load_all = [&](auto token) {   // of row r, one that exists
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            vl[r] = *(const u32x4 *)(L + pbase + token(r) * ld);
+            if constexpr (BWD) vu[r] = *(const u32x4 *)(dout + tbase + token(r) * D);
+            else vu[r] = *(const u32x4 *)(X + pbase + token(r) * ld);
+        }
+        if constexpr (BWD)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const long long t = token(r);
+                vo[r] = *(const u32x4 *)(out_in + tbase + (t > 0 ? t - 1 : 0) * D);
+                if constexpr (COUPLED) vx[r] = *(const u32x4 *)(X + pbase + t * ld);
+            }
+    };
+    if (whole) {
+        load_all(at);
+    } else {
+        load_all([&](int r) { return min(max(at(r), 0ll), (long long)max(c.n - 1, 0)); });
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)   // a row that does not exist leaves the state as it is
+            if (!there(r)) vl[r] = vu[r] = u32x4{0, 0, 0, 0};
+    }
+    // 1.
+    float S[W] = {}, Y[W] = {};   // the gates' product as its logarithm: a sum near 0 keeps the bits that a product near 1 would lose
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        float fl[W], fu[W], fw[W];
+        P::unpack(vl[r], fl);
+        P::unpack(vu[r], fu);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const Gate<T> g(fl[i]);
+            if constexpr (BWD) Y[i] = g.times(fu[i] + Y[i]);
+            else Y[i] = g.step(Y[i], COUPLED ? g.b() * fu[i] : fu[i]);
+            S[i] += fl[i];
+            fw[i] = g.w;
+        }
+        if constexpr (kKeepGates) vl[r] = P::pack(fw);
+    }
+    if constexpr (PARTS > 1) {   // joined with those in front, along the wave
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float l = __shfl_up(S[i], d), y = __shfl_up(Y[i], d);
+                if (lane >= d) {
+                    Y[i] = Gate<T>(S[i]).step(y, Y[i]);
+                    S[i] += l;
+                }
+            }
+    }
+    if (part == PARTS - 1) {
+        store_floats<W>(&sX[w][cl * W], Y);
+        store_floats<W>(&sL[w][cl * W], S);
+    }
+    // (the rows opaque from here on: the compiler would keep their gates as floats, twice the registers, for the second time)
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) asm volatile("" : "+v"(vl[r]), "+v"(vu[r]));
+    __syncthreads();
+    // 2. a thread per channel
+    const size_t nstate = (size_t)cols * W, stride = (size_t)nblocks * NCH;
+    for (int ch = threadIdx.x; ch < NCH; ch += NT) {
+        const size_t state = (size_t)block * NCH + ch, slot = tile * stride + state;
+        float tl = 0.0f, tx = 0.0f, y, gate[WAVES];
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const Gate<T> g(sL[i][ch]);
+            tx = g.step(tx, sX[i][ch]);
+            tl += sL[i][ch];
+            gate[i] = g.w;
+        }
+        const Gate<T> whole_tile(tl);
+        if (tile == 0) {
+            y = enter && state < nstate ? enter[state] : 0.0f;
+        } else {
+            if (tile + 1 < ntiles) show(lk.steps + slot, (unsigned long long)published(whole_tile.w) | (unsigned long long)published(tx) << 32);
+            y = entering<T, BACKN>(lk, tile, slot, stride);
+        }
+        const float end = whole_tile.step(y, tx);   // (as the tiles behind form it)
+        if (tile + 1 < ntiles) show(lk.ends + slot, published(end));
+        else if (leave && state < nstate) leave[state] = end;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float x = sX[i][ch];
+            sX[i][ch] = y;
+            y = Gate<T>::of_word(gate[i]).step(y, x);
+        }
+    }
+    __syncthreads();
+    // 3.
+    float y[W];
+    load_floats<W>(&sX[w][cl * W], y);
+    if constexpr (PARTS > 1)
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float l = __shfl_up(S[i], LANES), x = __shfl_up(Y[i], LANES);
+            if (part > 0) y[i] = Gate<T>(l).step(y[i], x);
+        }
+    auto again = [](float f) {
+        if constexpr (kKeepGates) return Gate<T>::of_word(f);
+        else return Gate<T>(f);
+    };
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        float fl[W], fu[W];
+        P::unpack(vl[r], fl);
+        P::unpack(vu[r], fu);
+        if constexpr (!BWD) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const Gate<T> g = again(fl[i]);
+                y[i] = g.step(y[i], COUPLED ? g.b() * fu[i] : fu[i]);
+            }
+            if (mine && (whole || at(r) < N))
+                *(u32x4 *)(out + tbase + at(r) * D) = whole || there(r) ? P::pack(y) : u32x4{0, 0, 0, 0};
+        } else {
+            float fo[W], fx[W], ox[W], ol[W];
+            P::unpack(vo[r], fo);
+            if constexpr (COUPLED) P::unpack(vx[r], fx);
+            if (at(r) == 0) {
+                if (h_in) load_floats<W>(h_in + (size_t)c.seq * D + c.ch, fo);
+                else
+#pragma unroll
+                    for (int i = 0; i < W; ++i) fo[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const Gate<T> g = again(fl[i]);
+                const float e = fu[i] + y[i];
+                y[i] = g.times(e);
+                ox[i] = COUPLED ? g.b() * e : e;
+                ol[i] = y[i] * (COUPLED ? fo[i] - fx[i] : fo[i]);
+            }
+            if (mine && (whole || at(r) >= 0)) {
+                const size_t to = pbase + at(r) * ld;
+                *(u32x4 *)(dx + to) = whole || there(r) ? P::pack(ox) : u32x4{0, 0, 0, 0};
+                *(u32x4 *)(dl + to) = whole || there(r) ? P::pack(ol) : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
+}
+
+// The scratch of k_rec_tiles as its workgroups expect it: the counter 0, nothing published.
+__global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256)
+        scratch[i] = i < 16 ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
+}
+
+// ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-size_t rec_scratch(const RecPlan &) { return 256; }
+namespace {
+struct RecCut {
+    bool tiles;          // k_rec_tiles, or a thread per column
+    int lanes, nblocks, ntiles;
+    size_t slots, bytes; // of the scratch, beside the counter
+};
+constexpr int rec_rows(bool bwd) { return bwd ? RRB : RRF; }
+constexpr int rec_waves(bool bwd) { return bwd ? RWB : RWF; }
+RecCut rec_cut(const RecPlan &p, bool bwd) {
+    const int w = p.dtype == 0 ? 4 : 8, cols = p.B * (p.D / w);
+    RecCut c{};
+    c.tiles = p.N > 16;
+#ifndef LNMAX
+#define LNMAX 8
+#endif
+    c.lanes = cols > 32 ? 64 : cols > 16 ? 32 : cols > 8 ? 16 : 8;
+    c.lanes = std::min(c.lanes, LNMAX);
+    c.nblocks = (cols + c.lanes - 1) / c.lanes;
+    const int rows = rec_waves(bwd) * (64 / c.lanes) * rec_rows(bwd);
+    c.ntiles = (p.N + rows - 1) / rows;
+    c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * c.lanes * w : 0;
+    c.bytes = (c.slots * 12 + 15) / 16 * 16;
+    return c;
+}
+template <typename T, bool C, bool BWD, int LANES>
+void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t s) {
+    char *base = (char *)a.scratch;
+    RecLook lk{(unsigned *)base, (unsigned long long *)(base + 256), (unsigned *)(base + 256 + c.slots * 8)};
+    if (c.ntiles > 1) {
+        const size_t n = (256 + c.bytes) / 16;
+        k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, n);
+    }
+    const int cols = p.B * (p.D / Piece<T>::W);
+    k_rec_tiles<T, C, BWD, LANES, rec_waves(BWD), rec_rows(BWD)><<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * rec_waves(BWD)), 0, s>>>(
+        (const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, BWD ? a.dh_out : a.h_in, a.len, (T *)a.out, (T *)a.dx,
+        (T *)a.dlog_a, BWD ? a.dh_in : a.h_out, lk, cols, p.N, p.D, p.ld, c.ntiles, c.nblocks);
+}
+template <typename T, bool C, bool BWD>
+hipError_t rec(const RecPlan &p, const RecArgs &a, hipStream_t s) {
+    const RecCut c = rec_cut(p, BWD);
+    const int cols = p.B * (p.D / Piece<T>::W);
+    const dim3 grid((cols + kStepThreads - 1) / kStepThreads), block(kStepThreads);
+    if (c.tiles) {
+        if (c.lanes == 64) rec_tiles<T, C, BWD, 64>(p, a, c, s);
+        else if (c.lanes == 32) rec_tiles<T, C, BWD, 32>(p, a, c, s);
+        else if (c.lanes == 16) rec_tiles<T, C, BWD, 16>(p, a, c, s);
+        else rec_tiles<T, C, BWD, 8>(p, a, c, s);
+    } else if constexpr (BWD) {
+        k_rec_step_bwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, a.dh_out,
+                                                    a.len, (T *)a.dx, (T *)a.dlog_a, a.dh_in, cols, p.N, p.D, p.ld);
+    } else {
+        k_rec_step_fwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, a.h_in, a.len, (T *)a.out, a.h_out, cols, p.N, p.D, p.ld);
+    }
+    return hipGetLastError();
+}
+template <bool BWD>
+hipError_t by_type(const RecPlan &p, const RecArgs &a, hipStream_t s) {
+    if (p.dtype == 0) return p.coupled ? rec<float, true, BWD>(p, a, s) : rec<float, false, BWD>(p, a, s);
+    return p.coupled ? rec<bf16_t, true, BWD>(p, a, s) : rec<bf16_t, false, BWD>(p, a, s);
+}
+}  // namespace
 
-template <typename T, bool C>
-static hipError_t rec_fwd(const RecPlan &p, const RecArgs &a, hipStream_t s) {
-    const int cols = p.B * (p.D / Piece<T>::W);
-    k_rec_step_fwd<T, C><<<dim3((cols + kStepThreads - 1) / kStepThreads), dim3(kStepThreads), 0, s>>>(
-        (const T *)a.x, (const T *)a.log_a, a.h_in, a.len, (T *)a.out, a.h_out, cols, p.N, p.D, p.ld);
-    return hipGetLastError();
-}
-template <typename T, bool C>
-static hipError_t rec_bwd(const RecPlan &p, const RecArgs &a, hipStream_t s) {
-    const int cols = p.B * (p.D / Piece<T>::W);
-    k_rec_step_bwd<T, C><<<dim3((cols + kStepThreads - 1) / kStepThreads), dim3(kStepThreads), 0, s>>>(
-        (const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, a.dh_out, a.len, (T *)a.dx, (T *)a.dlog_a,
-        a.dh_in, cols, p.N, p.D, p.ld);
-    return hipGetLastError();
-}
-hipError_t launch_rec_fwd(const RecPlan &p, const RecArgs &a, hipStream_t s) {
-    if (p.dtype == 0) return p.coupled ? rec_fwd<float, true>(p, a, s) : rec_fwd<float, false>(p, a, s);
-    return p.coupled ? rec_fwd<bf16_t, true>(p, a, s) : rec_fwd<bf16_t, false>(p, a, s);
-}
-hipError_t launch_rec_bwd(const RecPlan &p, const RecArgs &a, hipStream_t s) {
-    if (p.dtype == 0) return p.coupled ? rec_bwd<float, true>(p, a, s) : rec_bwd<float, false>(p, a, s);
-    return p.coupled ? rec_bwd<bf16_t, true>(p, a, s) : rec_bwd<bf16_t, false>(p, a, s);
-}
+size_t rec_scratch(const RecPlan &p) { return 256 + std::max(rec_cut(p, false).bytes, rec_cut(p, true).bytes); }
+hipError_t launch_rec_fwd(const RecPlan &p, const RecArgs &a, hipStream_t s) { return by_type<false>(p, a, s); }
+hipError_t launch_rec_bwd(const RecPlan &p, const RecArgs &a, hipStream_t s) { return by_type<true>(p, a, s); }
 
 }  // namespace lasp
