@@ -472,7 +472,11 @@ RowPlan row_plan(int tokens, int heads, int C, int dtype) {
     return p;
 }
 namespace {
-constexpr int kWorkgroups = 512;
+#ifndef WGF
+#define WGF 1024
+#define WGB 512
+#endif
+constexpr int kWorkgroups = WGB;
 int rows_at_a_time(const RowPlan &p) { return std::max(p.lanes, 256) / p.lanes; }
 // Workgroups: no more than there are rows for, and (rows that are heads) at least one row group for every head of a token.
 int workgroups(const RowPlan &p, int most) {
@@ -518,7 +522,7 @@ struct AddNormFwd {
     hipStream_t s;
     template <typename T, int LANES, int PIECES>
     void operator()() const {
-        k_addnorm_fwd<T, LANES, PIECES><<<dim3(workgroups(p, 2 * kWorkgroups)), dim3(Group<LANES>::NT), 0, s>>>(
+        k_addnorm_fwd<T, LANES, PIECES><<<dim3(workgroups(p, WGF)), dim3(Group<LANES>::NT), 0, s>>>(
             (const T *)a.r, (const T *)a.x, a.scale, a.weight, a.eps, (T *)a.r_out, (T *)a.y, p.tokens, p.C);
     }
 };
@@ -540,7 +544,7 @@ struct GateFwd {
     hipStream_t s;
     template <typename T, int LANES, int PIECES>
     void operator()() const {
-        k_gate_fwd<T, LANES, PIECES><<<dim3(workgroups(p, 2 * kWorkgroups)), dim3(Group<LANES>::NT), 0, s>>>(
+        k_gate_fwd<T, LANES, PIECES><<<dim3(workgroups(p, WGF)), dim3(Group<LANES>::NT), 0, s>>>(
             (const T *)a.o, (const T *)a.u, a.weight, a.eps, (T *)a.y, a.gate, p.tokens, p.heads, p.C, a.H, a.N, a.D, a.ld);
     }
 };

@@ -6,19 +6,6 @@
 
 #include "lasp_block.h"
 
-#ifndef RWF
-#define RWF 4
-#define RRF 8
-#define EUF 3
-#endif
-#ifndef RWB
-#define RWB 4
-#define RRB 8
-#define EUB 2
-#endif
-#ifndef BACKN
-#define BACKN 8
-#endif
 namespace lasp {
 
 // The gate of one token, or the product of several (log_a summed): a step of the recurrence is y -> a y + u.
@@ -79,7 +66,7 @@ struct Column {
 // ---------------------------------------------------------------------------
 // k_rec_step_fwd / k_rec_step_bwd: a thread carries a column's state over all tokens, AHEAD tokens requested ahead.
 // ---------------------------------------------------------------------------
-constexpr int kStepThreads = 64, kAhead = 4;
+constexpr int kStepThreads = 64, kAhead = 8;
 
 template <typename T, bool COUPLED>
 __global__ __launch_bounds__(kStepThreads) void k_rec_step_fwd(const T *__restrict__ X, const T *__restrict__ L, const float *h_in,
@@ -188,15 +175,19 @@ __global__ __launch_bounds__(kStepThreads) void k_rec_step_bwd(const T *__restri
 //   3. its rows again, from the state that enters them, to the outputs.
 // So every input is read once and every output written once. States are applied one tile after the other whatever is
 // published when: the same results on every run.
-// Workgroups take their tiles from a counter, in the order of the scan: a tile waits only for tiles whose workgroups have
-// started, and those for none behind them, so every wait ends. Values carry their own flag: a word that is kEmpty has not
+// Workgroups take their tiles from counters, in the order of the scan: a tile waits only for tiles whose workgroups have
+// started, and those for none behind them, so every wait ends. Each counter serves a quarter of the column blocks: a single one
+// passes a workgroup every 13 ns, which is all the time of short tiles (8 x 1777 x 2048, half of it padding: 40.2 us, with four 35.0).
+// One for every block 33.6, but then the blocks drift apart, and rows of memory are opened more than once: 4 x 16384 x 4096
+// forward / backward 314 / 608 us, with four 306 / 596. Values carry their own flag: a word that is kEmpty has not
 // been published (NaN are published as another one), so no fence is needed.
 // ---------------------------------------------------------------------------
 constexpr unsigned kEmpty = 0xffffffffu;
 DEVI unsigned published(float f) { return f != f ? 0x7fc00000u : __builtin_bit_cast(unsigned, f); }
 
+constexpr int kGroups = 4, kTicketStride = 32;
 struct RecLook {                 // in the scratch
-    unsigned *ticket;
+    unsigned *tickets;           // [kGroups], a line of 128 bytes each
     unsigned long long *steps;   // [tile][column block][channel]: the gate's word, X
     unsigned *ends;              // [tile][column block][channel]: the state behind the tile
 };
@@ -241,25 +232,32 @@ DEVI float entering(const RecLook &lk, int tile, size_t slot, size_t stride) {
     }
 }
 
-// LANES threads side by side along the columns; the others of a wave are further rows.
-template <typename T, bool COUPLED, bool BWD, int LANES, int WAVES, int ROWS>
-__global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const T *__restrict__ X, const T *__restrict__ L, const T *__restrict__ out_in,
+// LANES threads side by side along the columns; the others of a wave are further rows. Eight, a line of 128 bytes of every row:
+// the fewer columns, the longer the tile and the fewer there are to pass the state on through (bfloat16 32768 x 2048, tiles of
+// 4 waves, 64 / 16 / 8 lanes: forward 214 / 92 / 88 us, backward 216 / 137 / 134).
+constexpr int kLanes = 8, kBack = 8;
+template <typename T, bool COUPLED, bool BWD, int WAVES, int ROWS>
+__global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_tiles(const T *__restrict__ X, const T *__restrict__ L, const T *__restrict__ out_in,
                                                          const T *__restrict__ dout, const float *h_in, const float *enter,
                                                          const int *__restrict__ len, T *__restrict__ out, T *__restrict__ dx,
                                                          T *__restrict__ dl, float *leave, RecLook lk, int cols, int N, int D,
                                                          long long ld, int ntiles, int nblocks) {
     using P = Piece<T>;
-    constexpr int W = P::W, NT = 64 * WAVES, PARTS = 64 / LANES, NCH = LANES * W;
+    constexpr int W = P::W, NT = 64 * WAVES, LANES = kLanes, PARTS = 64 / LANES, NCH = LANES * W;
+    static_assert(NCH <= 64, "a thread per channel");
     constexpr bool kKeepGates = sizeof(T) == 4;   // the rows' gates, once computed, in the place of their log_a
     __shared__ float sL[WAVES][NCH], sX[WAVES][NCH];
     __shared__ unsigned sTicket;
-    unsigned ticket = blockIdx.x;
+    // (moved on by one from tile to tile: a block's tiles then go to all XCDs in turn)
+    const unsigned turn = (nblocks % 8 == 0 ? blockIdx.x + blockIdx.x / nblocks : blockIdx.x) % nblocks;
+    const int group = turn % kGroups, per = (nblocks - group + kGroups - 1) / kGroups;   // column blocks group, group + kGroups, ...
+    unsigned ticket = turn / kGroups;
     if (ntiles > 1) {
-        if (threadIdx.x == 0) sTicket = __hip_atomic_fetch_add(lk.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (threadIdx.x == 0) sTicket = __hip_atomic_fetch_add(lk.tickets + group * kTicketStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         ticket = sTicket;
     }
-    const int tile = __builtin_amdgcn_readfirstlane(ticket / nblocks), block = __builtin_amdgcn_readfirstlane(ticket % nblocks);
+    const int tile = __builtin_amdgcn_readfirstlane(ticket / per), block = group + kGroups * __builtin_amdgcn_readfirstlane(ticket % per);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, part = lane / LANES, cl = lane % LANES;
     const int col = block * LANES + cl;
     const bool mine = col < cols;
@@ -272,6 +270,7 @@ __global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const
     auto at = [&](int r) { return first + dir * r; };
     auto there = [&](int r) { return at(r) >= 0 && at(r) < c.n; };
     const bool whole = __all(there(0) && there(ROWS - 1));
+    const bool none = !BWD && __all(first >= c.n);   // behind every sequence's last token: nothing to load, the state stays
 
     u32x4 vu[ROWS], vl[ROWS];   // x, or the gradient of out
     [[maybe_unused]] u32x4 vo[BWD ? ROWS : 1], vx[BWD && COUPLED ? ROWS : 1];
@@ -292,6 +291,9 @@ __global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const
     };
     if (whole) {
         load_all(at);
+    } else if (none) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) vl[r] = vu[r] = u32x4{0, 0, 0, 0};
     } else {
         load_all([&](int r) { return min(max(at(r), 0ll), (long long)max(c.n - 1, 0)); });
 #pragma unroll
@@ -337,7 +339,7 @@ __global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const
     __syncthreads();
     // 2. a thread per channel
     const size_t nstate = (size_t)cols * W, stride = (size_t)nblocks * NCH;
-    for (int ch = threadIdx.x; ch < NCH; ch += NT) {
+    if (const int ch = threadIdx.x; ch < NCH) {
         const size_t state = (size_t)block * NCH + ch, slot = tile * stride + state;
         float tl = 0.0f, tx = 0.0f, y, gate[WAVES];
 #pragma unroll
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const
             y = enter && state < nstate ? enter[state] : 0.0f;
         } else {
             if (tile + 1 < ntiles) show(lk.steps + slot, (unsigned long long)published(whole_tile.w) | (unsigned long long)published(tx) << 32);
-            y = entering<T, BACKN>(lk, tile, slot, stride);
+            y = entering<T, kBack>(lk, tile, slot, stride);
         }
         const float end = whole_tile.step(y, tx);   // (as the tiles behind form it)
         if (tile + 1 < ntiles) show(lk.ends + slot, published(end));
@@ -418,67 +420,73 @@ __global__ __launch_bounds__(64 * WAVES, BWD ? EUB : EUF) void k_rec_tiles(const
     }
 }
 
-// The scratch of k_rec_tiles as its workgroups expect it: the counter 0, nothing published.
-__global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t n) {
+// The scratch of k_rec_tiles as its workgroups expect it: the counters 0 (they come first), nothing published.
+__global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t counters, size_t n) {
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256)
-        scratch[i] = i < 16 ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
+        scratch[i] = i < counters ? u32x4{0, 0, 0, 0} : u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
 }
 
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+// How a call is cut (bfloat16, forward / backward in us, from a graph):
+//   a thread per column    up to kShort tokens, where all is latency (8 x 16 x 2048 5.3 / 6.9, as a tile 7.0 / 8.6; 24 tokens 6.7 / 9.1
+//                          and 7.0 / 8.6), and where the columns alone fill the device (64 x 64 x 16384 85 / 134 and 90 / 146)
+//   one tile               of as few waves as cover the tokens (64 x 64 x 2048 12.6 / 17.5, in four waves 22.8 / 37.8)
+//   tiles of 8 waves       of few columns and many tokens, where the state's way from tile to tile takes the time, 1 us per kBack tiles
+//                          (131072 x 128 33 / 49, in four waves 73 / 75; 32768 x 2048 95 / 139 and 88 / 134; 4096 x 64 even)
+//   tiles of 4 waves       otherwise
+constexpr int kShort = 16, kLong = 4096, kFewBlocks = 8, kManyColumns = 1 << 17;
 namespace {
 struct RecCut {
-    bool tiles;          // k_rec_tiles, or a thread per column
-    int lanes, nblocks, ntiles;
-    size_t slots, bytes; // of the scratch, beside the counter
+    int waves;                       // of a workgroup of k_rec_tiles; 0: a thread per column
+    int nblocks, ntiles;
+    size_t counters, slots, bytes;   // of the scratch: of the counters, slots, bytes of everything
 };
-constexpr int rec_rows(bool bwd) { return bwd ? RRB : RRF; }
-constexpr int rec_waves(bool bwd) { return bwd ? RWB : RWF; }
+constexpr int thread_rows(int waves, bool bwd) { return waves == 8 && !bwd ? 16 : 8; }
 RecCut rec_cut(const RecPlan &p, bool bwd) {
     const int w = p.dtype == 0 ? 4 : 8, cols = p.B * (p.D / w);
     RecCut c{};
-    c.tiles = p.N > 16;
-#ifndef LNMAX
-#define LNMAX 8
-#endif
-    c.lanes = cols > 32 ? 64 : cols > 16 ? 32 : cols > 8 ? 16 : 8;
-    c.lanes = std::min(c.lanes, LNMAX);
-    c.nblocks = (cols + c.lanes - 1) / c.lanes;
-    const int rows = rec_waves(bwd) * (64 / c.lanes) * rec_rows(bwd);
-    c.ntiles = (p.N + rows - 1) / rows;
-    c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * c.lanes * w : 0;
-    c.bytes = (c.slots * 12 + 15) / 16 * 16;
+    c.nblocks = (cols + kLanes - 1) / kLanes;
+    if (p.N <= kShort || (p.N <= 128 && cols >= kManyColumns)) c.waves = 0;
+    else if (p.N <= 64) c.waves = 1;
+    else if (p.N <= 128) c.waves = 2;
+    else c.waves = c.nblocks <= kFewBlocks && p.N > kLong ? 8 : 4;
+    const int rows = std::max(c.waves, 1) * (64 / kLanes) * thread_rows(c.waves, bwd);
+    c.ntiles = c.waves ? (p.N + rows - 1) / rows : 1;
+    c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * kLanes * w : 0;
+    c.counters = (size_t)kGroups * kTicketStride * sizeof(unsigned);
+    c.bytes = c.counters + (c.slots * 12 + 15) / 16 * 16;
     return c;
 }
-template <typename T, bool C, bool BWD, int LANES>
+template <typename T, bool C, bool BWD, int WAVES>
 void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t s) {
     char *base = (char *)a.scratch;
-    RecLook lk{(unsigned *)base, (unsigned long long *)(base + 256), (unsigned *)(base + 256 + c.slots * 8)};
+    RecLook lk{(unsigned *)base, (unsigned long long *)(base + c.counters), (unsigned *)(base + c.counters + c.slots * 8)};
     if (c.ntiles > 1) {
-        const size_t n = (256 + c.bytes) / 16;
-        k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, n);
+        const size_t n = c.bytes / 16;
+        k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, c.counters / 16, n);
     }
-    const int cols = p.B * (p.D / Piece<T>::W);
-    k_rec_tiles<T, C, BWD, LANES, rec_waves(BWD), rec_rows(BWD)><<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * rec_waves(BWD)), 0, s>>>(
+    k_rec_tiles<T, C, BWD, WAVES, thread_rows(WAVES, BWD)><<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * WAVES), 0, s>>>(
         (const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, BWD ? a.dh_out : a.h_in, a.len, (T *)a.out, (T *)a.dx,
-        (T *)a.dlog_a, BWD ? a.dh_in : a.h_out, lk, cols, p.N, p.D, p.ld, c.ntiles, c.nblocks);
+        (T *)a.dlog_a, BWD ? a.dh_in : a.h_out, lk, p.B * (p.D / Piece<T>::W), p.N, p.D, p.ld, c.ntiles, c.nblocks);
 }
 template <typename T, bool C, bool BWD>
 hipError_t rec(const RecPlan &p, const RecArgs &a, hipStream_t s) {
     const RecCut c = rec_cut(p, BWD);
     const int cols = p.B * (p.D / Piece<T>::W);
     const dim3 grid((cols + kStepThreads - 1) / kStepThreads), block(kStepThreads);
-    if (c.tiles) {
-        if (c.lanes == 64) rec_tiles<T, C, BWD, 64>(p, a, c, s);
-        else if (c.lanes == 32) rec_tiles<T, C, BWD, 32>(p, a, c, s);
-        else if (c.lanes == 16) rec_tiles<T, C, BWD, 16>(p, a, c, s);
-        else rec_tiles<T, C, BWD, 8>(p, a, c, s);
-    } else if constexpr (BWD) {
-        k_rec_step_bwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, a.dh_out,
-                                                    a.len, (T *)a.dx, (T *)a.dlog_a, a.dh_in, cols, p.N, p.D, p.ld);
-    } else {
-        k_rec_step_fwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, a.h_in, a.len, (T *)a.out, a.h_out, cols, p.N, p.D, p.ld);
+    switch (c.waves) {
+        case 1: rec_tiles<T, C, BWD, 1>(p, a, c, s); break;
+        case 2: rec_tiles<T, C, BWD, 2>(p, a, c, s); break;
+        case 4: rec_tiles<T, C, BWD, 4>(p, a, c, s); break;
+        case 8: rec_tiles<T, C, BWD, 8>(p, a, c, s); break;
+        default:
+            if constexpr (BWD)
+                k_rec_step_bwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in,
+                                                            a.dh_out, a.len, (T *)a.dx, (T *)a.dlog_a, a.dh_in, cols, p.N, p.D, p.ld);
+            else
+                k_rec_step_fwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, a.h_in, a.len, (T *)a.out, a.h_out, cols, p.N, p.D, p.ld);
     }
     return hipGetLastError();
 }
@@ -489,7 +497,7 @@ hipError_t by_type(const RecPlan &p, const RecArgs &a, hipStream_t s) {
 }
 }  // namespace
 
-size_t rec_scratch(const RecPlan &p) { return 256 + std::max(rec_cut(p, false).bytes, rec_cut(p, true).bytes); }
+size_t rec_scratch(const RecPlan &p) { return std::max(rec_cut(p, false).bytes, rec_cut(p, true).bytes); }
 hipError_t launch_rec_fwd(const RecPlan &p, const RecArgs &a, hipStream_t s) { return by_type<false>(p, a, s); }
 hipError_t launch_rec_bwd(const RecPlan &p, const RecArgs &a, hipStream_t s) { return by_type<true>(p, a, s); }
 
