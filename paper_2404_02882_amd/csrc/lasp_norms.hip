@@ -25,12 +25,13 @@ DEVI void row_sums(float (&v)[K], float *lds) {
     for (int d = LANES < 64 ? LANES / 2 : 32; d > 0; d >>= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
-    if constexpr (LANES > 64) {   // a row has the workgroup to itself
+    if constexpr (LANES > 64) {   // over the waves of the row
         constexpr int WAVES = LANES / 64;
-        __syncthreads();          // the sums of the row before have been read
+        lds += threadIdx.x / LANES * (K * WAVES);
+        __syncthreads();          // the sums of the turn before have been read
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < K; ++k) lds[k * WAVES + (threadIdx.x >> 6)] = v[k];
+            for (int k = 0; k < K; ++k) lds[k * WAVES + (threadIdx.x % LANES >> 6)] = v[k];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -132,7 +133,7 @@ DEVI void write_partial(const Mine<T, LANES, PIECES> &my, const float (&acc)[PIE
 // ---------------------------------------------------------------------------
 // Before a block.
 // ---------------------------------------------------------------------------
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool STREAM>
 __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_fwd(const T *r, const T *__restrict__ x, const float *__restrict__ scale,
                                                                   const float *__restrict__ weight, float eps, T *r_out,
                                                                   T *__restrict__ y, int rows, int C) {
@@ -148,8 +149,8 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_fwd(const T *r, co
         u32x4 vr[PIECES], vx[PIECES];
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            vr[k] = *(const u32x4 *)(r + base + my.at(k));
-            if (x) vx[k] = *(const u32x4 *)(x + base + my.at(k));
+            vr[k] = gload<u32x4, STREAM>(r + base + my.at(k), 0);
+            if (x) vx[k] = gload<u32x4, STREAM>(x + base + my.at(k), 0);
         }
         float f[PIECES][W], sums[1] = {0.0f};
 #pragma unroll
@@ -172,17 +173,17 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_fwd(const T *r, co
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
                 if (my.has(k)) {
-                    if (r_out) *(u32x4 *)(r_out + base + my.at(k)) = P::pack(f[k]);
+                    if (r_out) put<STREAM>(r_out + base + my.at(k), P::pack(f[k]));
                     float o[W], w[W];
                     ws.get(k, my.at(k), w);
 #pragma unroll
                     for (int i = 0; i < W; ++i) o[i] = f[k][i] * rstd * w[i];
-                    *(u32x4 *)(y + base + my.at(k)) = P::pack(o);
+                    put<STREAM>(y + base + my.at(k), P::pack(o));
                 }
     }
 }
 
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool STREAM>
 __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_bwd(const T *__restrict__ r, const T *__restrict__ x,
                                                                   const float *__restrict__ scale, const float *__restrict__ weight,
                                                                   float eps, const T *__restrict__ dy, const T *dr_out, T *dr,
@@ -190,6 +191,7 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_bwd(const T *__res
                                                                   int rows, int C) {
     using P = Piece<T>;
     constexpr int W = P::W, ROWS = Group<LANES>::ROWS;
+    constexpr bool LATE = LANES == 1024;   // (128 registers a thread: what the sums do not need is loaded behind them)
     __shared__ float lds[2 * Group<LANES>::NT / 64];
     __shared__ __attribute__((aligned(16))) float part[ROWS > 1 ? LANES * PIECES * W : 4];
     const Mine<T, LANES, PIECES> my(C);
@@ -203,10 +205,12 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_bwd(const T *__res
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
             const size_t at = base + my.at(k);
-            vr[k] = *(const u32x4 *)(r + at);
-            vy[k] = *(const u32x4 *)(dy + at);
-            if (ps) vx[k] = *(const u32x4 *)(x + at);
-            if (dr_out) vd[k] = *(const u32x4 *)(dr_out + at);
+            vr[k] = gload<u32x4, STREAM>(r + at, 0);
+            vy[k] = gload<u32x4, STREAM>(dy + at, 0);
+            if constexpr (!LATE) {
+                if (ps) vx[k] = gload<u32x4, STREAM>(x + at, 0);
+                if (dr_out) vd[k] = gload<u32x4, STREAM>(dr_out + at, 0);
+            }
         }
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -229,6 +233,10 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_bwd(const T *__res
             for (int k = 0; k < PIECES; ++k)
                 if (my.has(k)) {
                     float f[W], g[W], d[W], o[W], w[W], sc[W];
+                    if constexpr (LATE) {
+                        if (ps) vx[k] = gload<u32x4, STREAM>(x + base + my.at(k), 0);
+                        if (dr_out) vd[k] = gload<u32x4, STREAM>(dr_out + base + my.at(k), 0);
+                    }
                     P::unpack(vr[k], f);
                     P::unpack(vy[k], g);
                     ws.get(k, my.at(k), w);
@@ -243,8 +251,8 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_addnorm_bwd(const T *__res
                         aw[k][i] = __builtin_fmaf(g[i] * f[i], rstd, aw[k][i]);
                         o[i] = sc[i] * d[i];
                     }
-                    *(u32x4 *)(dr + base + my.at(k)) = P::pack(d);
-                    if (dx) *(u32x4 *)(dx + base + my.at(k)) = P::pack(o);
+                    put<STREAM>(dr + base + my.at(k), P::pack(d));
+                    if (dx) put<STREAM>(dx + base + my.at(k), P::pack(o));
                     if (ps) {
                         P::unpack(vx[k], f);
 #pragma unroll
@@ -295,7 +303,7 @@ struct GatePlace {
     }
 };
 
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool STREAM>
 __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_fwd(const T *__restrict__ O, const T *__restrict__ U,
                                                                const float *__restrict__ weight, float eps, T *__restrict__ Y, int gate,
                                                                int tokens, int per, int C, int H, int N, int D, long long ld) {
@@ -316,8 +324,8 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_fwd(const T *__restri
         u32x4 vo[PIECES], vu[PIECES];
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            vo[k] = *(const u32x4 *)(o + at.o[k]);
-            if (gate) vu[k] = *(const u32x4 *)(U + tok * ld + at.t[k]);
+            vo[k] = gload<u32x4, STREAM>(o + at.o[k], 0);
+            if (gate) vu[k] = gload<u32x4, STREAM>(U + tok * ld + at.t[k], 0);
         }
         float f[PIECES][W], sums[1] = {0.0f};
 #pragma unroll
@@ -345,12 +353,12 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_fwd(const T *__restri
                             f[k][i] *= act;
                         }
                     }
-                    *(u32x4 *)(Y + tok * wide + at.t[k]) = P::pack(f[k]);
+                    put<STREAM>(Y + tok * wide + at.t[k], P::pack(f[k]));
                 }
     }
 }
 
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool STREAM>
 __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_bwd(const T *__restrict__ O, const T *__restrict__ U,
                                                                const float *__restrict__ weight, float eps, const T *__restrict__ dY,
                                                                T *__restrict__ dO, T *__restrict__ dU, float *__restrict__ pw, int gate,
@@ -372,9 +380,9 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_bwd(const T *__restri
         u32x4 vo[PIECES], vu[PIECES], vy[PIECES];
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            vo[k] = *(const u32x4 *)(O + head0 + at.o[k]);
-            vy[k] = *(const u32x4 *)(dY + tok * wide + at.t[k]);
-            if (gate) vu[k] = *(const u32x4 *)(U + tok * ld + at.t[k]);
+            vo[k] = gload<u32x4, STREAM>(O + head0 + at.o[k], 0);
+            vy[k] = gload<u32x4, STREAM>(dY + tok * wide + at.t[k], 0);
+            if (gate) vu[k] = gload<u32x4, STREAM>(U + tok * ld + at.t[k], 0);
         }
         float sums[2] = {0.0f, 0.0f};
         float g[PIECES][W], du[PIECES][W];   // dy act(u), dy weight act'(u)
@@ -415,11 +423,11 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_bwd(const T *__restri
                         d[i] = rstd * (w[i] * g[k][i] - f[i] * c);
                         aw[k][i] = __builtin_fmaf(g[k][i] * f[i], rstd, aw[k][i]);
                     }
-                    *(u32x4 *)(dO + head0 + at.o[k]) = P::pack(d);
+                    put<STREAM>(dO + head0 + at.o[k], P::pack(d));
                     if (gate) {
 #pragma unroll
                         for (int i = 0; i < W; ++i) d[i] = du[k][i] * f[i] * rstd;
-                        *(u32x4 *)(dU + tok * ld + at.t[k]) = P::pack(d);
+                        put<STREAM>(dU + tok * ld + at.t[k], P::pack(d));
                     }
                 }
     }
@@ -434,10 +442,10 @@ __global__ __launch_bounds__(Group<LANES>::NT) void k_gate_bwd(const T *__restri
 }
 
 // ---------------------------------------------------------------------------
-// k_column_sums: out[c] = part[0][c] + part[1][c] + ..., blockIdx.y one of two such sums. A workgroup takes 64 columns, 64
-// threads by 16 groups of rows; fixed order.
+// k_column_sums: out[c] = part[0][c] + part[1][c] + ..., blockIdx.y one of two such sums. A workgroup takes 32 columns, eight
+// threads by 32 groups of rows; fixed order.
 // ---------------------------------------------------------------------------
-constexpr int kSumColumns = 64, kSumGroups = 16;
+constexpr int kSumColumns = 32, kSumGroups = 32;
 __global__ __launch_bounds__(kSumColumns * kSumGroups / 4) void k_column_sums(const float *__restrict__ part0, float *__restrict__ out0,
                                                                               const float *__restrict__ part1, float *__restrict__ out1,
                                                                               int n, int C) {
@@ -448,7 +456,7 @@ __global__ __launch_bounds__(kSumColumns * kSumGroups / 4) void k_column_sums(co
     const int c = blockIdx.x * kSumColumns + 4 * c4;
     f32x4 sum{0, 0, 0, 0};
     if (c < C)
-#pragma unroll 4
+#pragma unroll 8
         for (int r = g; r < n; r += kSumGroups) sum += *(const f32x4 *)(part + (size_t)r * C + c);
     lds[g][c4] = sum;
     __syncthreads();
@@ -460,33 +468,41 @@ __global__ __launch_bounds__(kSumColumns * kSumGroups / 4) void k_column_sums(co
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+// A row over as many threads as it has pieces, up to 256; a wave with four pieces a thread needs no barrier, but keeps fewer rows on
+// their way (addnorm bfloat16 32768 x 2048, a wave / four: forward 91 / 90 us, backward 143 / 132; float 20011 x 1000 forward 62.5 / 57.4). Wider rows in
+// two and four pieces (16384 x 4096 backward, 256 threads / 512 148 / 151 us; 8192 x 8192, 256 / 512 / 1024 148 / 156 / 174; 4096 x 16384, 512 / 1024 182 / 204).
 RowPlan row_plan(int tokens, int heads, int C, int dtype) {
     RowPlan p{tokens, heads, C, dtype, 64, 1};
     const int n = C / (dtype == 0 ? 4 : 8);
-    if (n <= 8) p.lanes = 8;
-    else if (n <= 16) p.lanes = 16;
-    else if (n <= 32) p.lanes = 32;
-    else if (n > 1024) p.lanes = 1024;
-    else if (n > 256) p.lanes = 256;
+    p.lanes = 8;
+    while (p.lanes < n && p.lanes < 256) p.lanes *= 2;
+    if (n > 1024) p.lanes = n <= 2048 ? 512 : 1024;
     p.pieces = n <= p.lanes ? 1 : n <= 2 * p.lanes ? 2 : 4;
     return p;
 }
 namespace {
-#ifndef WGF
-#define WGF 1024
-#define WGB 512
-#endif
-constexpr int kWorkgroups = WGB;
+constexpr int kCus = 256, kForward = 4 * kCus;
 int rows_at_a_time(const RowPlan &p) { return std::max(p.lanes, 256) / p.lanes; }
 // Workgroups: no more than there are rows for, and (rows that are heads) at least one row group for every head of a token.
 int workgroups(const RowPlan &p, int most) {
     const long long rows = (long long)p.tokens * p.heads, at = rows_at_a_time(p);
     return (int)std::max<long long>(std::min<long long>((rows + at - 1) / at, most), (p.heads + at - 1) / at);
 }
-int partial_rows(const RowPlan &p) {   // of a backward pass
-    const int n = workgroups(p, kWorkgroups);
+// Workgroups of a backward pass that reads `loads` tensors. Rows of one piece a thread: as many on a CU (every CU the same) as keep
+// about the same number of bytes on their way, and no more, since each writes a partial row (addnorm bfloat16 32768 x 2048, four tensors
+// read, 512 / 576 / 768 / 1024 workgroups: 132 / 148 / 144 / 153 us; three: 109 / - / 92 / 97; float 65536 x 1024, four: 324 / - / 270 / 277). Small calls:
+// four turns or more each (8192 x 512 16.3 -> 14.8). Rows of more pieces have enough with two.
+int backward_workgroups(const RowPlan &p, int loads) {
+    if (p.pieces > 1) return workgroups(p, 2 * kCus);
+    const long long turns = ((long long)p.tokens * p.heads + rows_at_a_time(p) - 1) / rows_at_a_time(p);
+    return workgroups(p, (int)std::max<long long>(std::min<long long>(((p.dtype == 0 ? 7 : 6) - loads) * kCus, turns / 4), kCus));
+}
+// A partial row of the weights' gradients for every workgroup (rows that are tokens), or for every token of a turn.
+int partial_rows(const RowPlan &p, int loads) {
+    const int n = backward_workgroups(p, loads);
     return p.heads == 1 ? n : (int)((long long)n * rows_at_a_time(p) / p.heads);
 }
+constexpr int kLeastLoads = 2;   // (o or r, and dy)
 hipError_t column_sums(const float *p0, float *o0, const float *p1, float *o1, int n, int C, hipStream_t s) {
     if (!o0) {
         p0 = p1;
@@ -496,33 +512,34 @@ hipError_t column_sums(const float *p0, float *o0, const float *p1, float *o1, i
     if (o0) k_column_sums<<<dim3((C + kSumColumns - 1) / kSumColumns, o1 ? 2 : 1), dim3(kSumColumns * kSumGroups / 4), 0, s>>>(p0, o0, p1, o1, n, C);
     return hipGetLastError();
 }
-// f.template operator()<T, LANES, PIECES>() for the plan's.
-template <typename T, typename F>
+// f.template operator()<T, LANES, PIECES, STREAM>() for the plan's.
+template <typename T, bool STREAM, typename F>
 void by_lanes(const RowPlan &p, F f) {
-    switch (p.lanes) {
-        case 8: return f.template operator()<T, 8, 1>();
-        case 16: return f.template operator()<T, 16, 1>();
-        case 32: return f.template operator()<T, 32, 1>();
-        case 64: return p.pieces == 1 ? f.template operator()<T, 64, 1>() : p.pieces == 2 ? f.template operator()<T, 64, 2>() : f.template operator()<T, 64, 4>();
-        case 256: return p.pieces == 2 ? f.template operator()<T, 256, 2>() : f.template operator()<T, 256, 4>();
+    const int key = p.lanes * 8 + p.pieces;
+    switch (key) {
+#define LASP_ROWS(LANES, PIECES) \
+    case LANES * 8 + PIECES: return f.template operator()<T, LANES, PIECES, STREAM>();
+        LASP_ROWS(8, 1) LASP_ROWS(16, 1) LASP_ROWS(32, 1) LASP_ROWS(64, 1) LASP_ROWS(128, 1) LASP_ROWS(256, 1)
+        LASP_ROWS(256, 2) LASP_ROWS(256, 4) LASP_ROWS(512, 4)
+#undef LASP_ROWS
         default:
-            if constexpr (sizeof(T) == 4)
-                if (p.pieces == 4) return f.template operator()<T, 1024, 4>();
-            return f.template operator()<T, 1024, 2>();
+            if constexpr (sizeof(T) == 4) return f.template operator()<T, 1024, 4, STREAM>();   // (two-byte rows have 2048 pieces at most)
     }
 }
+// tensors: of the rows' size that the call reads and writes
 template <typename F>
-void by_plan(const RowPlan &p, F f) {
-    if (p.dtype == 0) by_lanes<float>(p, f);
-    else by_lanes<bf16_t>(p, f);
+void by_plan(const RowPlan &p, int tensors, F f) {
+    const bool stream = past_cache((size_t)tensors * p.tokens * p.heads * p.C * (p.dtype == 0 ? 4 : 2));
+    if (p.dtype == 0) stream ? by_lanes<float, true>(p, f) : by_lanes<float, false>(p, f);
+    else stream ? by_lanes<bf16_t, true>(p, f) : by_lanes<bf16_t, false>(p, f);
 }
 struct AddNormFwd {
     const RowPlan &p;
     const AddNormArgs &a;
     hipStream_t s;
-    template <typename T, int LANES, int PIECES>
+    template <typename T, int LANES, int PIECES, bool STREAM>
     void operator()() const {
-        k_addnorm_fwd<T, LANES, PIECES><<<dim3(workgroups(p, WGF)), dim3(Group<LANES>::NT), 0, s>>>(
+        k_addnorm_fwd<T, LANES, PIECES, STREAM><<<dim3(workgroups(p, kForward)), dim3(Group<LANES>::NT), 0, s>>>(
             (const T *)a.r, (const T *)a.x, a.scale, a.weight, a.eps, (T *)a.r_out, (T *)a.y, p.tokens, p.C);
     }
 };
@@ -530,10 +547,10 @@ struct AddNormBwd {
     const RowPlan &p;
     const AddNormArgs &a;
     hipStream_t s;
-    template <typename T, int LANES, int PIECES>
+    template <typename T, int LANES, int PIECES, bool STREAM>
     void operator()() const {
-        const int n = workgroups(p, kWorkgroups);
-        k_addnorm_bwd<T, LANES, PIECES><<<dim3(n), dim3(Group<LANES>::NT), 0, s>>>(
+        const int n = backward_workgroups(p, a.loads());
+        k_addnorm_bwd<T, LANES, PIECES, STREAM><<<dim3(n), dim3(Group<LANES>::NT), 0, s>>>(
             (const T *)a.r, (const T *)a.x, a.scale, a.weight, a.eps, (const T *)a.dy, (const T *)a.dr_out, (T *)a.dr, (T *)a.dx,
             a.dweight ? a.scratch : nullptr, a.dscale ? a.scratch + (size_t)n * p.C : nullptr, p.tokens, p.C);
     }
@@ -542,9 +559,9 @@ struct GateFwd {
     const RowPlan &p;
     const GateArgs &a;
     hipStream_t s;
-    template <typename T, int LANES, int PIECES>
+    template <typename T, int LANES, int PIECES, bool STREAM>
     void operator()() const {
-        k_gate_fwd<T, LANES, PIECES><<<dim3(workgroups(p, WGF)), dim3(Group<LANES>::NT), 0, s>>>(
+        k_gate_fwd<T, LANES, PIECES, STREAM><<<dim3(workgroups(p, kForward)), dim3(Group<LANES>::NT), 0, s>>>(
             (const T *)a.o, (const T *)a.u, a.weight, a.eps, (T *)a.y, a.gate, p.tokens, p.heads, p.C, a.H, a.N, a.D, a.ld);
     }
 };
@@ -552,34 +569,34 @@ struct GateBwd {
     const RowPlan &p;
     const GateArgs &a;
     hipStream_t s;
-    template <typename T, int LANES, int PIECES>
+    template <typename T, int LANES, int PIECES, bool STREAM>
     void operator()() const {
-        k_gate_bwd<T, LANES, PIECES><<<dim3(workgroups(p, kWorkgroups)), dim3(Group<LANES>::NT), 0, s>>>(
+        k_gate_bwd<T, LANES, PIECES, STREAM><<<dim3(backward_workgroups(p, a.loads())), dim3(Group<LANES>::NT), 0, s>>>(
             (const T *)a.o, (const T *)a.u, a.weight, a.eps, (const T *)a.dy, (T *)a.d_o, (T *)a.du, a.dweight ? a.scratch : nullptr,
             a.gate, p.tokens, p.heads, p.C, a.H, a.N, a.D, a.ld);
     }
 };
 }  // namespace
 
-size_t addnorm_scratch(const RowPlan &p) { return 2 * (size_t)partial_rows(p) * p.C * sizeof(float); }
-size_t gatenorm_scratch(const RowPlan &p) { return (size_t)partial_rows(p) * p.heads * p.C * sizeof(float); }
+size_t addnorm_scratch(const RowPlan &p) { return 2 * (size_t)partial_rows(p, kLeastLoads) * p.C * sizeof(float); }
+size_t gatenorm_scratch(const RowPlan &p) { return (size_t)partial_rows(p, kLeastLoads) * p.heads * p.C * sizeof(float); }
 
 hipError_t launch_addnorm_fwd(const RowPlan &p, const AddNormArgs &a, hipStream_t s) {
-    by_plan(p, AddNormFwd{p, a, s});
+    by_plan(p, a.x ? 4 : 2, AddNormFwd{p, a, s});
     return hipGetLastError();
 }
 hipError_t launch_addnorm_bwd(const RowPlan &p, const AddNormArgs &a, hipStream_t s) {
-    by_plan(p, AddNormBwd{p, a, s});
-    const int n = partial_rows(p);
+    by_plan(p, 3 + !!a.dscale + !!a.dr_out + !!a.dx, AddNormBwd{p, a, s});
+    const int n = partial_rows(p, a.loads());
     return column_sums(a.scratch, a.dweight, a.scratch + (size_t)n * p.C, a.dscale, n, p.C, s);
 }
 hipError_t launch_gatenorm_fwd(const RowPlan &p, const GateArgs &a, hipStream_t s) {
-    by_plan(p, GateFwd{p, a, s});
+    by_plan(p, 2 + !!a.gate, GateFwd{p, a, s});
     return hipGetLastError();
 }
 hipError_t launch_gatenorm_bwd(const RowPlan &p, const GateArgs &a, hipStream_t s) {
-    by_plan(p, GateBwd{p, a, s});
-    return column_sums(a.scratch, a.dweight, nullptr, nullptr, partial_rows(p), p.heads * p.C, s);
+    by_plan(p, 3 + 2 * !!a.gate, GateBwd{p, a, s});
+    return column_sums(a.scratch, a.dweight, nullptr, nullptr, partial_rows(p, a.loads()), p.heads * p.C, s);
 }
 
 }  // namespace lasp

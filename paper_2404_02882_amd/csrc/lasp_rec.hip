@@ -236,7 +236,7 @@ DEVI float entering(const RecLook &lk, int tile, size_t slot, size_t stride) {
 // the fewer columns, the longer the tile and the fewer there are to pass the state on through (bfloat16 32768 x 2048, tiles of
 // 4 waves, 64 / 16 / 8 lanes: forward 214 / 92 / 88 us, backward 216 / 137 / 134).
 constexpr int kLanes = 8, kBack = 8;
-template <typename T, bool COUPLED, bool BWD, int WAVES, int ROWS>
+template <typename T, bool COUPLED, bool BWD, int WAVES, int ROWS, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_tiles(const T *__restrict__ X, const T *__restrict__ L, const T *__restrict__ out_in,
                                                          const T *__restrict__ dout, const float *h_in, const float *enter,
                                                          const int *__restrict__ len, T *__restrict__ out, T *__restrict__ dx,
@@ -277,16 +277,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
     auto load_all = [&](auto token) {   // of row r, one that exists
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            vl[r] = *(const u32x4 *)(L + pbase + token(r) * ld);
-            if constexpr (BWD) vu[r] = *(const u32x4 *)(dout + tbase + token(r) * D);
-            else vu[r] = *(const u32x4 *)(X + pbase + token(r) * ld);
+            vl[r] = gload<u32x4, STREAM>(L + pbase + token(r) * ld, 0);
+            if constexpr (BWD) vu[r] = gload<u32x4, STREAM>(dout + tbase + token(r) * D, 0);
+            else vu[r] = gload<u32x4, STREAM>(X + pbase + token(r) * ld, 0);
         }
         if constexpr (BWD)
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
                 const long long t = token(r);
-                vo[r] = *(const u32x4 *)(out_in + tbase + (t > 0 ? t - 1 : 0) * D);
-                if constexpr (COUPLED) vx[r] = *(const u32x4 *)(X + pbase + t * ld);
+                vo[r] = gload<u32x4, STREAM>(out_in + tbase + (t > 0 ? t - 1 : 0) * D, 0);
+                if constexpr (COUPLED) vx[r] = gload<u32x4, STREAM>(X + pbase + t * ld, 0);
             }
     };
     if (whole) {
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
                 y[i] = g.step(y[i], COUPLED ? g.b() * fu[i] : fu[i]);
             }
             if (mine && (whole || at(r) < N))
-                *(u32x4 *)(out + tbase + at(r) * D) = whole || there(r) ? P::pack(y) : u32x4{0, 0, 0, 0};
+                put<STREAM>(out + tbase + at(r) * D, whole || there(r) ? P::pack(y) : u32x4{0, 0, 0, 0});
         } else {
             float fo[W], fx[W], ox[W], ol[W];
             P::unpack(vo[r], fo);
@@ -413,8 +413,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
             }
             if (mine && (whole || at(r) >= 0)) {
                 const size_t to = pbase + at(r) * ld;
-                *(u32x4 *)(dx + to) = whole || there(r) ? P::pack(ox) : u32x4{0, 0, 0, 0};
-                *(u32x4 *)(dl + to) = whole || there(r) ? P::pack(ol) : u32x4{0, 0, 0, 0};
+                put<STREAM>(dx + to, whole || there(r) ? P::pack(ox) : u32x4{0, 0, 0, 0});
+                put<STREAM>(dl + to, whole || there(r) ? P::pack(ol) : u32x4{0, 0, 0, 0});
             }
         }
     }
@@ -467,7 +467,9 @@ void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t 
         const size_t n = c.bytes / 16;
         k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, c.counters / 16, n);
     }
-    k_rec_tiles<T, C, BWD, WAVES, thread_rows(WAVES, BWD)><<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * WAVES), 0, s>>>(
+    const size_t bytes = (size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T);
+    const auto kernel = past_cache(bytes) ? k_rec_tiles<T, C, BWD, WAVES, thread_rows(WAVES, BWD), true> : k_rec_tiles<T, C, BWD, WAVES, thread_rows(WAVES, BWD), false>;
+    kernel<<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * WAVES), 0, s>>>(
         (const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, BWD ? a.dh_out : a.h_in, a.len, (T *)a.out, (T *)a.dx,
         (T *)a.dlog_a, BWD ? a.dh_in : a.h_out, lk, p.B * (p.D / Piece<T>::W), p.N, p.D, p.ld, c.ntiles, c.nblocks);
 }
