@@ -196,10 +196,11 @@ DEVI V look(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_ME
 template <typename V>
 DEVI void show(V *p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// The state behind tile `tile` - 1 for one channel, whose slots in consecutive tiles are `stride` apart, `slot` that of `tile`.
+// The state that enters a tile for one channel, whose slots in consecutive tiles are `stride` apart, `slot` that of this one. The
+// channel's first tile, `back` tiles in front, publishes no step, and nothing in front of it is looked at.
 template <typename T, int BACK>
-DEVI float entering(const RecLook &lk, int tile, size_t slot, size_t stride) {
-    auto at = [&](int k) { return slot - (size_t)min(k + 1, tile) * stride; };
+DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
+    auto at = [&](int k) { return slot - (size_t)min(k + 1, back) * stride; };
     unsigned long long step[BACK];
 #pragma unroll
     for (int k = 0; k < BACK; ++k) step[k] = look(lk.steps + at(k));
@@ -270,7 +271,21 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
     auto at = [&](int r) { return first + dir * r; };
     auto there = [&](int r) { return at(r) >= 0 && at(r) < c.n; };
     const bool whole = __all(there(0) && there(ROWS - 1));
-    const bool none = !BWD && __all(first >= c.n);   // behind every sequence's last token: nothing to load, the state stays
+    // A tile behind the last tokens of all its sequences (every wave has the same columns): zeros, and nobody waits for it.
+    constexpr int TOKENS = WAVES * PARTS * ROWS;
+    if (len && (BWD ? tile + 1 < ntiles : tile > 0) && __all((BWD ? N - (long long)(tile + 1) * TOKENS : (long long)tile * TOKENS) >= c.n)) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            if (mine && at(r) < N) {
+                if constexpr (BWD) {
+                    put<STREAM>(dx + pbase + at(r) * ld, u32x4{0, 0, 0, 0});
+                    put<STREAM>(dl + pbase + at(r) * ld, u32x4{0, 0, 0, 0});
+                } else {
+                    put<STREAM>(out + tbase + at(r) * D, u32x4{0, 0, 0, 0});
+                }
+            }
+        return;
+    }
 
     u32x4 vu[ROWS], vl[ROWS];   // x, or the gradient of out
     [[maybe_unused]] u32x4 vo[BWD ? ROWS : 1], vx[BWD && COUPLED ? ROWS : 1];
@@ -291,9 +306,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
     };
     if (whole) {
         load_all(at);
-    } else if (none) {
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) vl[r] = vu[r] = u32x4{0, 0, 0, 0};
     } else {
         load_all([&](int r) { return min(max(at(r), 0ll), (long long)max(c.n - 1, 0)); });
 #pragma unroll
@@ -350,15 +362,24 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
             gate[i] = g.w;
         }
         const Gate<T> whole_tile(tl);
-        if (tile == 0) {
+        // The channel's tiles, from that of its sequence's first token in the order of the scan to that of its last.
+        int begin = 0, last = ntiles - 1;
+        if (len) {
+            const Column<T> cc(min(block * LANES + ch / W, cols - 1), N, D, len);
+            if constexpr (BWD) begin = cc.n > 0 ? (N - cc.n) / TOKENS : last;
+            else last = cc.n > 0 ? (cc.n - 1) / TOKENS : 0;
+        }
+        if (tile < begin || tile > last) {
+            y = 0.0f;   // none of its tokens here: nothing uses the state, and nobody waits for it
+        } else if (tile == begin) {
             y = enter && state < nstate ? enter[state] : 0.0f;
         } else {
-            if (tile + 1 < ntiles) show(lk.steps + slot, (unsigned long long)published(whole_tile.w) | (unsigned long long)published(tx) << 32);
-            y = entering<T, kBack>(lk, tile, slot, stride);
+            if (tile < last) show(lk.steps + slot, (unsigned long long)published(whole_tile.w) | (unsigned long long)published(tx) << 32);
+            y = entering<T, kBack>(lk, tile - begin, slot, stride);
         }
         const float end = whole_tile.step(y, tx);   // (as the tiles behind form it)
-        if (tile + 1 < ntiles) show(lk.ends + slot, published(end));
-        else if (leave && state < nstate) leave[state] = end;
+        if (begin <= tile && tile < last) show(lk.ends + slot, published(end));
+        if (tile == last && leave && state < nstate) leave[state] = end;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) {
             const float x = sX[i][ch];

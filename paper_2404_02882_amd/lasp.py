@@ -488,128 +488,122 @@ def gatenorm_scratch_bytes(shape: GateShape) -> int:
     return int(lib.lasp_gatenorm_scratch_bytes(ctypes.byref(shape)))
 
 
-class _Args:
-    """Addresses of a call's tensors, each checked for type, size, layout and device (these calls take no shape but the
-    plan's, so that a tensor of another one would be read past its end)."""
+def _refuse(t, name, numel, dtype, at):
+    if t.get_device() < 0:
+        raise ValueError(f"{name}: must be on a GPU")
+    if t.get_device() != at:
+        raise ValueError(f"{name}: on device {t.get_device()}, other tensors of the call on {at}")
+    raise ValueError(f"{name}: must be contiguous, {numel} elements of {dtype}, not {tuple(t.shape)} of {t.dtype}")
 
-    __slots__ = ("device", "dtype")
 
-    def __init__(self, dtype):
-        self.device, self.dtype = None, _TORCH.get(dtype)
+def _addr(t, name, numel, dtype, at):
+    """The address of a contiguous tensor of `numel` elements on device `at` (None passes). These calls take no sizes but the
+    plan's: a tensor of another one would be read past its end. (Five look-ups, 0.6 us.)"""
+    if t is None:
+        return None
+    if t.numel() != numel or t.dtype is not dtype or t.get_device() != at or at < 0 or not t.is_contiguous():
+        _refuse(t, name, numel, dtype, at)
+    return t.data_ptr()
 
-    def _placed(self, t, name):
-        if not t.is_cuda:
-            raise ValueError(f"{name}: must be on a GPU")
-        at = t.get_device()
-        if self.device is None:
-            self.device = at
-        elif at != self.device:
-            raise ValueError(f"{name}: on device {at}, other tensors of the call on {self.device}")
-        return t.data_ptr()
 
-    def of(self, t, name, numel, dtype=None):
-        """A contiguous tensor of `numel` elements (None passes)."""
-        if t is None:
-            return None
-        dtype = dtype or self.dtype
-        if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
-            raise ValueError(f"{name}: must be contiguous, {numel} elements of {dtype}, not {tuple(t.shape)} of {t.dtype}")
-        return self._placed(t, name)
+def _addr_rows(t, name, B, N, width, ld, dtype, at):
+    """The same of [B][N] rows of `width` elements, `ld` from row to row (0 = width)."""
+    if t is None or ld == 0 or ld == width:
+        return _addr(t, name, B * N * width, dtype, at)
+    if t.get_device() != at or at < 0 or t.dtype is not dtype:
+        _refuse(t, name, B * N * width, dtype, at)
+    if t.shape != (B, N, width) or (width > 1 and t.stride(2) != 1) or (N > 1 and t.stride(1) != ld) or (B > 1 and t.stride(0) != N * ld):
+        raise ValueError(f"{name}: must be [{B}][{N}][{width}], rows {ld} apart, not {tuple(t.shape)} with strides {t.stride()}")
+    return t.data_ptr()
 
-    def rows(self, t, name, B, N, width, ld):
-        """[B][N] rows of `width` elements, `ld` from row to row (0 = width)."""
-        if t is None:
-            return None
-        ld = ld or width
-        if t.dtype is not self.dtype or t.shape != (B, N, width) or (width > 1 and t.stride(2) != 1) or \
-                (N > 1 and t.stride(1) != ld) or (B > 1 and t.stride(0) != N * ld):
-            raise ValueError(f"{name}: must be [{B}][{N}][{width}] of {self.dtype}, rows {ld} apart, not {tuple(t.shape)} with "
-                             f"strides {t.stride()} of {t.dtype}")
-        return self._placed(t, name)
 
-    def scratch(self, t, name="scratch"):
-        if t is None:
-            return None, 0
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: must be contiguous")
-        return self._placed(t, name), t.numel() * t.element_size()
+def _room(t, at):
+    """Address and size of a workspace."""
+    if t is None:
+        return None, 0
+    n = t.numel()
+    return _addr(t, "scratch", n, t.dtype, at), n * t.element_size()
 
-    def call(self, fn, where, args, stream):
-        """On `stream`, or the current one of the tensors' device."""
-        at = self.device
-        if at is None:                     # a required tensor is missing: the library says which status that is
-            rc = fn(*args, None)
-        elif at == torch.cuda.current_device():
+
+def _call(fn, where, at, stream, *args):
+    """On `stream`, or the current one of the tensors' device."""
+    if at == torch.cuda.current_device():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(at):
             rc = fn(*args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
-        else:
-            with torch.cuda.device(at):
-                rc = fn(*args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
-        if rc != 0:
-            raise LaspError(rc, where)
+    if rc != 0:
+        raise LaspError(rc, where)
+
+
+def _home(t, name, shape, check):
+    """The data type and device of a call: those of the plan and of its first tensor."""
+    dtype = _TORCH.get(shape.dtype)
+    if dtype is None or t is None:
+        raise LaspError(check(shape) or 1, name)
+    return dtype, t.get_device()
 
 
 def lasp_rec_fwd(shape: RecShape, x, log_a, h_in, lens, out, h_out, scratch, stream=None) -> None:
     """h_s = exp(log_a_s) h_{s-1} + b_s x_s per channel: x, log_a [B,N,D] (rows shape.ld apart), out [B,N,D], h_in, h_out float32
     [B,D] or None, lens int32 [B] or None; raises LaspError on a non-zero status."""
-    a, s = _Args(shape.dtype), shape
-    f, n = torch.float32, s.B * s.D
-    args = (ctypes.byref(s), a.rows(x, "x", s.B, s.N, s.D, s.ld), a.rows(log_a, "log_a", s.B, s.N, s.D, s.ld), a.of(h_in, "h_in", n, f),
-            a.of(lens, "lens", s.B, torch.int32), a.of(out, "out", s.N * n), a.of(h_out, "h_out", n, f), *a.scratch(scratch))
-    a.call(lib.lasp_rec_fwd, "lasp_rec_fwd", args, stream)
+    (d, at), f, B, N, D, ld = _home(x, "lasp_rec_fwd", shape, check_rec), torch.float32, shape.B, shape.N, shape.D, shape.ld
+    n = B * D
+    _call(lib.lasp_rec_fwd, "lasp_rec_fwd", at, stream, ctypes.byref(shape), _addr_rows(x, "x", B, N, D, ld, d, at),
+          _addr_rows(log_a, "log_a", B, N, D, ld, d, at), _addr(h_in, "h_in", n, f, at), _addr(lens, "lens", B, torch.int32, at),
+          _addr(out, "out", N * n, d, at), _addr(h_out, "h_out", n, f, at), *_room(scratch, at))
 
 
 def lasp_rec_bwd(shape: RecShape, x, log_a, out, h_in, lens, dout, dh_out, dx, dlog_a, dh_in, scratch, stream=None) -> None:
     """Gradients dx, dlog_a (as x, log_a), dh_in of lasp_rec_fwd, from its `out` (x: needed when coupled); raises LaspError on a
     non-zero status."""
-    a, s = _Args(shape.dtype), shape
-    f, n = torch.float32, s.B * s.D
-    args = (ctypes.byref(s), a.rows(x, "x", s.B, s.N, s.D, s.ld), a.rows(log_a, "log_a", s.B, s.N, s.D, s.ld), a.of(out, "out", s.N * n),
-            a.of(h_in, "h_in", n, f), a.of(lens, "lens", s.B, torch.int32), a.of(dout, "dout", s.N * n), a.of(dh_out, "dh_out", n, f),
-            a.rows(dx, "dx", s.B, s.N, s.D, s.ld), a.rows(dlog_a, "dlog_a", s.B, s.N, s.D, s.ld), a.of(dh_in, "dh_in", n, f),
-            *a.scratch(scratch))
-    a.call(lib.lasp_rec_bwd, "lasp_rec_bwd", args, stream)
+    (d, at), f, B, N, D, ld = _home(log_a, "lasp_rec_bwd", shape, check_rec), torch.float32, shape.B, shape.N, shape.D, shape.ld
+    n = B * D
+    _call(lib.lasp_rec_bwd, "lasp_rec_bwd", at, stream, ctypes.byref(shape), _addr_rows(x, "x", B, N, D, ld, d, at),
+          _addr_rows(log_a, "log_a", B, N, D, ld, d, at), _addr(out, "out", N * n, d, at), _addr(h_in, "h_in", n, f, at),
+          _addr(lens, "lens", B, torch.int32, at), _addr(dout, "dout", N * n, d, at), _addr(dh_out, "dh_out", n, f, at),
+          _addr_rows(dx, "dx", B, N, D, ld, d, at), _addr_rows(dlog_a, "dlog_a", B, N, D, ld, d, at), _addr(dh_in, "dh_in", n, f, at),
+          *_room(scratch, at))
 
 
 def lasp_addnorm_fwd(shape: RowsShape, r, x, scale, weight, eps, r_out, y, stream=None) -> None:
     """r_out = r + scale * x, y = weight * r_out / rms(r_out), rows of C (scale, weight float32 [C] or None; x, r_out None: the norm
     of r alone); raises LaspError on a non-zero status."""
-    a, s, f = _Args(shape.dtype), shape, torch.float32
-    n = s.rows * s.C
-    args = (ctypes.byref(s), a.of(r, "r", n), a.of(x, "x", n), a.of(scale, "scale", s.C, f), a.of(weight, "weight", s.C, f), float(eps),
-            a.of(r_out, "r_out", n), a.of(y, "y", n))
-    a.call(lib.lasp_addnorm_fwd, "lasp_addnorm_fwd", args, stream)
+    (d, at), f, C = _home(r, "lasp_addnorm_fwd", shape, check_rows), torch.float32, shape.C
+    n = shape.rows * C
+    _call(lib.lasp_addnorm_fwd, "lasp_addnorm_fwd", at, stream, ctypes.byref(shape), _addr(r, "r", n, d, at), _addr(x, "x", n, d, at),
+          _addr(scale, "scale", C, f, at), _addr(weight, "weight", C, f, at), eps, _addr(r_out, "r_out", n, d, at), _addr(y, "y", n, d, at))
 
 
 def lasp_addnorm_bwd(shape: RowsShape, r_out, x, scale, weight, eps, dy, dr_out, dr, dx, dweight, dscale, scratch, stream=None) -> None:
     """Gradients of lasp_addnorm_fwd from its r_out (dr_out: what reaches r_out past the norm, or None; dx, dweight, dscale may be
     None, scratch then too); raises LaspError on a non-zero status."""
-    a, s, f = _Args(shape.dtype), shape, torch.float32
-    n = s.rows * s.C
-    args = (ctypes.byref(s), a.of(r_out, "r_out", n), a.of(x, "x", n), a.of(scale, "scale", s.C, f), a.of(weight, "weight", s.C, f),
-            float(eps), a.of(dy, "dy", n), a.of(dr_out, "dr_out", n), a.of(dr, "dr", n), a.of(dx, "dx", n),
-            a.of(dweight, "dweight", s.C, f), a.of(dscale, "dscale", s.C, f), *a.scratch(scratch))
-    a.call(lib.lasp_addnorm_bwd, "lasp_addnorm_bwd", args, stream)
+    (d, at), f, C = _home(r_out, "lasp_addnorm_bwd", shape, check_rows), torch.float32, shape.C
+    n = shape.rows * C
+    _call(lib.lasp_addnorm_bwd, "lasp_addnorm_bwd", at, stream, ctypes.byref(shape), _addr(r_out, "r_out", n, d, at),
+          _addr(x, "x", n, d, at), _addr(scale, "scale", C, f, at), _addr(weight, "weight", C, f, at), eps, _addr(dy, "dy", n, d, at),
+          _addr(dr_out, "dr_out", n, d, at), _addr(dr, "dr", n, d, at), _addr(dx, "dx", n, d, at), _addr(dweight, "dweight", C, f, at),
+          _addr(dscale, "dscale", C, f, at), *_room(scratch, at))
 
 
 def lasp_gatenorm_fwd(shape: GateShape, o, u, weight, eps, y, stream=None) -> None:
     """y = weight * o / rms(o) * act(u): o [B,H,N,D], u [B,N,H*D] (rows shape.ld apart), y [B,N,H*D], weight float32 [H*D] or None;
     raises LaspError on a non-zero status."""
-    a, s = _Args(shape.dtype), shape
-    wide, n = s.H * s.D, s.B * s.N * s.H * s.D
-    args = (ctypes.byref(s), a.of(o, "o", n), a.rows(u, "u", s.B, s.N, wide, s.ld), a.of(weight, "weight", wide, torch.float32), float(eps),
-            a.of(y, "y", n))
-    a.call(lib.lasp_gatenorm_fwd, "lasp_gatenorm_fwd", args, stream)
+    (d, at), B, N, C = _home(o, "lasp_gatenorm_fwd", shape, check_gate), shape.B, shape.N, shape.H * shape.D
+    n = B * N * C
+    _call(lib.lasp_gatenorm_fwd, "lasp_gatenorm_fwd", at, stream, ctypes.byref(shape), _addr(o, "o", n, d, at),
+          _addr_rows(u, "u", B, N, C, shape.ld, d, at), _addr(weight, "weight", C, torch.float32, at), eps, _addr(y, "y", n, d, at))
 
 
 def lasp_gatenorm_bwd(shape: GateShape, o, u, weight, eps, dy, do, du, dweight, scratch, stream=None) -> None:
     """Gradients of lasp_gatenorm_fwd: do as o, du as u, dweight (may be None, scratch then too); raises LaspError on a non-zero
     status."""
-    a, s = _Args(shape.dtype), shape
-    wide, n = s.H * s.D, s.B * s.N * s.H * s.D
-    args = (ctypes.byref(s), a.of(o, "o", n), a.rows(u, "u", s.B, s.N, wide, s.ld), a.of(weight, "weight", wide, torch.float32), float(eps),
-            a.of(dy, "dy", n), a.of(do, "do", n), a.rows(du, "du", s.B, s.N, wide, s.ld), a.of(dweight, "dweight", wide, torch.float32),
-            *a.scratch(scratch))
-    a.call(lib.lasp_gatenorm_bwd, "lasp_gatenorm_bwd", args, stream)
+    (d, at), f, B, N, C = _home(o, "lasp_gatenorm_bwd", shape, check_gate), torch.float32, shape.B, shape.N, shape.H * shape.D
+    n = B * N * C
+    _call(lib.lasp_gatenorm_bwd, "lasp_gatenorm_bwd", at, stream, ctypes.byref(shape), _addr(o, "o", n, d, at),
+          _addr_rows(u, "u", B, N, C, shape.ld, d, at), _addr(weight, "weight", C, f, at), eps, _addr(dy, "dy", n, d, at),
+          _addr(do, "do", n, d, at), _addr_rows(du, "du", B, N, C, shape.ld, d, at), _addr(dweight, "dweight", C, f, at),
+          *_room(scratch, at))
 
 
 class Workspace:

@@ -106,6 +106,10 @@ CASES = [  # B, N, D, lens, packed, fused
     (1, 4100, 8, None, True, False),
     (1, 2111, 1040, None, False, False),
     (17, 600, 64, None, False, False),
+    (9, 3000, 8, [3000, 0, 1, 256, 257, 2999, 512, 1000, 40], True, False),     # sequences of one column block end in different tiles
+    (4, 1500, 72, [1500, 300, 0, 700], False, True),
+    (3, 700, 64, [1, 0, 256], False, False),                                    # and none of them in the last
+    (3, 5000, 8, [700, 4600, 0], False, False),
 ]
 
 
@@ -118,10 +122,10 @@ def test_against_the_definition(L, B, N, D, lens, packed, fused, dtype, coupled)
     check(run(L, inp, dtype, coupled, fused=fused), inp, dtype, coupled, "rec")
 
 
-@pytest.mark.parametrize("N", [1, 3, 200, 2500])
+@pytest.mark.parametrize("N,lens", [(1, None), (3, [1, 0, 3]), (200, None), (2500, None), (2500, [2500, 0, 900])])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_states_updated_in_place(L, dtype, N):
-    inp = make(dtype, 3, N, 128, seed=N)
+def test_states_updated_in_place(L, dtype, N, lens):
+    inp = make(dtype, 3, N, 128, seed=N, lens=lens)
     a, b = run(L, inp, dtype, False), run(L, inp, dtype, False, in_place=True)
     for k in a:
         assert torch.equal(a[k], b[k]), k
