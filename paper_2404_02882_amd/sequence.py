@@ -192,3 +192,49 @@ class BidirSequence:
         if self.T:
             lasp.lasp_bidir_seq_bwd(self._shapes, self.T, q, k, v, dout, self.kv, self.dkv, dq, dk, dv, self.scratch)
         return self.dkv
+
+
+class RecurrenceSequence:
+    """Gated linear recurrence h_s = exp(log_a_s) h_{s-1} + b_s x_s over T sub-sequences (lasp_rec_*): h_out of one is
+    h_in of the next, dh_in of one the dh_out of the one before, as LaspSequence hands its states on.
+
+    x, log_a, dx, dlog_a are lists of T tensors [B,N/T,D] (with `ld`, views of rows that far apart, as the halves of one
+    projection's output), out and dout lists of T contiguous ones. All buffers are allocated once, up front; the calls only
+    enqueue kernels and can be captured (GraphedStep).
+    """
+
+    def __init__(self, B, N, D, dtype: torch.dtype, T=1, coupled=False, ld=0, device="cuda", need_backward=True):
+        if N % T != 0:
+            raise ValueError("N must be a multiple of T")
+        self.T = T
+        self.shape = lasp.make_rec_shape(B, N // T, D, dtype, coupled, ld)
+        rc = lasp.check_rec(self.shape)
+        if rc != 0:
+            raise lasp.LaspError(rc, "RecurrenceSequence")
+        self.coupled = bool(coupled)
+        self.scratch = torch.empty(lasp.rec_scratch_bytes(self.shape), dtype=torch.uint8, device=device)
+        # h[t] = state entering sub-sequence t (h[T] = final); dh[t] = gradient w.r.t. h[t]
+        self.h = [torch.zeros(B, D, dtype=torch.float32, device=device) for _ in range(T + 1)]
+        self.dh = [torch.zeros(B, D, dtype=torch.float32, device=device) for _ in range(T + 1)] if need_backward else None
+        self.has_h_in = False
+
+    def forward(self, x: List[torch.Tensor], log_a, out: List[torch.Tensor], h_in: Optional[torch.Tensor] = None,
+                lens: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
+        """lens: per sub-sequence the int32 [B] tokens that each sequence has in it (None: all)."""
+        self.has_h_in = h_in is not None
+        if h_in is not None:
+            self.h[0].copy_(h_in)
+        for t in range(self.T):
+            lasp.lasp_rec_fwd(self.shape, x[t], log_a[t], self.h[t] if t or self.has_h_in else None, lens[t] if lens else None, out[t],
+                              self.h[t + 1], self.scratch)
+        return self.h[self.T]
+
+    def backward(self, x, log_a, out, dout, dx, dlog_a, dh_out: Optional[torch.Tensor] = None,
+                 lens: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
+        if dh_out is not None:
+            self.dh[self.T].copy_(dh_out)
+        for t in reversed(range(self.T)):
+            lasp.lasp_rec_bwd(self.shape, x[t] if self.coupled else None, log_a[t], out[t], self.h[t] if t or self.has_h_in else None,
+                              lens[t] if lens else None, dout[t], self.dh[t + 1] if t + 1 < self.T or dh_out is not None else None, dx[t],
+                              dlog_a[t], self.dh[t], self.scratch)
+        return self.dh[0]
