@@ -235,17 +235,18 @@ DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
 
 // LANES threads side by side along the columns; the others of a wave are further rows. Eight, a line of 128 bytes of every row:
 // the fewer columns, the longer the tile and the fewer there are to pass the state on through (bfloat16 32768 x 2048, tiles of
-// 4 waves, 64 / 16 / 8 lanes: forward 214 / 92 / 88 us, backward 216 / 137 / 134).
-constexpr int kLanes = 8, kBack = 8;
-template <typename T, bool COUPLED, bool BWD, int WAVES, int ROWS, bool STREAM>
+// 4 waves, 64 / 16 / 8 lanes: forward 214 / 92 / 88 us, backward 216 / 137 / 134). Rows that are no whole lines: two column blocks
+// share the lines between them, so those are wider (see rec_cut).
+constexpr int kBack = 8;
+template <typename T, bool COUPLED, bool BWD, int LANES, int WAVES, int ROWS, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_tiles(const T *__restrict__ X, const T *__restrict__ L, const T *__restrict__ out_in,
                                                          const T *__restrict__ dout, const float *h_in, const float *enter,
                                                          const int *__restrict__ len, T *__restrict__ out, T *__restrict__ dx,
                                                          T *__restrict__ dl, float *leave, RecLook lk, int cols, int N, int D,
                                                          long long ld, int ntiles, int nblocks) {
     using P = Piece<T>;
-    constexpr int W = P::W, NT = 64 * WAVES, LANES = kLanes, PARTS = 64 / LANES, NCH = LANES * W;
-    static_assert(NCH <= 64, "a thread per channel");
+    constexpr int W = P::W, NT = 64 * WAVES, PARTS = 64 / LANES, NCH = LANES * W;
+    static_assert(NCH <= NT, "a thread per channel");
     constexpr bool kKeepGates = sizeof(T) == 4;   // the rows' gates, once computed, in the place of their log_a
     __shared__ float sL[WAVES][NCH], sX[WAVES][NCH];
     __shared__ unsigned sTicket;
@@ -457,9 +458,14 @@ __global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t counte
 //   tiles of 8 waves       of few columns and many tokens, where the state's way from tile to tile takes the time, 1 us per kBack tiles
 //                          (131072 x 128 33 / 49, in four waves 73 / 75; 32768 x 2048 95 / 139 and 88 / 134; 4096 x 64 even)
 //   tiles of 4 waves       otherwise
+// Rows that are no whole lines, in blocks of 8 / 16 / 32 / 64 lanes: 4 x 16384 x 1000 forward 119 / 108 / 109 / 105, backward 205 / 178 / 167 / 166;
+// float 32768 x 296 42 / 36.5 / 38.5 / 50 and 58 / 51 / 51 / 75; of 37 columns 22 / 25 / 34 / 44 and 34 / 36 / 46 / 70. (With non-temporal accesses in
+// blocks of 8 163 / 300: a line goes before the other workgroup's half has come.)
 constexpr int kShort = 16, kLong = 4096, kFewBlocks = 8, kManyColumns = 1 << 17;
 namespace {
 struct RecCut {
+    int lanes;                       // of a column block
+    bool lines;                      // rows are whole lines of 128 bytes
     int waves;                       // of a workgroup of k_rec_tiles; 0: a thread per column
     int nblocks, ntiles;
     size_t counters, slots, bytes;   // of the scratch: of the counters, slots, bytes of everything
@@ -468,19 +474,22 @@ constexpr int thread_rows(int waves, bool bwd) { return waves == 8 && !bwd ? 16 
 RecCut rec_cut(const RecPlan &p, bool bwd) {
     const int w = p.dtype == 0 ? 4 : 8, cols = p.B * (p.D / w);
     RecCut c{};
-    c.nblocks = (cols + kLanes - 1) / kLanes;
+    const int size = p.dtype == 0 ? 4 : 2;
+    c.lines = p.D * size % 128 == 0 && p.ld * size % 128 == 0;
+    c.lanes = c.lines || p.N <= 128 || cols < 64 ? 8 : cols < 512 ? 16 : 32;
+    c.nblocks = (cols + c.lanes - 1) / c.lanes;
     if (p.N <= kShort || (p.N <= 128 && cols >= kManyColumns)) c.waves = 0;
     else if (p.N <= 64) c.waves = 1;
     else if (p.N <= 128) c.waves = 2;
     else c.waves = c.nblocks <= kFewBlocks && p.N > kLong ? 8 : 4;
-    const int rows = std::max(c.waves, 1) * (64 / kLanes) * thread_rows(c.waves, bwd);
+    const int rows = std::max(c.waves, 1) * (64 / c.lanes) * thread_rows(c.waves, bwd);
     c.ntiles = c.waves ? (p.N + rows - 1) / rows : 1;
-    c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * kLanes * w : 0;
+    c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * c.lanes * w : 0;
     c.counters = (size_t)kGroups * kTicketStride * sizeof(unsigned);
     c.bytes = c.counters + (c.slots * 12 + 15) / 16 * 16;
     return c;
 }
-template <typename T, bool C, bool BWD, int WAVES>
+template <typename T, bool C, bool BWD, int LANES, int WAVES>
 void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t s) {
     char *base = (char *)a.scratch;
     RecLook lk{(unsigned *)base, (unsigned long long *)(base + c.counters), (unsigned *)(base + c.counters + c.slots * 8)};
@@ -488,8 +497,11 @@ void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t 
         const size_t n = c.bytes / 16;
         k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, c.counters / 16, n);
     }
-    const size_t bytes = (size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T);
-    const auto kernel = past_cache(bytes) ? k_rec_tiles<T, C, BWD, WAVES, thread_rows(WAVES, BWD), true> : k_rec_tiles<T, C, BWD, WAVES, thread_rows(WAVES, BWD), false>;
+    constexpr int ROWS = thread_rows(WAVES, BWD);
+    auto kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, false>;
+    if constexpr (LANES == 8 && WAVES >= 4)   // (lines that two workgroups share have to stay in the cache)
+        if (c.lines && past_cache((size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T)))
+            kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, true>;
     kernel<<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * WAVES), 0, s>>>(
         (const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, BWD ? a.dh_out : a.h_in, a.len, (T *)a.out, (T *)a.dx,
         (T *)a.dlog_a, BWD ? a.dh_in : a.h_out, lk, p.B * (p.D / Piece<T>::W), p.N, p.D, p.ld, c.ntiles, c.nblocks);
@@ -500,10 +512,17 @@ hipError_t rec(const RecPlan &p, const RecArgs &a, hipStream_t s) {
     const int cols = p.B * (p.D / Piece<T>::W);
     const dim3 grid((cols + kStepThreads - 1) / kStepThreads), block(kStepThreads);
     switch (c.waves) {
-        case 1: rec_tiles<T, C, BWD, 1>(p, a, c, s); break;
-        case 2: rec_tiles<T, C, BWD, 2>(p, a, c, s); break;
-        case 4: rec_tiles<T, C, BWD, 4>(p, a, c, s); break;
-        case 8: rec_tiles<T, C, BWD, 8>(p, a, c, s); break;
+        case 1: rec_tiles<T, C, BWD, 8, 1>(p, a, c, s); break;
+        case 2: rec_tiles<T, C, BWD, 8, 2>(p, a, c, s); break;
+        case 4:
+            if (c.lanes == 8) rec_tiles<T, C, BWD, 8, 4>(p, a, c, s);
+            else if (c.lanes == 16) rec_tiles<T, C, BWD, 16, 4>(p, a, c, s);
+            else rec_tiles<T, C, BWD, 32, 4>(p, a, c, s);
+            break;
+        case 8:   // (of 8 column blocks at most: not 32 lanes)
+            if (c.lanes == 8) rec_tiles<T, C, BWD, 8, 8>(p, a, c, s);
+            else rec_tiles<T, C, BWD, 16, 8>(p, a, c, s);
+            break;
         default:
             if constexpr (BWD)
                 k_rec_step_bwd<T, C><<<grid, block, 0, s>>>((const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in,

@@ -527,7 +527,7 @@ def _room(t, at):
 
 def _call(fn, where, at, stream, *args):
     """On `stream`, or the current one of the tensors' device."""
-    if at == torch.cuda.current_device():
+    if at == torch._C._cuda_getDevice():
         rc = fn(*args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(at):
