@@ -96,38 +96,35 @@ struct Weights {
     }
 };
 
-// A workgroup's sums for a vector of C floats, one partial row: its row groups are added one after the other in LDS.
+// A workgroup's sums for a vector of C floats, one partial row: the row groups of a wave are added by shuffles, those of several
+// waves (or rows of two waves) one after the other in LDS.
 template <typename T, int LANES, int PIECES>
-DEVI void write_partial(const Mine<T, LANES, PIECES> &my, const float (&acc)[PIECES][Piece<T>::W], float *dst, float *lds) {
-    constexpr int W = Piece<T>::W, ROWS = Group<LANES>::ROWS;
-    const int row = threadIdx.x / LANES;
-    if constexpr (ROWS > 1) {
-        for (int r = 0; r < ROWS; ++r) {
-            __syncthreads();
-            if (row == r)
+DEVI void write_partial(const Mine<T, LANES, PIECES> &my, float (&acc)[PIECES][Piece<T>::W], float *dst, float *lds) {
+    constexpr int W = Piece<T>::W, SPAN = LANES < 64 ? 64 : LANES, PARTS = Group<LANES>::NT / SPAN;
 #pragma unroll
-                for (int k = 0; k < PIECES; ++k)
-                    if (my.has(k)) {
-                        float *p = lds + my.at(k);
-                        float f[W];
-#pragma unroll
-                        for (int i = 0; i < W; ++i) f[i] = acc[k][i];
-                        if (r > 0) {
-                            float g[W];
-                            load_floats<W>(p, g);
-#pragma unroll
-                            for (int i = 0; i < W; ++i) f[i] += g[i];
-                        }
-                        if (r == ROWS - 1) store_floats<W>(dst + my.at(k), f);
-                        else store_floats<W>(p, f);
-                    }
-        }
-        __syncthreads();
-    } else {
+    for (int d = LANES; d < 64; d *= 2)
 #pragma unroll
         for (int k = 0; k < PIECES; ++k)
-            if (my.has(k)) store_floats<W>(dst + my.at(k), acc[k]);
+#pragma unroll
+            for (int i = 0; i < W; ++i) acc[k][i] += __shfl_xor(acc[k][i], d);
+    const bool writes = threadIdx.x % SPAN < LANES;
+    for (int r = 0; r < PARTS; ++r) {
+        if (r > 0) __syncthreads();
+        if (writes && threadIdx.x / SPAN == r)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                if (my.has(k)) {
+                    float *p = lds + my.at(k);
+                    if (r > 0) {
+                        float g[W];
+                        load_floats<W>(p, g);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) acc[k][i] += g[i];
+                    }
+                    store_floats<W>(r == PARTS - 1 ? dst + my.at(k) : p, acc[k]);
+                }
     }
+    if (PARTS > 1) __syncthreads();   // (LDS is free again)
 }
 
 // ---------------------------------------------------------------------------
@@ -474,7 +471,7 @@ __global__ __launch_bounds__(kSumColumns * kSumGroups / 4) void k_column_sums(co
 RowPlan row_plan(int tokens, int heads, int C, int dtype) {
     RowPlan p{tokens, heads, C, dtype, 64, 1};
     const int n = C / (dtype == 0 ? 4 : 8);
-    p.lanes = 8;
+    p.lanes = 2;
     while (p.lanes < n && p.lanes < 256) p.lanes *= 2;
     if (n > 1024) p.lanes = n <= 2048 ? 512 : 1024;
     p.pieces = n <= p.lanes ? 1 : n <= 2 * p.lanes ? 2 : 4;
@@ -490,12 +487,17 @@ int workgroups(const RowPlan &p, int most) {
 }
 // Workgroups of a backward pass that reads `loads` tensors. Rows of one piece a thread: as many on a CU (every CU the same) as keep
 // about the same number of bytes on their way, and no more, since each writes a partial row (addnorm bfloat16 32768 x 2048, four tensors
-// read, 512 / 576 / 768 / 1024 workgroups: 132 / 148 / 144 / 153 us; three: 109 / - / 92 / 97; float 65536 x 1024, four: 324 / - / 270 / 277). Small calls:
-// four turns or more each (8192 x 512 16.3 -> 14.8). Rows of more pieces have enough with two.
+// read, 512 / 576 / 768 / 1024 workgroups: 132 / 148 / 144 / 153 us; three: 109 / - / 92 / 97; float 65536 x 1024, four: 324 / - / 270 / 277);
+// more where a row leaves half of its threads without a piece (129055 x 520, 512 / 1024: 212 / 166; float 768 / 1536: 419 / 305). Small
+// calls: four turns or more each (8192 x 512 16.3 -> 14.8). Rows of more pieces have enough with two.
 int backward_workgroups(const RowPlan &p, int loads) {
-    if (p.pieces > 1) return workgroups(p, 2 * kCus);
     const long long turns = ((long long)p.tokens * p.heads + rows_at_a_time(p) - 1) / rows_at_a_time(p);
-    return workgroups(p, (int)std::max<long long>(std::min<long long>(((p.dtype == 0 ? 7 : 6) - loads) * kCus, turns / 4), kCus));
+    int a_cu = 2;
+    if (p.pieces == 1) {
+        const int n = p.C / (p.dtype == 0 ? 4 : 8), full = (p.dtype == 0 ? 7 : 6) - loads;
+        a_cu = std::min((full * p.lanes + n / 2) / n, p.dtype == 0 ? 2 * full : 4);
+    }
+    return workgroups(p, (int)std::max<long long>(std::min<long long>(a_cu * kCus, turns / 4), kCus));
 }
 // A partial row of the weights' gradients for every workgroup (rows that are tokens), or for every token of a turn.
 int partial_rows(const RowPlan &p, int loads) {
@@ -519,7 +521,7 @@ void by_lanes(const RowPlan &p, F f) {
     switch (key) {
 #define LASP_ROWS(LANES, PIECES) \
     case LANES * 8 + PIECES: return f.template operator()<T, LANES, PIECES, STREAM>();
-        LASP_ROWS(8, 1) LASP_ROWS(16, 1) LASP_ROWS(32, 1) LASP_ROWS(64, 1) LASP_ROWS(128, 1) LASP_ROWS(256, 1)
+        LASP_ROWS(2, 1) LASP_ROWS(4, 1) LASP_ROWS(8, 1) LASP_ROWS(16, 1) LASP_ROWS(32, 1) LASP_ROWS(64, 1) LASP_ROWS(128, 1) LASP_ROWS(256, 1)
         LASP_ROWS(256, 2) LASP_ROWS(256, 4) LASP_ROWS(512, 4)
 #undef LASP_ROWS
         default:

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "lasp_block.h"
 
@@ -489,6 +490,11 @@ RecCut rec_cut(const RecPlan &p, bool bwd) {
     c.bytes = c.counters + (c.slots * 12 + 15) / 16 * 16;
     return c;
 }
+bool on_lines(std::initializer_list<const void *> buffers) {
+    for (const void *b : buffers)
+        if ((uintptr_t)b % 128 != 0) return false;
+    return true;
+}
 template <typename T, bool C, bool BWD, int LANES, int WAVES>
 void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t s) {
     char *base = (char *)a.scratch;
@@ -500,7 +506,7 @@ void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t 
     constexpr int ROWS = thread_rows(WAVES, BWD);
     auto kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, false>;
     if constexpr (LANES == 8 && WAVES >= 4)   // (lines that two workgroups share have to stay in the cache)
-        if (c.lines && past_cache((size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T)))
+        if (c.lines && on_lines({a.x, a.log_a, a.out_in, a.dout, a.out, a.dx, a.dlog_a}) && past_cache((size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T)))
             kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, true>;
     kernel<<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * WAVES), 0, s>>>(
         (const T *)a.x, (const T *)a.log_a, (const T *)a.out_in, (const T *)a.dout, a.h_in, BWD ? a.dh_out : a.h_in, a.len, (T *)a.out, (T *)a.dx,
