@@ -454,7 +454,8 @@ int lasp_rec_bwd(const lasp_rec_shape *shape, const void *x, const void *log_a, 
  *
  *   r, x, r_out, y, dy, dr_out, dr, dx  [rows][C] of `dtype`.    scale, weight, dscale, dweight  [C] float.
  *   x       forward: NULL = nothing is added (r_out and scale must then be NULL). backward: read for dscale only.
- *   scale, weight  NULL = ones.      dr_out  NULL = zeros.      eps  >= 0, finite (LASP_ERR_SHAPE otherwise).
+ *   scale, weight  NULL = ones.      dr_out  NULL = zeros.
+ *   eps     >= 0, finite (LASP_ERR_SHAPE otherwise); with 0 a row of zeros gives NaN.
  *   r_out   may be r, and dr may be dr_out (the same pointer): updated in place.
  *   dx      NULL = not wanted (without a scale it equals dr).     dweight, dscale  NULL = not wanted.
  *   scratch lasp_addnorm_scratch_bytes() bytes; not looked at when neither dweight nor dscale is wanted.
@@ -483,7 +484,7 @@ int lasp_addnorm_bwd(const lasp_rows *shape, const void *r_out, const void *x, c
  *
  *   o, do   [B][H][N][D] of `dtype`.     y, dy  [B][N][H D] of `dtype`.     weight, dweight  [H D] float.
  *   u, du   [B][N] rows of H D elements of `dtype`, `ld` elements from row to row (0 = H D); not looked at with LASP_GATE_NONE.
- *   weight  NULL = ones.      dweight  NULL = not wanted.      eps  >= 0, finite (LASP_ERR_SHAPE otherwise).
+ *   weight  NULL = ones.      dweight  NULL = not wanted.      eps  as above.
  *   scratch lasp_gatenorm_scratch_bytes() bytes; not looked at when dweight is not wanted.
  * Sums as for the norm before a block. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, H, N < 1; D no
  * positive multiple of 8; more than 16384 elements in H D; more than 2^31 - 1 in B N H; an unknown gate or
