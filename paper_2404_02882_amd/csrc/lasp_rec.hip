@@ -65,7 +65,8 @@ struct Column {
 };
 
 // ---------------------------------------------------------------------------
-// k_rec_step_fwd / k_rec_step_bwd: a thread carries a column's state over all tokens, AHEAD tokens requested ahead.
+// k_rec_step_fwd / k_rec_step_bwd: a thread carries a column's state over all tokens, kAhead tokens requested together. One token for
+// 64 sequences x 2048: 3.0 us, all of it launch and one trip to memory.
 // ---------------------------------------------------------------------------
 constexpr int kStepThreads = 64, kAhead = 8;
 
@@ -174,7 +175,8 @@ __global__ __launch_bounds__(kStepThreads) void k_rec_step_bwd(const T *__restri
 //   2. the tile's step is published, and the state that enters the tile found: the nearest tile in front whose end state
 //      is published, and the steps of those between, applied in order,
 //   3. its rows again, from the state that enters them, to the outputs.
-// So every input is read once and every output written once. States are applied one tile after the other whatever is
+// So every input is read once and every output written once, which is what bounds it: bfloat16 4 x 16384 x 4096 1.6 GB in 283 us, backward
+// 3.2 GB in 561, 5.7 TB/s either way (a copy 4.9). States are applied one tile after the other whatever is
 // published when: the same results on every run.
 // Workgroups take their tiles from counters, in the order of the scan: a tile waits only for tiles whose workgroups have
 // started, and those for none behind them, so every wait ends. Each counter serves a quarter of the column blocks: a single one
@@ -475,8 +477,8 @@ constexpr int thread_rows(int waves, bool bwd) { return waves == 8 && !bwd ? 16 
 RecCut rec_cut(const RecPlan &p, bool bwd) {
     const int w = p.dtype == 0 ? 4 : 8, cols = p.B * (p.D / w);
     RecCut c{};
-    const int size = p.dtype == 0 ? 4 : 2;
-    c.lines = p.D * size % 128 == 0 && p.ld * size % 128 == 0;
+    const int line = 128 / (p.dtype == 0 ? 4 : 2);   // elements
+    c.lines = p.D % line == 0 && p.ld % line == 0;
     c.lanes = c.lines || p.N <= 128 || cols < 64 ? 8 : cols < 512 ? 16 : 32;
     c.nblocks = (cols + c.lanes - 1) / c.lanes;
     if (p.N <= kShort || (p.N <= 128 && cols >= kManyColumns)) c.waves = 0;
