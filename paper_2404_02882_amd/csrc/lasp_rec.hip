@@ -12,8 +12,8 @@ namespace lasp {
 // The gate of one token, or the product of several (log_a summed): a step of the recurrence is y -> a y + u.
 template <typename T>
 struct Gate;
-// bfloat16 data: a as a float. Its rounding, 2^-25 of a, is a relative 2^-25 / (1 - a) of what the state converges to;
-// log_a itself comes rounded to 2^-9, which weighs more for any a that a memory of fewer than 2^16 tokens has.
+// bfloat16 data: a as a float. Its rounding, 2^-24 of 1, is a relative 2^-24 / (1 - a) of what the state converges to;
+// log_a itself comes rounded to 2^-8, which weighs more for any a that a memory of fewer than 2^16 tokens has.
 template <>
 struct Gate<bf16_t> {
     float w;

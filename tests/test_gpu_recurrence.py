@@ -295,3 +295,61 @@ def test_captured_and_replayed(L):
                 assert torch.equal(w[k], o[k]), k
         both()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("N", [5, 60, 1500])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gates_at_the_ends(L, dtype, N):
+    """Gates that are open (log a = 0: sums), shut (-inf: the inputs themselves), nearly shut, and above 1."""
+    inp = make(dtype, 2, N, 64, seed=31)
+    la = inp["log_a"]
+    la[:, :, :16] = 0.0
+    la[:, :, 16:32] = -float("inf")
+    la[:, :, 32:40] = -60.0
+    la[:, :, 40:48] = torch.tensor(0.004).to(la.dtype)      # 1.004^1500 = 400
+    got = run(L, inp, dtype, False)
+    check(got, inp, dtype, False, "ends")
+    assert torch.equal(got["out"][:, :, 16:32], inp["x"][:, :, 16:32]) and not got["dlog_a"][:, :, 16:32].any()
+    check(run(L, inp, dtype, True), inp, dtype, True, "ends, coupled")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_is_broken_stays_in_its_channel(L, dtype, bad):
+    """A NaN or infinity in x spoils its channel of its sequence from its token on, and nothing else, in any direction."""
+    N, at = 1300, 700
+    inp = make(dtype, 2, N, 64, seed=32)
+    clean = run(L, inp, dtype, False)
+    inp["x"] = inp["x"].clone()
+    inp["x"][1, at, 5] = bad
+    got = run(L, inp, dtype, False)
+    spoilt = torch.zeros(2, N, 64, dtype=torch.bool)
+    spoilt[1, at:, 5] = True
+    assert torch.equal(got["out"][~spoilt], clean["out"][~spoilt]) and not got["out"][spoilt].isfinite().any()
+    after = torch.zeros(2, N, 64, dtype=torch.bool)
+    after[1, at + 1:, 5] = True          # dlog_a takes the state in front of a token
+    assert torch.equal(got["dx"], clean["dx"]) and torch.equal(got["dlog_a"][~after], clean["dlog_a"][~after])
+
+
+def test_two_calls_at_once(L):
+    """Calls on two streams, each with a workspace of its own."""
+    sets = []
+    for seed, (B, N, D) in enumerate(((1, 20000, 512), (4, 3000, 1000))):
+        inp = {k: v.cuda() for k, v in make("bf16", B, N, D, seed=seed).items()}
+        shape = L.make_rec_shape(B, N, D, torch.bfloat16, True)
+        new = lambda: [torch.empty_like(inp["x"]) for _ in range(3)] + [torch.empty_like(inp["h_in"]) for _ in range(2)]   # noqa: E731
+        sets.append((shape, inp, new(), new(), torch.empty(L.rec_scratch_bytes(shape), dtype=torch.uint8, device="cuda"), torch.cuda.Stream()))
+
+    def both_passes(shape, i, o, scratch, stream):
+        L.lasp_rec_fwd(shape, i["x"], i["log_a"], i["h_in"], None, o[0], o[3], scratch, stream=stream)
+        L.lasp_rec_bwd(shape, i["x"], i["log_a"], o[0], i["h_in"], None, i["dout"], i["dh_out"], o[1], o[2], o[4], scratch, stream=stream)
+
+    for shape, inp, want, _, scratch, _ in sets:
+        both_passes(shape, inp, want, scratch, None)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for shape, inp, _, got, scratch, stream in sets:
+            both_passes(shape, inp, got, scratch, stream)
+    torch.cuda.synchronize()
+    for _, _, want, got, _, _ in sets:
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
