@@ -457,36 +457,39 @@ __global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t counte
 // How a call is cut (bfloat16, forward / backward in us, from a graph):
 //   a thread per column    up to kShort tokens, where all is latency (8 x 16 x 2048 5.3 / 6.9, as a tile 7.0 / 8.6; 24 tokens 6.7 / 9.1
 //                          and 7.0 / 8.6), and where the columns alone fill the device (64 x 64 x 16384 85 / 134 and 90 / 146)
-//   one tile               of as few waves as cover the tokens (64 x 64 x 2048 12.6 / 17.5, in four waves 22.8 / 37.8)
+//   one tile               of as few waves as cover the tokens (64 x 64 x 2048 12.6 / 17.5, in four waves 22.8 / 37.8), up to 512 tokens if that
+//                          needs no more than two workgroups a CU (8 x 512 x 2048 with the host's time 11.9 / 17.3, as two tiles with what they
+//                          need cleared first 16.0 / 21.1; 64 x 512 x 2048 87.7 / 136 and 77.0 / 124)
 //   tiles of 8 waves       of few columns and many tokens, where the state's way from tile to tile takes the time, 1 us per kBack tiles
 //                          (131072 x 128 33 / 49, in four waves 73 / 75; 32768 x 2048 95 / 139 and 88 / 134; 4096 x 64 even)
 //   tiles of 4 waves       otherwise
 // Rows that are no whole lines, in blocks of 8 / 16 / 32 / 64 lanes: 4 x 16384 x 1000 forward 119 / 108 / 109 / 105, backward 205 / 178 / 167 / 166;
 // float 32768 x 296 42 / 36.5 / 38.5 / 50 and 58 / 51 / 51 / 75; of 37 columns 22 / 25 / 34 / 44 and 34 / 36 / 46 / 70. (With non-temporal accesses in
 // blocks of 8 163 / 300: a line goes before the other workgroup's half has come.)
-constexpr int kShort = 16, kLong = 4096, kFewBlocks = 8, kManyColumns = 1 << 17;
+constexpr int kShort = 16, kLong = 4096, kFewBlocks = 8, kManyColumns = 1 << 17, kCus = 256;
 namespace {
 struct RecCut {
     int lanes;                       // of a column block
     bool lines;                      // rows are whole lines of 128 bytes
-    int waves;                       // of a workgroup of k_rec_tiles; 0: a thread per column
+    int waves, rows;                 // of a workgroup of k_rec_tiles, of a thread; 0: a thread per column
     int nblocks, ntiles;
     size_t counters, slots, bytes;   // of the scratch: of the counters, slots, bytes of everything
 };
-constexpr int thread_rows(int waves, bool bwd) { return waves == 8 && !bwd ? 16 : 8; }
 RecCut rec_cut(const RecPlan &p, bool bwd) {
     const int w = p.dtype == 0 ? 4 : 8, cols = p.B * (p.D / w);
     RecCut c{};
     const int line = 128 / (p.dtype == 0 ? 4 : 2);   // elements
     c.lines = p.D % line == 0 && p.ld % line == 0;
-    c.lanes = c.lines || p.N <= 128 || cols < 64 ? 8 : cols < 512 ? 16 : 32;
+    const bool one = p.N <= 512 && (cols + 7) / 8 <= (c.lines || p.N <= 256 ? 2 * kCus : kCus);   // tile of eight waves, at most
+    c.lanes = c.lines || p.N <= 128 || cols < 64 || one ? 8 : cols < 512 ? 16 : 32;
     c.nblocks = (cols + c.lanes - 1) / c.lanes;
     if (p.N <= kShort || (p.N <= 128 && cols >= kManyColumns)) c.waves = 0;
     else if (p.N <= 64) c.waves = 1;
     else if (p.N <= 128) c.waves = 2;
-    else c.waves = c.nblocks <= kFewBlocks && p.N > kLong ? 8 : 4;
-    const int rows = std::max(c.waves, 1) * (64 / c.lanes) * thread_rows(c.waves, bwd);
-    c.ntiles = c.waves ? (p.N + rows - 1) / rows : 1;
+    else c.waves = (c.nblocks <= kFewBlocks && p.N > kLong) || (one && p.N > 256) ? 8 : 4;
+    c.rows = c.waves == 8 && p.N > kLong && !bwd ? 16 : 8;
+    const int tokens = std::max(c.waves, 1) * (64 / c.lanes) * c.rows;
+    c.ntiles = c.waves ? (p.N + tokens - 1) / tokens : 1;
     c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * c.lanes * w : 0;
     c.counters = (size_t)kGroups * kTicketStride * sizeof(unsigned);
     c.bytes = c.counters + (c.slots * 12 + 15) / 16 * 16;
@@ -497,7 +500,7 @@ bool on_lines(std::initializer_list<const void *> buffers) {
         if ((uintptr_t)b % 128 != 0) return false;
     return true;
 }
-template <typename T, bool C, bool BWD, int LANES, int WAVES>
+template <typename T, bool C, bool BWD, int LANES, int WAVES, int ROWS = 8>
 void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t s) {
     char *base = (char *)a.scratch;
     RecLook lk{(unsigned *)base, (unsigned long long *)(base + c.counters), (unsigned *)(base + c.counters + c.slots * 8)};
@@ -505,7 +508,6 @@ void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t 
         const size_t n = c.bytes / 16;
         k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, c.counters / 16, n);
     }
-    constexpr int ROWS = thread_rows(WAVES, BWD);
     auto kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, false>;
     if constexpr (LANES == 8 && WAVES >= 4)   // (lines that two workgroups share have to stay in the cache)
         if (c.lines && on_lines({a.x, a.log_a, a.out_in, a.dout, a.out, a.dx, a.dlog_a}) && past_cache((size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T)))
@@ -528,8 +530,10 @@ hipError_t rec(const RecPlan &p, const RecArgs &a, hipStream_t s) {
             else rec_tiles<T, C, BWD, 32, 4>(p, a, c, s);
             break;
         case 8:   // (of 8 column blocks at most: not 32 lanes)
-            if (c.lanes == 8) rec_tiles<T, C, BWD, 8, 8>(p, a, c, s);
-            else rec_tiles<T, C, BWD, 16, 8>(p, a, c, s);
+            if (c.rows == 8 && c.lanes == 8) rec_tiles<T, C, BWD, 8, 8>(p, a, c, s);
+            else if constexpr (BWD) rec_tiles<T, C, BWD, 16, 8>(p, a, c, s);
+            else if (c.lanes == 8) rec_tiles<T, C, BWD, 8, 8, 16>(p, a, c, s);
+            else rec_tiles<T, C, BWD, 16, 8, 16>(p, a, c, s);
             break;
         default:
             if constexpr (BWD)

@@ -114,6 +114,9 @@ CASES = [  # B, N, D, lens, packed, fused
     (2, 1300, 1000, [900, 1300], True, False), # and in tiles of 4
     (1, 400, 4104, None, False, False),        # blocks of 32
     (1, 400, 4096, None, False, True),
+    (2, 512, 72, [257, 512], True, False),     # one tile of 8 waves, and one token more
+    (2, 513, 64, [513, 100], False, False),
+    (33, 300, 1024, None, False, False),       # too many columns for it
 ]
 
 
