@@ -521,8 +521,9 @@ def _room(t, at):
     """Address and size of a workspace."""
     if t is None:
         return None, 0
-    n = t.numel()
-    return _addr(t, "scratch", n, t.dtype, at), n * t.element_size()
+    if t.get_device() != at or at < 0 or not t.is_contiguous():
+        _refuse(t, "scratch", t.numel(), t.dtype, at)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _call(fn, where, at, stream, *args):
