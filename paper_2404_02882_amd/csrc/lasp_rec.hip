@@ -461,12 +461,13 @@ __global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t counte
 //                          needs no more than two workgroups a CU (8 x 512 x 2048 with the host's time 11.9 / 17.3, as two tiles with what they
 //                          need cleared first 16.0 / 21.1; 64 x 512 x 2048 87.7 / 136 and 77.0 / 124)
 //   tiles of 8 waves       of few columns and many tokens, where the state's way from tile to tile takes the time, 1 us per kBack tiles
-//                          (131072 x 128 33 / 49, in four waves 73 / 75; 32768 x 2048 95 / 139 and 88 / 134; 4096 x 64 even)
+//                          (131072 x 128 33 / 49, in four waves 73 / 75; 16384 x 128 16.2 / 16.6 and 15.2 / 18.2; 8192 x 128
+//                          15.1 / 14.3 and 11.7 / 14.8; of more columns, 32768 x 2048, 95 / 139 and 88 / 134)
 //   tiles of 4 waves       otherwise
 // Rows that are no whole lines, in blocks of 8 / 16 / 32 / 64 lanes: 4 x 16384 x 1000 forward 119 / 108 / 109 / 105, backward 205 / 178 / 167 / 166;
 // float 32768 x 296 42 / 36.5 / 38.5 / 50 and 58 / 51 / 51 / 75; of 37 columns 22 / 25 / 34 / 44 and 34 / 36 / 46 / 70. (With non-temporal accesses in
 // blocks of 8 163 / 300: a line goes before the other workgroup's half has come.)
-constexpr int kShort = 16, kLong = 4096, kFewBlocks = 8, kManyColumns = 1 << 17, kCus = 256;
+constexpr int kShort = 16, kLongForward = 16384, kLongBackward = 8192, kFewBlocks = 8, kManyColumns = 1 << 17, kCus = 256;
 namespace {
 struct RecCut {
     int lanes;                       // of a column block
@@ -483,11 +484,12 @@ RecCut rec_cut(const RecPlan &p, bool bwd) {
     const bool one = p.N <= 512 && (cols + 7) / 8 <= (c.lines || p.N <= 256 ? 2 * kCus : kCus);   // tile of eight waves, at most
     c.lanes = c.lines || p.N <= 128 || cols < 64 || one ? 8 : cols < 512 ? 16 : 32;
     c.nblocks = (cols + c.lanes - 1) / c.lanes;
+    const bool long_tiles = c.nblocks <= kFewBlocks && p.N >= (bwd ? kLongBackward : kLongForward);
     if (p.N <= kShort || (p.N <= 128 && cols >= kManyColumns)) c.waves = 0;
     else if (p.N <= 64) c.waves = 1;
     else if (p.N <= 128) c.waves = 2;
-    else c.waves = (c.nblocks <= kFewBlocks && p.N > kLong) || (one && p.N > 256) ? 8 : 4;
-    c.rows = c.waves == 8 && p.N > kLong && !bwd ? 16 : 8;
+    else c.waves = long_tiles || (one && p.N > 256) ? 8 : 4;
+    c.rows = long_tiles && !bwd ? 16 : 8;
     const int tokens = std::max(c.waves, 1) * (64 / c.lanes) * c.rows;
     c.ntiles = c.waves ? (p.N + tokens - 1) / tokens : 1;
     c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * c.lanes * w : 0;

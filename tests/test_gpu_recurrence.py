@@ -110,8 +110,11 @@ CASES = [  # B, N, D, lens, packed, fused
     (4, 1500, 72, [1500, 300, 0, 700], False, True),
     (3, 700, 64, [1, 0, 256], False, False),                                    # and none of them in the last
     (3, 5000, 8, [700, 4600, 0], False, False),
-    (1, 4500, 1000, None, False, False),       # rows that are no whole lines: blocks of 16 columns in tiles of 8 waves
+    (1, 8200, 600, None, False, False),        # rows that are no whole lines: blocks of 16 columns, backward in tiles of 8 waves
+    (1, 16400, 520, None, True, False),        # forward too
     (2, 1300, 1000, [900, 1300], True, False), # and in tiles of 4
+    (2, 16500, 8, [16500, 9000], False, False),
+    (1, 16384, 64, None, False, True),
     (1, 400, 4104, None, False, False),        # blocks of 32
     (1, 400, 4096, None, False, True),
     (2, 512, 72, [257, 512], True, False),     # one tile of 8 waves, and one token more
