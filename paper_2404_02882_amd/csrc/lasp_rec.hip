@@ -238,7 +238,7 @@ DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
 
 // LANES threads side by side along the columns; the others of a wave are further rows. Eight, a line of 128 bytes of every row:
 // the fewer columns, the longer the tile and the fewer there are to pass the state on through (bfloat16 32768 x 2048, tiles of
-// 4 waves, 64 / 16 / 8 lanes: forward 214 / 92 / 88 us, backward 216 / 137 / 134). Rows that are no whole lines: two column blocks
+// 4 waves, one counter, no streaming: 64 / 16 / 8 lanes forward 214 / 92 / 88 us, backward 216 / 137 / 134). Rows that are no whole lines: two column blocks
 // share the lines between them, so those are wider (see rec_cut).
 constexpr int kBack = 8;
 template <typename T, bool COUPLED, bool BWD, int LANES, int WAVES, int ROWS, bool STREAM>
