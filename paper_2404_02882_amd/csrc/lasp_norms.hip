@@ -273,10 +273,11 @@ DEVI void activate(int gate, float u, float &act, float &slope) {
         act = u;
         slope = 1.0f;
     } else {
-        // 1 / (1 + 2^-u log2 e): 0 and 1 at the ends, where the power is infinite or 0
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.44269504f));
+        // s = 1 / (1 + e^-u): 0 and 1 at the ends, where the power is infinite or 0. Its complement s(-u) where s is near 1, e^-u s, has the
+        // precision that 1 - s loses there (at u = 16 6 %, from 17 on everything).
+        const float e = __builtin_amdgcn_exp2f(u * -1.44269504f), s = __builtin_amdgcn_rcpf(1.0f + e), c = u > 0.0f ? e * s : 1.0f - s;
         act = gate == 2 ? s : u * s;
-        slope = gate == 2 ? s * (1.0f - s) : s * __builtin_fmaf(u, 1.0f - s, 1.0f);
+        slope = s * (gate == 2 ? c : __builtin_fmaf(u, c, 1.0f));
     }
 }
 
