@@ -424,8 +424,9 @@ int lasp_bidir_seq_bwd(const lasp_shape *shapes, int32_t T, const void *const *q
  *   x       (backward) read only when coupled, may be NULL otherwise. out: as the forward call wrote it; h_{s-1} is taken
  *           from there, so for bfloat16 data dlog_a carries that rounding (2^-8 of h).
  *   scratch lasp_rec_scratch_bytes() bytes, for either call.
- * The state is carried in float. Float data: for log_a < 0 the distance 1 - a keeps its 24 bits however near to 1 a is; otherwise, and
- * for bfloat16 data, it is exact to 2^-22 (for bfloat16 log_a's own precision down to 1 - a = 2^-14). An infinite state, as infinite inputs make, may go on as NaN.
+ * The state is carried in float. Float data: for log_a < 0 the distance 1 - a keeps its 24 bits however near to 1 a is, above it is exact
+ * to 2^-22. bfloat16 data: 1 - a is exact to 2^-12 of itself for log_a <= 0; a is held as a float, off by at most 2^-24, which is
+ * at most N 2^-24 of the state after N tokens. An infinite state, as infinite inputs make, may go on as NaN.
  * Sequences continue as with lasp_fwd: h_out of one call is h_in of the next, dh_in the dh_out of the call before.
  * Results are bit-reproducible. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, N < 1; D no
  * positive multiple of 8; ld neither 0 nor a multiple of 8 from D up; more than 2^31 - 1 in B N or B D.

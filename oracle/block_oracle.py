@@ -67,8 +67,10 @@ def rec_bounds(dtype, x, log_a, dout=None, h_in=None, lens=None, dh_out=None, co
 
     b_abs = np.abs(np.expm1(log_a)) if coupled else np.ones_like(a)
     # 1 - a from a as a single float, as bfloat16 calls and float ones with log_a > 0 form it: the power is off by at most 2^-24 of its
-    # exponent's rounding and 2^-23 of its own for a <= 2, and the difference rounds once more, 2^-24: below 2^-22 of 1
+    # exponent's rounding and 2^-23 of its own for a <= 2, and the difference rounds once more, 2^-24: below 2^-22 of 1. bfloat16 calls take
+    # -log_a within 2^-11 of 0, which is off by at most 2^-12 of 1 - a: below 2^-11 of it everywhere up to log_a = 0
     b_err = np.where((log_a > 0) | (dtype == "bf16"), 2.0 ** -22, 0.0) if coupled else np.zeros_like(a)
+    b_err = np.where(log_a > 0, b_err, np.minimum(b_err, 2.0 ** -11 * b_abs))
     H, E, _, E_out = carry(b_abs * np.abs(x), range, a, zero if h_in is None else h_in, b_err * np.abs(x))
     out, h_out = rec_fwd(x, log_a, h_in, lens, coupled)
     got = {"out": half * np.abs(out) + E, "h_out": E_out + 2.0 ** -24 * np.abs(h_out)}

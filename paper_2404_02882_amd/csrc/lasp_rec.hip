@@ -12,19 +12,20 @@ namespace lasp {
 // The gate of one token, or the product of several (log_a summed): a step of the recurrence is y -> a y + u.
 template <typename T>
 struct Gate;
-// bfloat16 data: a as a float. Its rounding, 2^-24 of 1, is a relative 2^-24 / (1 - a) of what the state converges to;
-// log_a itself comes rounded to 2^-8, which weighs more for any a that a memory of fewer than 2^16 tokens has.
+// bfloat16 data: a as a float, off by at most a step of 2^-24, which is at most N 2^-24 of a state after N tokens. 1 - a to a relative 2^-12, an
+// eighth of what rounding to bfloat16 does at most, however near to 1 a is: from -2^-11 on as -log_a (what is left out is log_a / 2 of it),
+// elsewhere from the power (off by a step of 2^-24 of 1). Gates near 1 held as float data's are: 32768 x 2048 forward + backward 211 -> 242 us.
 template <>
 struct Gate<bf16_t> {
-    float w;
-    DEVI explicit Gate(float log_a) : w(__builtin_amdgcn_exp2f(log_a * 1.44269504f)) {}
+    float w, l;
+    DEVI explicit Gate(float log_a) : w(__builtin_amdgcn_exp2f(log_a * 1.44269504f)), l(log_a) {}
     static DEVI Gate of_word(float w) { return Gate(w, 0); }
     DEVI float step(float y, float u) const { return __builtin_fmaf(w, y, u); }
     DEVI float times(float y) const { return w * y; }
-    DEVI float b() const { return 1.0f - w; }
+    DEVI float b() const { return __builtin_fabsf(l) < 1.0f / 2048 ? -l : 1.0f - w; }
 
 private:
-    DEVI Gate(float word, int) : w(word) {}
+    DEVI Gate(float word, int) : w(word), l(0) {}
 };
 // Float data: for -1/4 < log_a < 0 the distance a - 1 from 1, by its power series (what is left out, log_a^6 / 7! < 2^-24 of it,
 // rounds away), so that 1 - a has 24 bits however near to 1 a is: with a itself 20000 tokens of a = 1 - 1e-6 are 1.4e-4 off, as
