@@ -415,7 +415,7 @@ int lasp_bidir_seq_bwd(const lasp_shape *shapes, int32_t T, const void *const *q
  *   x, log_a, dx, dlog_a  [B][N] rows of D elements of `dtype`, `ld` elements from row to row (0 = D): the value and the
  *           gate may lie side by side in the output of one projection, their gradients in that of its gradient.
  *   out, dout  [B][N][D] of `dtype`.      h_in, h_out, dh_out, dh_in  [B][D] float.
- *   log_a   any value up to 0 (above, the state grows). -inf: a = 0, the state starts anew at that token (documents
+ *   log_a   any value up to 88 (above 0 the state grows; a state of 0 stays 0, whatever the product of its gates). -inf: a = 0, the state starts anew at that token (documents
  *           packed into one sequence); the gradient there is 0.
  *   len     NULL, or DEVICE int32 [B]: tokens of every sequence, 0 <= len <= N (other values count as the nearest of
  *           these). What the inputs hold past it is not looked at; out, dx and dlog_a are 0 there.

@@ -9,7 +9,7 @@
 
 namespace lasp {
 
-// The gate of one token, or the product of several (log_a summed): a step of the recurrence is y -> a y + u.
+// The gate of one token, or the product of several (log_a summed, up to 88): a step of the recurrence is y -> a y + u.
 template <typename T>
 struct Gate;
 // bfloat16 data: a as a float, off by at most a step of 2^-24, which is at most N 2^-24 of a state after N tokens. 1 - a to a relative 2^-12, an
@@ -52,6 +52,32 @@ struct Gate<float> {
 private:
     DEVI Gate(float word, int) : w(word) {}
 };
+
+// The product of several gates, given their log_a summed, as one word, and a step by that word. Small: sums of up to kMostLog.
+constexpr float kMostLog = 88.0f;
+template <typename T>
+struct SmallProduct {
+    static DEVI float word(float l) { return Gate<T>(l).w; }
+    static DEVI float step(float w, float y, float u) { return Gate<T>::of_word(w).step(y, u); }
+};
+// Any: above e^88, which is near the largest float, the word is minus the sum (those of gates lie above -1). Such a product of a state
+// of 0 is 0, and that of a tiny state need not be infinite.
+template <typename T>
+struct AnyProduct {
+    static DEVI float word(float l) { return l > kMostLog ? -l : Gate<T>(l).w; }
+    static DEVI float step(float w, float y, float u) {
+        if (w < -1.0f) {   // e^-w y as 2^n (2^rest y), the rest up to 1/2; from 2^300 on anything but 0 is infinite
+            const float e = fminf(w * -1.44269504f, 300.0f), n = __builtin_rintf(e);
+            return __builtin_ldexpf(y * __builtin_amdgcn_exp2f(e - n), (int)n) + u;
+        }
+        return Gate<T>::of_word(w).step(y, u);
+    }
+};
+template <typename T, typename F>
+DEVI auto by_product(bool small, F f) {
+    if (__all(small)) return f(SmallProduct<T>{});
+    return f(AnyProduct<T>{});
+}
 
 // Where a column lies: its sequence, first channel, tokens that exist.
 template <typename T>
@@ -212,6 +238,9 @@ DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
         unsigned end[BACK];
 #pragma unroll
         for (int k = 0; k < BACK; ++k) end[k] = look(lk.ends + at(k));
+        float least = 0.0f;               // (a word below -1: a product above e^88)
+#pragma unroll
+        for (int k = 0; k < BACK; ++k) least = fminf(least, __builtin_bit_cast(float, (unsigned)step[k]));
         int found = -1, missing = BACK;   // nearest end; nearest tile without a step
 #pragma unroll
         for (int k = BACK - 1; k >= 0; --k) {
@@ -219,13 +248,15 @@ DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
             if ((unsigned)step[k] == kEmpty) missing = k;
         }
         if (found >= 0 && found <= missing) {
-            float y = 0.0f;
+            return by_product<T>(least >= -1.0f, [&](auto p) {
+                float y = 0.0f;
 #pragma unroll
-            for (int k = BACK - 1; k >= 0; --k) {
-                if (k == found) y = __builtin_bit_cast(float, end[k]);
-                else if (k < found) y = Gate<T>::of_word(__builtin_bit_cast(float, (unsigned)step[k])).step(y, __builtin_bit_cast(float, (unsigned)(step[k] >> 32)));
-            }
-            return y;
+                for (int k = BACK - 1; k >= 0; --k) {
+                    if (k == found) y = __builtin_bit_cast(float, end[k]);
+                    else if (k < found) y = p.step(__builtin_bit_cast(float, (unsigned)step[k]), y, __builtin_bit_cast(float, (unsigned)(step[k] >> 32)));
+                }
+                return y;
+            });
         }
         // (a published step stays: asked for again only where one is missing)
         if (missing < BACK) {
@@ -334,18 +365,23 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
         }
         if constexpr (kKeepGates) vl[r] = P::pack(fw);
     }
-    if constexpr (PARTS > 1) {   // joined with those in front, along the wave
+    float most = S[0];   // (of PARTS sums of up to 88 / PARTS none adds up to more than 88)
 #pragma unroll
-        for (int d = LANES; d < 64; d *= 2)
+    for (int i = 1; i < W; ++i) most = fmaxf(most, S[i]);
+    const bool small = __all(most <= kMostLog / PARTS);
+    if constexpr (PARTS > 1)   // joined with those in front, along the wave
+        by_product<T>(small, [&](auto p) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                const float l = __shfl_up(S[i], d), y = __shfl_up(Y[i], d);
-                if (lane >= d) {
-                    Y[i] = Gate<T>(S[i]).step(y, Y[i]);
-                    S[i] += l;
+            for (int d = LANES; d < 64; d *= 2)
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float l = __shfl_up(S[i], d), y = __shfl_up(Y[i], d);
+                    if (lane >= d) {
+                        Y[i] = p.step(p.word(S[i]), y, Y[i]);
+                        S[i] += l;
+                    }
                 }
-            }
-    }
+        });
     if (part == PARTS - 1) {
         store_floats<W>(&sX[w][cl * W], Y);
         store_floats<W>(&sL[w][cl * W], S);
@@ -358,15 +394,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
     const size_t nstate = (size_t)cols * W, stride = (size_t)nblocks * NCH;
     if (const int ch = threadIdx.x; ch < NCH) {
         const size_t state = (size_t)block * NCH + ch, slot = tile * stride + state;
-        float tl = 0.0f, tx = 0.0f, y, gate[WAVES];
+        float tl = 0.0f, tx = 0.0f, y, gate[WAVES], whole_tile, end, most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) {
-            const Gate<T> g(sL[i][ch]);
-            tx = g.step(tx, sX[i][ch]);
-            tl += sL[i][ch];
-            gate[i] = g.w;
-        }
-        const Gate<T> whole_tile(tl);
+        for (int i = 0; i < WAVES; ++i) most = fmaxf(most, sL[i][ch]);
+        const bool small = __all(most <= kMostLog / WAVES);
+        by_product<T>(small, [&](auto p) {
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                gate[i] = p.word(sL[i][ch]);
+                tx = p.step(gate[i], tx, sX[i][ch]);
+                tl += sL[i][ch];
+            }
+            whole_tile = p.word(tl);
+        });
         // The channel's tiles, from that of its sequence's first token in the order of the scan to that of its last.
         int begin = 0, last = ntiles - 1;
         if (len) {
@@ -379,29 +419,33 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
         } else if (tile == begin) {
             y = enter && state < nstate ? enter[state] : 0.0f;
         } else {
-            if (tile < last) show(lk.steps + slot, (unsigned long long)published(whole_tile.w) | (unsigned long long)published(tx) << 32);
+            if (tile < last) show(lk.steps + slot, (unsigned long long)published(whole_tile) | (unsigned long long)published(tx) << 32);
             y = entering<T, kBack>(lk, tile - begin, slot, stride);
         }
-        const float end = whole_tile.step(y, tx);   // (as the tiles behind form it)
+        by_product<T>(small, [&](auto p) { end = p.step(whole_tile, y, tx); });   // (as the tiles behind form it)
         if (begin <= tile && tile < last) show(lk.ends + slot, published(end));
         if (tile == last && leave && state < nstate) leave[state] = end;
+        by_product<T>(small, [&](auto p) {
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) {
-            const float x = sX[i][ch];
-            sX[i][ch] = y;
-            y = Gate<T>::of_word(gate[i]).step(y, x);
-        }
+            for (int i = 0; i < WAVES; ++i) {
+                const float x = sX[i][ch];
+                sX[i][ch] = y;
+                y = p.step(gate[i], y, x);
+            }
+        });
     }
     __syncthreads();
     // 3.
     float y[W];
     load_floats<W>(&sX[w][cl * W], y);
     if constexpr (PARTS > 1)
+        by_product<T>(small, [&](auto p) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float l = __shfl_up(S[i], LANES), x = __shfl_up(Y[i], LANES);
-            if (part > 0) y[i] = Gate<T>(l).step(y[i], x);
-        }
+            for (int i = 0; i < W; ++i) {
+                const float l = __shfl_up(S[i], LANES), x = __shfl_up(Y[i], LANES);
+                if (part > 0) y[i] = p.step(p.word(l), y[i], x);
+            }
+        });
     auto again = [](float f) {
         if constexpr (kKeepGates) return Gate<T>::of_word(f);
         else return Gate<T>(f);
