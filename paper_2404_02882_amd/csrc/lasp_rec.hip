@@ -536,7 +536,7 @@ RecCut rec_cut(const RecPlan &p, bool bwd) {
     else c.waves = long_tiles || (one && p.N > 256) ? 8 : 4;
     c.rows = long_tiles && !bwd ? 16 : 8;
     const int tokens = std::max(c.waves, 1) * (64 / c.lanes) * c.rows;
-    c.ntiles = c.waves ? (p.N + tokens - 1) / tokens : 1;
+    c.ntiles = c.waves ? (int)(((long long)p.N + tokens - 1) / tokens) : 1;
     c.slots = c.ntiles > 1 ? (size_t)c.ntiles * c.nblocks * c.lanes * w : 0;
     c.counters = (size_t)kGroups * kTicketStride * sizeof(unsigned);
     c.bytes = c.counters + (c.slots * 12 + 15) / 16 * 16;
