@@ -283,7 +283,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
     constexpr int W = P::W, NT = 64 * WAVES, PARTS = 64 / LANES, NCH = LANES * W;
     static_assert(NCH <= NT, "a thread per channel");
     constexpr bool kKeepGates = sizeof(T) == 4;   // the rows' gates, once computed, in the place of their log_a
-    __shared__ float sL[WAVES][NCH], sX[WAVES][NCH];
+    __shared__ __attribute__((aligned(16))) float sL[WAVES][NCH], sX[WAVES][NCH];   // (moved in pieces)
     __shared__ unsigned sTicket;
     // (moved on by one from tile to tile: a block's tiles then go to all XCDs in turn)
     const unsigned turn = (nblocks % 8 == 0 ? blockIdx.x + blockIdx.x / nblocks : blockIdx.x) % nblocks;
