@@ -423,7 +423,9 @@ int lasp_bidir_seq_bwd(const lasp_shape *shapes, int32_t T, const void *const *q
  *   h_out, dh_in  may be NULL.     dh_out  NULL = zeros.
  *   x       (backward) read only when coupled, may be NULL otherwise. out: as the forward call wrote it; h_{s-1} is taken
  *           from there, so for bfloat16 data dlog_a carries that rounding (2^-8 of h).
- *   scratch lasp_rec_scratch_bytes() bytes, for either call.
+ *   scratch lasp_rec_scratch_bytes() bytes, for either call. Its workgroups wait for words that others write there: a call that
+ *           overlaps another in time (two streams, two graphs replayed at once) needs a scratch of its own, or the results of
+ *           both are wrong, NaN among them, and they may take seconds or minutes to end.
  * The state is carried in float. Float data: for log_a < 0 the distance 1 - a keeps its 24 bits however near to 1 a is, above it is exact
  * to 2^-22. bfloat16 data: 1 - a is exact to 2^-12 of itself for log_a <= 0; a is held as a float, off by at most 2^-24, which is
  * at most N 2^-24 of the state after N tokens. An infinite state, as infinite inputs make, may go on as NaN.

@@ -227,14 +227,16 @@ template <typename V>
 DEVI void show(V *p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // The state that enters a tile for one channel, whose slots in consecutive tiles are `stride` apart, `slot` that of this one. The
-// channel's first tile, `back` tiles in front, publishes no step, and nothing in front of it is looked at.
+// channel's first tile, `back` tiles in front, publishes no step, and nothing in front of it is looked at. NaN after kMostLooks, some
+// seconds: only where a call that overlaps in time has cleared the scratch, and the words never come.
+constexpr int kMostLooks = 1 << 22;
 template <typename T, int BACK>
 DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
     auto at = [&](int k) { return slot - (size_t)min(k + 1, back) * stride; };
     unsigned long long step[BACK];
 #pragma unroll
     for (int k = 0; k < BACK; ++k) step[k] = look(lk.steps + at(k));
-    for (;;) {
+    for (int looks = 0; looks < kMostLooks; ++looks) {
         unsigned end[BACK];
 #pragma unroll
         for (int k = 0; k < BACK; ++k) end[k] = look(lk.ends + at(k));
@@ -266,6 +268,7 @@ DEVI float entering(const RecLook &lk, int back, size_t slot, size_t stride) {
         }
         __builtin_amdgcn_s_sleep(1);
     }
+    return __builtin_nanf("");
 }
 
 // LANES threads side by side along the columns; the others of a wave are further rows. Eight, a line of 128 bytes of every row:
