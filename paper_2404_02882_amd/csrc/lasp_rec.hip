@@ -559,7 +559,8 @@ void rec_tiles(const RecPlan &p, const RecArgs &a, const RecCut &c, hipStream_t 
         k_rec_clear<<<dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)), dim3(256), 0, s>>>((u32x4 *)base, c.counters / 16, n);
     }
     auto kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, false>;
-    if constexpr (LANES == 8 && WAVES >= 4)   // (lines that two workgroups share have to stay in the cache)
+    // (lines that two workgroups share have to stay in the cache; forward, 8 waves of 8 rows take one tile of 100 MB at most)
+    if constexpr (LANES == 8 && (WAVES == 4 || (WAVES == 8 && (BWD || ROWS == 16))))
         if (c.lines && on_lines({a.x, a.log_a, a.out_in, a.dout, a.out, a.dx, a.dlog_a}) && past_cache((size_t)(BWD ? (C ? 6 : 5) : 3) * p.B * p.N * p.D * sizeof(T)))
             kernel = k_rec_tiles<T, C, BWD, LANES, WAVES, ROWS, true>;
     kernel<<<dim3((unsigned)c.ntiles * c.nblocks), dim3(64 * WAVES), 0, s>>>(
