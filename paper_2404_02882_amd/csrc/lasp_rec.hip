@@ -504,18 +504,21 @@ __global__ __launch_bounds__(256) void k_rec_clear(u32x4 *scratch, size_t counte
 // ---------------------------------------------------------------------------
 // How a call is cut (bfloat16, forward / backward in us, from a graph):
 //   a thread per column    up to kShort tokens, where all is latency (8 x 16 x 2048 5.3 / 6.9, as a tile 7.0 / 8.6; 24 tokens 6.7 / 9.1
-//                          and 7.0 / 8.6), and where the columns alone fill the device (64 x 64 x 16384 85 / 134 and 90 / 146)
+//                          and 7.0 / 8.6), and up to 128 where the columns alone fill the device: of 65536 columns 24 tokens
+//                          16 / 25, 64 34 / 66, 128 81 / 132, as tiles 27 / 41, 38 / 82, 88 / 149; of 131072 26 / 42, 81 / 133, 155 / 265
+//                          and 47 / 73, 90 / 147, 169 / 285; of 32768 9 / 16, 25 / 33, 40 / 72 and 17 / 24, 23 / 32, 37 / 82
 //   one tile               of as few waves as cover the tokens (64 x 64 x 2048 12.6 / 17.5, in four waves 22.8 / 37.8), up to 512 tokens if that
 //                          needs no more than two workgroups a CU (8 x 512 x 2048 with the host's time 11.9 / 17.3, as two tiles with what they
 //                          need cleared first 16.0 / 21.1; 64 x 512 x 2048 87.7 / 136 and 77.0 / 124)
 //   tiles of 8 waves       of few columns and many tokens, where the state's way from tile to tile takes the time, 1 us per kBack tiles
 //                          (131072 x 128 33 / 49, in four waves 73 / 75; 16384 x 128 16.2 / 16.6 and 15.2 / 18.2; 8192 x 128
-//                          15.1 / 14.3 and 11.7 / 14.8; of more columns, 32768 x 2048, 95 / 139 and 88 / 134)
+//                          15.1 / 14.3 and 11.7 / 14.8; 131072 tokens of 8 column blocks 92 / 137 and 96 / 139, of 16 162 / 255 and 155 / 246,
+//                          32768 of 8 28 / 42 and 34 / 46, of 16 47 / 79 and 48 / 78, of 32 96 / 136 and 83 / 128)
 //   tiles of 4 waves       otherwise
 // Rows that are no whole lines, in blocks of 8 / 16 / 32 / 64 lanes: 4 x 16384 x 1000 forward 119 / 108 / 109 / 105, backward 205 / 178 / 167 / 166;
 // float 32768 x 296 42 / 36.5 / 38.5 / 50 and 58 / 51 / 51 / 75; of 37 columns 22 / 25 / 34 / 44 and 34 / 36 / 46 / 70. (With non-temporal accesses in
 // blocks of 8 163 / 300: a line goes before the other workgroup's half has come.)
-constexpr int kShort = 16, kLongForward = 16384, kLongBackward = 8192, kFewBlocks = 8, kManyColumns = 1 << 17, kCus = 256;
+constexpr int kShort = 16, kLongForward = 16384, kLongBackward = 8192, kFewBlocks = 8, kManyColumns = 1 << 16, kCus = 256;
 namespace {
 struct RecCut {
     int lanes;                       // of a column block
