@@ -218,9 +218,16 @@ class RecurrenceSequence:
         self.dh = [torch.zeros(B, D, dtype=torch.float32, device=device) for _ in range(T + 1)] if need_backward else None
         self.has_h_in = False
 
+    def _check(self, **lists) -> None:
+        """A list that is too short is refused before the first sub-sequence runs."""
+        for name, tensors in lists.items():
+            if tensors is not None and len(tensors) < self.T:
+                raise ValueError(f"{name}: {len(tensors)} tensors for {self.T} sub-sequences")
+
     def forward(self, x: List[torch.Tensor], log_a, out: List[torch.Tensor], h_in: Optional[torch.Tensor] = None,
                 lens: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
         """lens: per sub-sequence the int32 [B] tokens that each sequence has in it (None: all)."""
+        self._check(x=x, log_a=log_a, out=out, lens=lens)
         self.has_h_in = h_in is not None
         if h_in is not None:
             self.h[0].copy_(h_in)
@@ -231,6 +238,7 @@ class RecurrenceSequence:
 
     def backward(self, x, log_a, out, dout, dx, dlog_a, dh_out: Optional[torch.Tensor] = None,
                  lens: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
+        self._check(x=x if self.coupled else None, log_a=log_a, out=out, dout=dout, dx=dx, dlog_a=dlog_a, lens=lens)
         if dh_out is not None:
             self.dh[self.T].copy_(dh_out)
         for t in reversed(range(self.T)):

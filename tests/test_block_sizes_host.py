@@ -28,3 +28,25 @@ def test_norm_scratch_stays_small(L, dtype, rows, C):
     """One partial row of C floats for every workgroup and sum, of at most ten workgroups a CU."""
     assert 0 < L.addnorm_scratch_bytes(L.make_rows(rows, C, dtype)) <= 2 * 4 * 256 * 10 * C
     assert 0 < L.gatenorm_scratch_bytes(L.make_gate_shape(1, 1, rows, C, dtype)) <= 4 * 256 * 10 * C
+
+
+def test_recurrence_sequence_refuses_short_lists_first():
+    """Before any of its calls: the first would refuse these tensors for lying on the host."""
+    import torch
+    from paper_2404_02882_amd import sequence
+    seq = sequence.RecurrenceSequence(1, 16, 8, torch.float32, T=2, device="cpu")
+    full, short = [torch.zeros(1, 8, 8)] * 2, [torch.zeros(1, 8, 8)]
+    for i in range(3):
+        args = [full] * 3
+        args[i] = short
+        with pytest.raises(ValueError, match="1 tensors for 2 sub-sequences"):
+            seq.forward(*args)
+    with pytest.raises(ValueError, match="lens: 1 tensors"):
+        seq.forward(full, full, full, lens=[torch.zeros(1, dtype=torch.int32)])
+    for i in range(1, 6):       # (x is not read)
+        args = [None] + [full] * 5
+        args[i] = short
+        with pytest.raises(ValueError, match="1 tensors for 2 sub-sequences"):
+            seq.backward(*args)
+    with pytest.raises(ValueError, match="GPU"):
+        seq.forward(full, full, full)
