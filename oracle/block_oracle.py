@@ -169,10 +169,13 @@ def gatenorm(o, u, weight, eps, gate, over, dy=None):
     n = rows * rstd
     w = (np.ones(H * D) if weight is None else np.asarray(weight)).reshape((1, 1) + shape[2:])
     act, slope = (np.ones(shape), np.zeros(shape)) if gate == "none" else [v.reshape(shape) for v in _act(u, gate)]
-    # the sigmoid: a relative (|u| + 4) 2^-23, its complement that of 1
+    # the sigmoid and its complement: a relative (|u| + 4) 2^-23 each; the slope: twice that of s (1 - s), or of s (1 + |u| (1 - s))
     au = np.zeros(shape) if gate == "none" else np.abs(u).reshape(shape)
     act_off = 2.0 ** -21 * (1 + au) ** 2 * (np.abs(act) + (0 if gate in ("none", "identity") else 2.0 ** -6))
-    slope_off = 0 if gate in ("none", "identity") else 2.0 ** -21 * (1 + au) ** 2
+    slope_off = 0
+    if gate not in ("none", "identity"):
+        s, c = 1.0 / (1.0 + np.exp(-u.reshape(shape))), 1.0 / (1.0 + np.exp(u.reshape(shape)))
+        slope_off = 2.0 ** -21 * (1 + au) ** 2 * s * (c if gate == "sigmoid" else 1.0 + au * c)
     flat = lambda t: t.reshape(B, N, H * D)   # noqa: E731
     y = w * n * act
     got = {"y": flat(y)}

@@ -137,17 +137,18 @@ def gatenorm_both_passes(L, dtype, B, H, N, D, over, gate):
             rstd = 1.0 / (O.square().mean(-1, keepdim=True) + EPS).sqrt()
             n = O * rstd
             if gate == "identity":
-                act, slope, loose = U, torch.ones_like(U), 0.0
+                act, slope, loose, size = U, torch.ones_like(U), 0.0, 1.0
             else:
                 sg = torch.sigmoid(U)
                 act, slope = (sg, sg * (1 - sg)) if gate == "sigmoid" else (U * sg, sg * (1 + U * (1 - sg)))
-                loose = 2.0 ** -21 * (1 + U.abs()) ** 2       # (|u| below 6: a sigmoid of a relative (|u| + 4) 2^-23, its slope twice that)
+                size = slope if gate == "sigmoid" else sg * (1 + U.abs() * (1 - sg))
+                loose = 2.0 ** -21 * (1 + U.abs()) ** 2       # (a sigmoid and its complement: a relative (|u| + 4) 2^-23, the slope twice that)
             # (rows of one token again)
             flat = lambda t: t.reshape(-1, H * D)   # noqa: E731
             ref, t = flat(W * n * act), Y * act
             parts = {"y": (y[b, s], ref, half * ref.abs() + flat((W * n).abs() * loose * act.abs()) + k * ref.abs())}
             ref = flat(Y * W * n * slope)
-            parts["du"] = (du[b, s], ref, half * ref.abs() + flat((Y * W * n).abs() * loose) + k * ref.abs())
+            parts["du"] = (du[b, s], ref, half * ref.abs() + flat((Y * W * n).abs() * loose * size) + k * ref.abs())
             wt, off = W * t, (W * t).abs() * loose
             ref = flat(rstd * (wt - n * (wt * n).mean(-1, keepdim=True)))
             room = half * ref.abs() + flat(rstd * (off + n.abs() * (off * n.abs()).mean(-1, keepdim=True)
