@@ -29,8 +29,8 @@ hipError_t launch_rec_fwd(const RecPlan &p, const RecArgs &a, hipStream_t s);
 hipError_t launch_rec_bwd(const RecPlan &p, const RecArgs &a, hipStream_t s);
 
 // Whether a call moves more bytes than the last-level cache holds: its loads and stores then leave the cache to what is used
-// again (non-temporal). bfloat16 32768 x 2048: recurrence forward / backward 84 / 135 -> 82 / 129 us, 4 x 16384 x 4096 305 / 594 -> 288 / 563,
-// norm before a block backward 150 -> 137; smaller calls find their inputs there (float 2 x 4099 x 1000, 30 / 61 us as they are, 41 / 72 so).
+// again (non-temporal). bfloat16 32768 x 2048: recurrence forward / backward 87 / 135 -> 83 / 129 us, 4 x 16384 x 4096 coupled 311 / 589 -> 292 / 557,
+// norm before a block forward / backward 94 / 145 -> 87 / 130; smaller calls find their inputs there (float 2 x 4099 x 1000, 30 / 61 us as they are, 41 / 72 so).
 constexpr bool past_cache(size_t bytes) { return bytes > ((size_t)256 << 20); }
 
 // Norms: rows of C elements, each handled by `lanes` threads with `pieces` 16-byte pieces apiece. A token of `heads` rows.

@@ -4,8 +4,8 @@
 // All of them stream: a row is read once, kept in registers while its sums are formed, and written once. `LANES` threads
 // take a row, `PIECES` pieces of 16 bytes each; a workgroup takes several rows where one does not need it whole, and goes
 // on to further rows, so that weights are loaded once and the gradients of weights are summed in registers.
-// Bound by memory (bfloat16, a copy reaches 4.9 TB/s): k_addnorm_bwd 32768 x 2048 with scale and weight 805 MB in 130 us, 6.2 TB/s; 16 heads x 32768 x 128
-// k_gate_fwd 403 MB in 74 us, 5.4, k_gate_bwd 671 MB in 123 us, 5.5. Small calls are one launch: 64 rows of 2048 3.0 us.
+// Bound by memory (bfloat16, a copy reaches 4.9 TB/s): k_addnorm_bwd 32768 x 2048 with scale and weight 805 MB in 132 us, 6.1 TB/s; 16 heads x 32768 x 128
+// k_gate_fwd 403 MB in 74 us, 5.4, k_gate_bwd 671 MB in 123 us, 5.5. Small calls are one launch: 64 rows of 2048 3.2 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -93,7 +93,7 @@ struct Column {
 
 // ---------------------------------------------------------------------------
 // k_rec_step_fwd / k_rec_step_bwd: a thread carries a column's state over all tokens, kAhead tokens requested together. One token for
-// 64 sequences x 2048: 3.0 us, all of it launch and one trip to memory.
+// 64 sequences x 2048: 3.2 us, all of it launch and one trip to memory.
 // ---------------------------------------------------------------------------
 constexpr int kStepThreads = 64, kAhead = 8;
 
@@ -202,8 +202,8 @@ __global__ __launch_bounds__(kStepThreads) void k_rec_step_bwd(const T *__restri
 //   2. the tile's step is published, and the state that enters the tile found: the nearest tile in front whose end state
 //      is published, and the steps of those between, applied in order,
 //   3. its rows again, from the state that enters them, to the outputs.
-// So every input is read once and every output written once, which is what bounds it: bfloat16 4 x 16384 x 4096 1.6 GB in 283 us, backward
-// 3.2 GB in 561, 5.7 TB/s either way (a copy 4.9). States are applied one tile after the other whatever is
+// So every input is read once and every output written once, which is what bounds it: bfloat16 4 x 16384 x 4096, coupled, 1.6 GB in 291 us,
+// backward 3.2 GB in 562, 5.5 and 5.7 TB/s (a copy 4.9). States are applied one tile after the other whatever is
 // published when: the same results on every run.
 // Workgroups take their tiles from counters, in the order of the scan: a tile waits only for tiles whose workgroups have
 // started, and those for none behind them, so every wait ends. Each counter serves a quarter of the column blocks: a single one
@@ -482,6 +482,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES <= 4 && !BWD ? 3 : 2) void k_rec_
                 const float e = fu[i] + y[i];
                 y[i] = g.times(e);
                 ox[i] = COUPLED ? g.b() * e : e;
+                // (h_{s-1} as it was stored: bfloat16 rounds it to 2^-8, as it will round the gradient; to form it again would take x and log_a twice)
                 ol[i] = y[i] * (COUPLED ? fo[i] - fx[i] : fo[i]);
             }
             if (mine && (whole || at(r) >= 0)) {
