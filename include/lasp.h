@@ -510,6 +510,52 @@ int lasp_gatenorm_fwd(const lasp_gate_shape *shape, const void *o, const void *u
 int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u, const float *weight, float eps, const void *dy,
                       void *d_o, void *du, float *dweight, void *scratch, size_t scratch_bytes, void *hip_stream);
 
+/*
+ * ---- Gated delta rule -------------------------------------------------------------
+ * A member of the family of App. A.4 whose oscillation is a matrix: before a token is written, what the state returns for its key
+ * is taken out. For every head and token s = 1..len, with a_s = exp(log_g_s) and the state [D][Dv] as for lasp_fwd:
+ *     w_s = v_s - a_s kv_{s-1}^T k_s,     kv_s = a_s kv_{s-1} + beta_s k_s w_s^T,     out_s = kv_s^T q_s,     kv_0 = kv_in,   kv_out = kv_len.
+ * Backward: gradients of sum(out * dout) + sum(kv_out * dkv_out) with respect to q, k, v, log_g, beta and kv_in.
+ * Sequences continue as with lasp_fwd: kv_out of one call is kv_in of the next, dkv_in the dkv_out of the call before.
+ *
+ *   q, k, dq, dk      [B][key_heads][N][D] of `dtype`.    v, out, dout, dv  [B][H][N][Dv] of `dtype`.
+ *   beta, dbeta       [B][H][N] float, any finite value (0..1, or up to 2).
+ *   log_g, dlog_g     [B][H][N] float, <= 0; -inf: a = 0, the state starts anew at that token (documents packed into one sequence),
+ *                     and the gradient there is 0. Both NULL = no decay (a = 1). From 2^-150 down a counts as 0. Values
+ *                     > 0 or NaN give undefined numbers (never a fault).
+ *   len               NULL, or DEVICE int32 [B]: tokens of every sequence, 0 <= len <= N (other values count as the nearest of these). What the
+ *                     inputs hold past it is not looked at; out and all gradients are 0 there.
+ *   kv_in, kv_out, dkv_out, dkv_in   [B][H][D][Dv] float. kv_in, dkv_out: NULL = zeros. kv_out may be kv_in and dkv_in may be dkv_out (the
+ *                     same pointer): updated in place.
+ *   state_cache       forward: NULL = no backward pass will follow; else lasp_delta_cache_bytes() bytes, to be handed to lasp_delta_bwd
+ *                     with the same shape and inputs (it holds kv_in too). One float state for every 64 tokens (float data: 32).
+ *   scratch           lasp_delta_scratch_bytes() bytes forward, lasp_delta_bwd_scratch_bytes() backward (one state a tile and one
+ *                     float for every value). Not looked at by forward calls of at most 16 tokens without a cache, which run token by token.
+ * Keys are expected to be of length 1 or shorter (lasp_qk_fwd's norm LASP_NORM_L2), with 0 <= beta <= 2: then no state grows; with
+ * longer ones it may, as the formula says. States, gates and sums are held in float, sums of log_g in 64 bits. Factors that a call computes
+ * go into products in two bfloat16 parts with bfloat16 data (off by at most 2^-18 of themselves), in three with float data, which is split as for lasp_fwd
+ * (infinities and numbers that round to infinity as bfloat16 come out NaN).
+ * Results are bit-reproducible. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, H, N < 1; more than 65535 in B H; D or
+ * Dv (0 = D) not 64 or 128; key_heads (0 = H) no divisor of H: H / key_heads consecutive states share a head of q and k, whose gradients are summed.
+ */
+typedef struct {
+    int32_t B, H, N, D;
+    int32_t dtype;      /* lasp_dtype */
+    int32_t Dv;         /* 0 = D */
+    int32_t key_heads;  /* 0 = H */
+} lasp_delta_shape;
+int lasp_check_delta(const lasp_delta_shape *shape);
+/* 0 on an invalid shape. */
+size_t lasp_delta_cache_bytes(const lasp_delta_shape *shape);
+size_t lasp_delta_scratch_bytes(const lasp_delta_shape *shape);
+size_t lasp_delta_bwd_scratch_bytes(const lasp_delta_shape *shape);
+int lasp_delta_fwd(const lasp_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_g, const float *beta,
+                   const float *kv_in, const int32_t *len, void *out, float *kv_out, void *state_cache, void *scratch,
+                   size_t scratch_bytes, void *hip_stream);
+int lasp_delta_bwd(const lasp_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_g, const float *beta,
+                   const int32_t *len, const void *dout, const float *dkv_out, const void *state_cache, void *dq, void *dk, void *dv,
+                   float *dlog_g, float *dbeta, float *dkv_in, void *scratch, size_t scratch_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,6 +40,11 @@ class GateShape(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("over", ctypes.c_int32), ("ld", ctypes.c_int32)]
 
 
+class DeltaShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("Dv", ctypes.c_int32), ("key_heads", ctypes.c_int32)]
+
+
 class LaspError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -145,7 +150,19 @@ def _bind_blocks(handle):
     return handle
 
 
-lib = _bind_blocks(_bind_bidir_sequence(_bind(ctypes.CDLL(LIB_PATH))))
+def _bind_delta(handle):
+    """The same for the gated delta rule."""
+    delta = ctypes.POINTER(DeltaShape)
+    for name in ("cache", "scratch", "bwd_scratch"):
+        size = getattr(handle, f"lasp_delta_{name}_bytes")
+        size.argtypes, size.restype = [delta], _sz
+    handle.lasp_check_delta.argtypes = [delta]
+    handle.lasp_delta_fwd.argtypes = [delta] + [_vp] * 11 + [_sz, _vp]
+    handle.lasp_delta_bwd.argtypes = [delta] + [_vp] * 16 + [_sz, _vp]
+    return handle
+
+
+lib = _bind_delta(_bind_blocks(_bind_bidir_sequence(_bind(ctypes.CDLL(LIB_PATH)))))
 
 
 def profile_begin(max_calls: int) -> None:
@@ -605,6 +622,65 @@ def lasp_gatenorm_bwd(shape: GateShape, o, u, weight, eps, dy, do, du, dweight, 
           _addr_rows(u, "u", B, N, C, shape.ld, d, at), _addr(weight, "weight", C, f, at), eps, _addr(dy, "dy", n, d, at),
           _addr(do, "do", n, d, at), _addr_rows(du, "du", B, N, C, shape.ld, d, at), _addr(dweight, "dweight", C, f, at),
           *_room(scratch, at))
+
+
+# ---- The gated delta rule ---------------------------------------------------------
+def make_delta_shape(B, H, N, D, dtype, Dv=0, key_heads=0) -> DeltaShape:
+    return DeltaShape(int(B), int(H), int(N), int(D), _dtype_code(dtype), int(Dv), int(key_heads))
+
+
+def check_delta(shape: DeltaShape) -> int:
+    return int(lib.lasp_check_delta(ctypes.byref(shape)))
+
+
+def delta_cache_bytes(shape: DeltaShape) -> int:
+    return int(lib.lasp_delta_cache_bytes(ctypes.byref(shape)))
+
+
+def delta_scratch_bytes(shape: DeltaShape) -> int:
+    return int(lib.lasp_delta_scratch_bytes(ctypes.byref(shape)))
+
+
+def delta_bwd_scratch_bytes(shape: DeltaShape) -> int:
+    return int(lib.lasp_delta_bwd_scratch_bytes(ctypes.byref(shape)))
+
+
+def _delta_numels(shape: DeltaShape):
+    """Elements of q, of v, of a state and of beta."""
+    tokens, Dv = shape.B * shape.N, shape.Dv or shape.D
+    return (tokens * (shape.key_heads or shape.H) * shape.D, tokens * shape.H * Dv, shape.B * shape.H * shape.D * Dv, tokens * shape.H)
+
+
+def _cache_addr(cache, shape, at):
+    """The address of a state cache (None passes), which the library takes without its size."""
+    addr, size = _room(cache, at)
+    if addr is not None and size < delta_cache_bytes(shape):
+        raise LaspError(5, "state_cache")
+    return addr
+
+
+def lasp_delta_fwd(shape: DeltaShape, q, k, v, log_g, beta, kv_in, lens, out, kv_out, state_cache, scratch, stream=None) -> None:
+    """Gated delta rule: q, k [B,key_heads,N,D], v, out [B,H,N,Dv], log_g (or None), beta float32 [B,H,N], kv_in (or None), kv_out float32
+    [B,H,D,Dv], lens int32 [B] or None, state_cache None when no backward pass follows; raises LaspError on a non-zero status."""
+    (d, at), f = _home(q, "lasp_delta_fwd", shape, check_delta), torch.float32
+    nq, nv, ns, ng = _delta_numels(shape)
+    _call(lib.lasp_delta_fwd, "lasp_delta_fwd", at, stream, ctypes.byref(shape), _addr(q, "q", nq, d, at), _addr(k, "k", nq, d, at),
+          _addr(v, "v", nv, d, at), _addr(log_g, "log_g", ng, f, at), _addr(beta, "beta", ng, f, at), _addr(kv_in, "kv_in", ns, f, at),
+          _addr(lens, "lens", shape.B, torch.int32, at), _addr(out, "out", nv, d, at), _addr(kv_out, "kv_out", ns, f, at),
+          _cache_addr(state_cache, shape, at) if state_cache is not None else None, *_room(scratch, at))
+
+
+def lasp_delta_bwd(shape: DeltaShape, q, k, v, log_g, beta, lens, dout, dkv_out, state_cache, dq, dk, dv, dlog_g, dbeta, dkv_in, scratch,
+                   stream=None) -> None:
+    """Gradients of lasp_delta_fwd from the state_cache it filled (dkv_out may be None; dlog_g goes with log_g); raises LaspError on a
+    non-zero status."""
+    (d, at), f = _home(q, "lasp_delta_bwd", shape, check_delta), torch.float32
+    nq, nv, ns, ng = _delta_numels(shape)
+    _call(lib.lasp_delta_bwd, "lasp_delta_bwd", at, stream, ctypes.byref(shape), _addr(q, "q", nq, d, at), _addr(k, "k", nq, d, at),
+          _addr(v, "v", nv, d, at), _addr(log_g, "log_g", ng, f, at), _addr(beta, "beta", ng, f, at),
+          _addr(lens, "lens", shape.B, torch.int32, at), _addr(dout, "dout", nv, d, at), _addr(dkv_out, "dkv_out", ns, f, at),
+          _cache_addr(state_cache, shape, at), _addr(dq, "dq", nq, d, at), _addr(dk, "dk", nq, d, at), _addr(dv, "dv", nv, d, at),
+          _addr(dlog_g, "dlog_g", ng, f, at), _addr(dbeta, "dbeta", ng, f, at), _addr(dkv_in, "dkv_in", ns, f, at), *_room(scratch, at))
 
 
 class Workspace:
