@@ -556,6 +556,56 @@ int lasp_delta_bwd(const lasp_delta_shape *shape, const void *q, const void *k, 
                    const int32_t *len, const void *dout, const float *dkv_out, const void *state_cache, void *dq, void *dk, void *dv,
                    float *dlog_g, float *dbeta, float *dkv_in, void *scratch, size_t scratch_bytes, void *hip_stream);
 
+/*
+ * ---- In front of a block's mixer: queries and keys ---------------------------------
+ * From rows of a projection (tokens first) to what the mixers read (heads first), each head of D features normalised, weighted and
+ * rotated by its position, queries and keys in one pass:
+ *     n = w * x * r,    r = (mean_c x^2 + eps)^(-1/2) (LASP_NORM_RMS), (sum_c x^2 + eps)^(-1/2) (LASP_NORM_L2) or 1 (LASP_NORM_NONE),
+ *     pairs (a, b) of the first `rot` features, i = 0 .. rot/2 - 1, with t = pos freq_i:
+ *     y_a = amplitude (n_a cos t - n_b sin t),    y_b = amplitude (n_a sin t + n_b cos t);    y = n for the others.
+ * A pair is (i, i + rot/2) with LASP_ROT_HALF, (2 i, 2 i + 1) with LASP_ROT_INTERLEAVED. Backward: gradients with respect to x and w.
+ *
+ *   xq, dxq   [B][N] rows of H D elements of `dtype`, `ld` elements from row to row (0 = H D).
+ *   xk, dxk   the same of key_heads D, `ld` apart too (0 = key_heads D): queries and keys may lie side by side in the output of one projection,
+ *             their gradients in that of its gradient. (backward: x is read only with a norm or when a gradient of a weight is wanted, and may be NULL otherwise.)
+ *   q, dq     [B][H][N][D] of `dtype`.     k, dk  [B][key_heads][N][D]. With key_heads 0 what belongs to keys is not looked at.
+ *   wq, wk    [D] float, shared by the heads; NULL = ones.   dwq, dwk  [D] float; NULL = not wanted.
+ *   freq      DEVICE double [rot/2], radians per position (lasp_rope_frequencies fills a host copy). Angles and whole turns are taken in 64 bits.
+ *   pos       NULL = 0 .. N-1 in every sequence, or DEVICE int32 [B][N]. (freq and pos are not looked at with rot = 0.)
+ *   amplitude finite; multiplies what is rotated (1, or the factor that goes with some scalings).     eps  as above.
+ *   scratch   lasp_qk_scratch_bytes() bytes; not looked at when neither dwq nor dwk is wanted.
+ * Sums as for the norm before a block. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, H, N < 1, key_heads < 0, more than 65536
+ * heads; D no multiple of 8 in 8..256; rot no multiple of 16 in 0..D; more than 2^31 - 1 in B N (H + key_heads), 2^30 - 1 in B N; an unknown norm or layout;
+ * ld neither 0 nor a multiple of 8 from H D and key_heads D up.
+ */
+typedef enum { LASP_NORM_NONE = 0, LASP_NORM_RMS = 1, LASP_NORM_L2 = 2 } lasp_norm;
+typedef enum { LASP_ROT_HALF = 0, LASP_ROT_INTERLEAVED = 1 } lasp_rot;
+typedef struct {
+    int32_t B, N, H, key_heads, D;
+    int32_t dtype;    /* lasp_dtype */
+    int32_t norm;     /* lasp_norm */
+    int32_t rot;      /* features rotated; 0 = none */
+    int32_t layout;   /* lasp_rot */
+    int32_t ld;       /* 0 = H D (keys: key_heads D) */
+} lasp_qk_shape;
+int lasp_check_qk(const lasp_qk_shape *shape);
+size_t lasp_qk_scratch_bytes(const lasp_qk_shape *shape);
+int lasp_qk_fwd(const lasp_qk_shape *shape, const void *xq, const void *xk, const float *wq, const float *wk, float eps, const double *freq,
+                const int32_t *pos, float amplitude, void *q, void *k, void *hip_stream);
+int lasp_qk_bwd(const lasp_qk_shape *shape, const void *xq, const void *xk, const float *wq, const float *wk, float eps, const double *freq,
+                const int32_t *pos, float amplitude, const void *dq, const void *dk, void *dxq, void *dxk, float *dwq, float *dwk, void *scratch,
+                size_t scratch_bytes, void *hip_stream);
+/*
+ * freq_host[i] = base^(-2 i / rot), i = 0 .. rot/2 - 1 (rot even, from 4 up; LASP_ERR_SHAPE otherwise), for a context `factor` times as long as the trained one:
+ *   LASP_ROPE_LINEAR  divided by factor;      LASP_ROPE_BASE  from base * factor^(rot / (rot - 2)): the slowest is divided by it, the fastest kept;
+ *   LASP_ROPE_BANDS   kept where a pair makes many_turns or more within `trained` positions, divided by factor where few_turns or less, and
+ *                     between the two by the turns linearly. (trained, few_turns, many_turns are looked at here only.)
+ * Host only.
+ */
+typedef enum { LASP_ROPE_PLAIN = 0, LASP_ROPE_LINEAR = 1, LASP_ROPE_BASE = 2, LASP_ROPE_BANDS = 3 } lasp_rope;
+int lasp_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double trained, double few_turns, double many_turns,
+                          double *freq_host);
+
 #ifdef __cplusplus
 }
 #endif

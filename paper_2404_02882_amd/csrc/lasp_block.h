@@ -66,6 +66,29 @@ hipError_t launch_addnorm_bwd(const RowPlan &p, const AddNormArgs &a, hipStream_
 hipError_t launch_gatenorm_fwd(const RowPlan &p, const GateArgs &a, hipStream_t s);
 hipError_t launch_gatenorm_bwd(const RowPlan &p, const GateArgs &a, hipStream_t s);
 
+// out0 = the sum of n rows of C floats at part0, in a fixed order; the same for part1 and out1. An out may be null.
+hipError_t launch_column_sums(const float *part0, float *out0, const float *part1, float *out1, int n, int C, hipStream_t s);
+
+// Queries and keys by head: norm and position rotation, from rows of projections to heads-first tensors.
+struct QkPlan {
+    int B, N, H, Hk, D, dtype;
+    int norm;               // 0 none, 1 over the mean of squares, 2 over their sum
+    int rot, half;          // features rotated; pairs by halves (else neighbours)
+    long long ldq, ldk;     // elements between the rows of the projections
+};
+struct QkArgs {
+    const void *xq, *xk, *dq, *dk;
+    const float *wq, *wk;   // may be null
+    float eps, amplitude;
+    const double *freq;
+    const int *pos;         // may be null
+    void *q, *k, *dxq, *dxk;
+    float *dwq, *dwk, *scratch;   // may be null
+};
+size_t qk_scratch(const QkPlan &p);
+hipError_t launch_qk_fwd(const QkPlan &p, const QkArgs &a, hipStream_t s);
+hipError_t launch_qk_bwd(const QkPlan &p, const QkArgs &a, hipStream_t s);
+
 }  // namespace lasp
 
 #ifdef __HIPCC__

@@ -1,7 +1,8 @@
-// C-ABI host layer of the gated recurrence and of the norms around a mixer (lasp_rec_*, lasp_addnorm_*, lasp_gatenorm_*):
+// C-ABI host layer of the gated recurrence and of the norms around a mixer (lasp_rec_*, lasp_addnorm_*, lasp_gatenorm_*, lasp_qk_*):
 // argument checks and dispatch. No device memory is allocated or freed here and nothing synchronises.
 #include "../../include/lasp.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "lasp_block.h"
@@ -48,6 +49,20 @@ int make_gate(const lasp_gate_shape *s, lasp::RowPlan *p) {
     return LASP_OK;
 }
 
+int make_qk(const lasp_qk_shape *s, lasp::QkPlan *p) {
+    if (!s) return LASP_ERR_NULL;
+    if (!known(s->dtype)) return LASP_ERR_DTYPE;
+    if (s->B < 1 || s->N < 1 || s->H < 1 || s->key_heads < 0 || !eighths(s->D) || s->D > 256) return LASP_ERR_SHAPE;
+    const int64_t tokens = (int64_t)s->B * s->N, heads = (int64_t)s->H + s->key_heads, q = (int64_t)s->H * s->D, k = (int64_t)s->key_heads * s->D;
+    // (a group's rows are counted in 32 bits, tokens on their way past the last one too)
+    if (heads > 65536 || tokens > kMost / 2 || tokens * heads > kMost || !valid_ld(s->ld, std::max(q, k))) return LASP_ERR_SHAPE;
+    if (s->norm < LASP_NORM_NONE || s->norm > LASP_NORM_L2) return LASP_ERR_SHAPE;
+    if (s->rot < 0 || s->rot > s->D || s->rot % 16 != 0) return LASP_ERR_SHAPE;
+    if (s->layout != LASP_ROT_HALF && s->layout != LASP_ROT_INTERLEAVED) return LASP_ERR_SHAPE;
+    *p = {s->B, s->N, s->H, s->key_heads, s->D, s->dtype, s->norm, s->rot, s->layout == LASP_ROT_HALF, s->ld ? s->ld : q, s->ld ? s->ld : k};
+    return LASP_OK;
+}
+
 // A tensor of rows: `width` of the `ld` bytes from row to row are its own. Two of the same row stride may lie in each other's gaps.
 struct Rows {
     const void *p;
@@ -89,6 +104,23 @@ struct RecSizes {
     Rows gate(const void *p) const { return {p, rows, width, ld}; }
     Rows token(const void *p) const { return whole(p, rows * width); }
 };
+
+// What the buffers of a call on queries and keys take.
+struct QkSizes {
+    size_t e, tokens, q, k, ldq, ldk, weight, freq, pos;
+    explicit QkSizes(const lasp::QkPlan &p)
+        : e(lasp::elem_bytes(p.dtype)), tokens((size_t)p.B * p.N), q((size_t)p.H * p.D * e), k((size_t)p.Hk * p.D * e), ldq(p.ldq * e), ldk(p.ldk * e),
+          weight(p.D * sizeof(float)), freq(p.rot / 2 * sizeof(double)), pos(tokens * sizeof(int32_t)) {}
+    Rows xq(const void *p) const { return {p, tokens, q, ldq}; }
+    Rows xk(const void *p) const { return k ? Rows{p, tokens, k, ldk} : whole(nullptr, 0); }
+    Rows yq(const void *p) const { return whole(p, tokens * q); }
+    Rows yk(const void *p) const { return whole(p, tokens * k); }
+};
+// What both calls are refused for beside their shape and buffers.
+int check_qk(const lasp::QkPlan &p, float eps, float amplitude, const double *freq) {
+    if (!(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(amplitude)) return LASP_ERR_SHAPE;
+    return p.rot > 0 && !freq ? LASP_ERR_NULL : LASP_OK;
+}
 
 bool bad_eps(float eps) { return !(eps >= 0.0f) || !std::isfinite(eps); }
 int status(hipError_t e) { return e == hipSuccess ? LASP_OK : LASP_ERR_HIP; }
@@ -292,6 +324,103 @@ int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u
     a.dweight = dweight;
     a.scratch = (float *)scratch;
     return status(lasp::launch_gatenorm_bwd(p, a, (hipStream_t)hip_stream));
+}
+
+int lasp_check_qk(const lasp_qk_shape *shape) {
+    lasp::QkPlan p;
+    return make_qk(shape, &p);
+}
+
+size_t lasp_qk_scratch_bytes(const lasp_qk_shape *shape) {
+    lasp::QkPlan p;
+    return make_qk(shape, &p) == LASP_OK ? lasp::qk_scratch(p) : 0;
+}
+
+int lasp_qk_fwd(const lasp_qk_shape *shape, const void *xq, const void *xk, const float *wq, const float *wk, float eps, const double *freq,
+                const int32_t *pos, float amplitude, void *q, void *k, void *hip_stream) {
+    lasp::QkPlan p;
+    if (int rc = make_qk(shape, &p); rc != LASP_OK) return rc;
+    if (int rc = check_qk(p, eps, amplitude, freq); rc != LASP_OK) return rc;
+    if (p.Hk == 0) xk = wk = nullptr, k = nullptr;
+    if (p.rot == 0) freq = nullptr, pos = nullptr;
+    if (!xq || !q || (p.Hk > 0 && (!xk || !k))) return LASP_ERR_NULL;
+    const QkSizes b(p);
+    if (int rc = check_rows({b.xq(xq), b.xk(xk), whole(wq, b.weight), whole(wk, b.weight), whole(freq, b.freq), whole(pos, b.pos)}, {b.yq(q), b.yk(k)});
+        rc != LASP_OK)
+        return rc;
+    lasp::QkArgs a{};
+    a.xq = xq;
+    a.xk = xk;
+    a.wq = wq;
+    a.wk = wk;
+    a.eps = eps;
+    a.amplitude = amplitude;
+    a.freq = freq;
+    a.pos = pos;
+    a.q = q;
+    a.k = k;
+    return status(lasp::launch_qk_fwd(p, a, (hipStream_t)hip_stream));
+}
+
+int lasp_qk_bwd(const lasp_qk_shape *shape, const void *xq, const void *xk, const float *wq, const float *wk, float eps, const double *freq,
+                const int32_t *pos, float amplitude, const void *dq, const void *dk, void *dxq, void *dxk, float *dwq, float *dwk, void *scratch,
+                size_t scratch_bytes, void *hip_stream) {
+    lasp::QkPlan p;
+    if (int rc = make_qk(shape, &p); rc != LASP_OK) return rc;
+    if (int rc = check_qk(p, eps, amplitude, freq); rc != LASP_OK) return rc;
+    if (p.Hk == 0) xk = wk = nullptr, dk = nullptr, dxk = nullptr, dwk = nullptr;
+    if (p.rot == 0) freq = nullptr, pos = nullptr;
+    const bool sums = dwq || dwk;
+    if (p.norm == LASP_NORM_NONE && !sums) xq = xk = nullptr;
+    else if (!xq || (p.Hk > 0 && !xk)) return LASP_ERR_NULL;
+    if (!dq || !dxq || (p.Hk > 0 && (!dk || !dxk))) return LASP_ERR_NULL;
+    const size_t need = sums ? lasp::qk_scratch(p) : 0;
+    if (sums && (!scratch || scratch_bytes < need)) return LASP_ERR_WORKSPACE;
+    if (!sums) scratch = nullptr;
+    const QkSizes b(p);
+    if (int rc = check_rows({b.xq(xq), b.xk(xk), whole(wq, b.weight), whole(wk, b.weight), whole(freq, b.freq), whole(pos, b.pos), b.yq(dq), b.yk(dk)},
+                            {b.xq(dxq), b.xk(dxk), whole(dwq, b.weight), whole(dwk, b.weight), whole(scratch, need)});
+        rc != LASP_OK)
+        return rc;
+    lasp::QkArgs a{};
+    a.xq = xq;
+    a.xk = xk;
+    a.wq = wq;
+    a.wk = wk;
+    a.eps = eps;
+    a.amplitude = amplitude;
+    a.freq = freq;
+    a.pos = pos;
+    a.dq = dq;
+    a.dk = dk;
+    a.dxq = dxq;
+    a.dxk = dxk;
+    a.dwq = dwq;
+    a.dwk = dwk;
+    a.scratch = (float *)scratch;
+    return status(lasp::launch_qk_bwd(p, a, (hipStream_t)hip_stream));
+}
+
+int lasp_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double trained, double few_turns, double many_turns,
+                          double *freq_host) {
+    if (!freq_host) return LASP_ERR_NULL;
+    const auto good = [](double x) { return std::isfinite(x) && x > 0.0; };
+    if (rot < 4 || rot % 2 != 0 || !good(base) || scaling < LASP_ROPE_PLAIN || scaling > LASP_ROPE_BANDS) return LASP_ERR_SHAPE;
+    if (scaling != LASP_ROPE_PLAIN && !good(factor)) return LASP_ERR_SHAPE;
+    if (scaling == LASP_ROPE_BANDS && (!good(trained) || !std::isfinite(few_turns) || !std::isfinite(many_turns) || few_turns >= many_turns))
+        return LASP_ERR_SHAPE;
+    if (scaling == LASP_ROPE_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (scaling == LASP_ROPE_LINEAR) f /= factor;
+        if (scaling == LASP_ROPE_BANDS) {
+            const double turns = trained * f / 6.283185307179586477;
+            const double keep = std::min(1.0, std::max(0.0, (turns - few_turns) / (many_turns - few_turns)));
+            f = keep * f + (1.0 - keep) * f / factor;
+        }
+        freq_host[i] = f;
+    }
+    return LASP_OK;
 }
 
 }  // extern "C"

@@ -508,15 +508,6 @@ int partial_rows(const RowPlan &p, int loads) {
     return p.heads == 1 ? n : (int)((long long)n * rows_at_a_time(p) / p.heads);
 }
 constexpr int kLeastLoads = 2;   // (o or r, and dy)
-hipError_t column_sums(const float *p0, float *o0, const float *p1, float *o1, int n, int C, hipStream_t s) {
-    if (!o0) {
-        p0 = p1;
-        o0 = o1;
-        o1 = nullptr;
-    }
-    if (o0) k_column_sums<<<dim3((C + kSumColumns - 1) / kSumColumns, o1 ? 2 : 1), dim3(kSumColumns * kSumGroups / 4), 0, s>>>(p0, o0, p1, o1, n, C);
-    return hipGetLastError();
-}
 // f.template operator()<T, LANES, PIECES, STREAM>() for the plan's.
 template <typename T, bool STREAM, typename F>
 void by_lanes(const RowPlan &p, F f) {
@@ -583,6 +574,15 @@ struct GateBwd {
 };
 }  // namespace
 
+hipError_t launch_column_sums(const float *p0, float *o0, const float *p1, float *o1, int n, int C, hipStream_t s) {
+    if (!o0) {
+        p0 = p1;
+        o0 = o1;
+        o1 = nullptr;
+    }
+    if (o0) k_column_sums<<<dim3((C + kSumColumns - 1) / kSumColumns, o1 ? 2 : 1), dim3(kSumColumns * kSumGroups / 4), 0, s>>>(p0, o0, p1, o1, n, C);
+    return hipGetLastError();
+}
 size_t addnorm_scratch(const RowPlan &p) { return 2 * (size_t)partial_rows(p, kLeastLoads) * p.C * sizeof(float); }
 size_t gatenorm_scratch(const RowPlan &p) { return (size_t)partial_rows(p, kLeastLoads) * p.heads * p.C * sizeof(float); }
 
@@ -593,7 +593,7 @@ hipError_t launch_addnorm_fwd(const RowPlan &p, const AddNormArgs &a, hipStream_
 hipError_t launch_addnorm_bwd(const RowPlan &p, const AddNormArgs &a, hipStream_t s) {
     by_plan(p, 3 + !!a.dscale + !!a.dr_out + !!a.dx, AddNormBwd{p, a, s});
     const int n = partial_rows(p, a.loads());
-    return column_sums(a.scratch, a.dweight, a.scratch + (size_t)n * p.C, a.dscale, n, p.C, s);
+    return launch_column_sums(a.scratch, a.dweight, a.scratch + (size_t)n * p.C, a.dscale, n, p.C, s);
 }
 hipError_t launch_gatenorm_fwd(const RowPlan &p, const GateArgs &a, hipStream_t s) {
     by_plan(p, 2 + !!a.gate, GateFwd{p, a, s});
@@ -601,7 +601,7 @@ hipError_t launch_gatenorm_fwd(const RowPlan &p, const GateArgs &a, hipStream_t 
 }
 hipError_t launch_gatenorm_bwd(const RowPlan &p, const GateArgs &a, hipStream_t s) {
     by_plan(p, 3 + 2 * !!a.gate, GateBwd{p, a, s});
-    return column_sums(a.scratch, a.dweight, nullptr, nullptr, partial_rows(p, a.loads()), p.heads * p.C, s);
+    return launch_column_sums(a.scratch, a.dweight, nullptr, nullptr, partial_rows(p, a.loads()), p.heads * p.C, s);
 }
 
 }  // namespace lasp

@@ -1,0 +1,311 @@
+// HIP kernels (gfx950 / CDNA4) for what stands between a projection and a mixer: queries and keys normalised by head, rotated by
+// position and laid out heads first, in one pass over them.
+//     y = amplitude R(pos) n  on the first `rot` features, y = n on the others;   n = w * x * r,   r = (mean x^2 + eps)^(-1/2), (sum x^2 + eps)^(-1/2) or 1
+//     backward: dn = amplitude R(pos)^T dy,   dw = sum dn * x * r,   dx = r (w dn - x r^2 mean(w dn * x))   (sum for the second r, none for 1)
+// A head of a token is a row: LANES threads with one piece of 16 bytes each. The workgroup first makes the table of cosines and
+// sines of the tokens it takes, each angle once for all heads (an angle costs about as much as ten rows' pieces: position times frequency in 64 bits, whole turns
+// taken off there, so that far positions keep the float's precision), then its threads go over the rows of these tokens, queries and keys.
+// Bound by memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "lasp_block.h"
+
+namespace lasp {
+namespace {
+
+constexpr int kThreads = 256, kTable = 512;   // entries of the table: tokens times pairs
+
+struct QkCall {
+    int B, N, H, Hk, D, rot, half, norm, tokens, group;   // tokens of the call; of a group (one table)
+    long long ldq, ldk;                                    // elements between rows of the projections
+    float eps, amplitude;
+    const double *freq;
+    const int *pos;
+};
+
+struct Row {   // where a row lies
+    bool key;
+    size_t x, y;
+    int table;
+};
+DEVI Row place(const QkCall &c, int token, int slot, int head) {
+    const int b = token / c.N, s = token - b * c.N;
+    Row r;
+    r.key = head >= c.H;
+    const int h = r.key ? head - c.H : head, heads = r.key ? c.Hk : c.H;
+    r.x = (size_t)token * (r.key ? c.ldk : c.ldq) + h * c.D;
+    r.y = (((size_t)b * heads + h) * c.N + s) * c.D;
+    r.table = slot * (c.rot / 2);
+    return r;
+}
+DEVI void make_table(const QkCall &c, float2 *table, int token0, int count) {
+    const int pairs = c.rot / 2;
+    for (int e = threadIdx.x; e < count * pairs; e += kThreads) {
+        const int slot = e / pairs, i = e - slot * pairs, token = token0 + slot;
+        const int p = c.pos ? c.pos[token] : token % c.N;
+        double turns = (double)p * c.freq[i] * 0.15915494309189533577;
+        turns -= rint(turns);
+        float s, co;
+        sincospif(2.0f * (float)turns, &s, &co);
+        table[e] = float2{co * c.amplitude, s * c.amplitude};
+    }
+}
+
+// Sum over the threads of a row, in every one of them.
+template <int LANES>
+DEVI float row_sum(float v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// What a thread does to its piece of a row: features at .. at + W - 1.
+template <typename T, int LANES>
+struct Turn {
+    static constexpr int W = Piece<T>::W;
+    int at, other;   // first feature; lane of the piece that holds the pairs' other features (layout by halves)
+    int first;       // first pair of the piece, -1: it is not rotated
+    bool low;        // the piece holds the pairs' first features
+    DEVI Turn(const QkCall &c, int lane) {
+        at = lane * W;
+        const int pairs = c.rot / 2;
+        first = at >= c.rot ? -1 : !c.half ? at / 2 : at < pairs ? at : at - pairs;
+        low = at < pairs;
+        other = c.half && first >= 0 ? lane + (low ? pairs / W : -(pairs / W)) : lane;
+        other += (int)(threadIdx.x & 63) - lane;
+    }
+    DEVI u32x4 partner(const QkCall &c, u32x4 v) const {   // every lane of the wave calls it
+        if (!c.half || c.rot == 0) return v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __shfl((int)v[i], other);
+        return v;
+    }
+    // own (and, by halves, the partner's) features turned; BACK: the other way
+    template <bool BACK>
+    DEVI void turn(const QkCall &c, const float2 *t, float (&own)[W], const float (&oth)[W]) const {
+        if (first < 0) return;
+        if (c.half) {
+#pragma unroll
+            for (int i = 0; i < W; i += 2) {
+                const f32x4 cs = *(const f32x4 *)(t + first + i);
+                const float sign = low != BACK ? -1.0f : 1.0f;
+                own[i] = own[i] * cs[0] + sign * (oth[i] * cs[1]);
+                own[i + 1] = own[i + 1] * cs[2] + sign * (oth[i + 1] * cs[3]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 4) {
+                const f32x4 cs = *(const f32x4 *)(t + first + i / 2);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float co = cs[2 * j], si = BACK ? -cs[2 * j + 1] : cs[2 * j + 1], a = own[i + 2 * j], b = own[i + 2 * j + 1];
+                    own[i + 2 * j] = a * co - b * si;
+                    own[i + 2 * j + 1] = a * si + b * co;
+                }
+            }
+        }
+    }
+};
+DEVI float scale_of(const QkCall &c, float squares) {
+    if (c.norm == 0) return 1.0f;
+    return 1.0f / __builtin_sqrtf((c.norm == 1 ? squares / (float)c.D : squares) + c.eps);
+}
+template <int W>
+DEVI void weights_of(const float *w, int at, bool has, float (&f)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) f[i] = 1.0f;
+    if (w && has) load_floats<W>(w + at, f);
+}
+
+template <typename T, int LANES, bool STREAM>
+__global__ __launch_bounds__(kThreads) void k_qk_fwd(const T *__restrict__ xq, const T *__restrict__ xk, const float *__restrict__ wq,
+                                                     const float *__restrict__ wk, T *__restrict__ yq, T *__restrict__ yk, QkCall c) {
+    using P = Piece<T>;
+    constexpr int W = P::W, ROWS = kThreads / LANES;
+    __shared__ __attribute__((aligned(16))) float2 table[kTable];
+    const int lane = threadIdx.x % LANES, heads = c.H + c.Hk;
+    const bool has = lane * W < c.D;
+    const Turn<T, LANES> my(c, lane);
+    const int at = has ? my.at : 0;
+    // the weights of this piece and of its partner's, for queries and keys
+    float w[2][W], wo[2][W];
+    weights_of<W>(wq, at, has, w[0]);
+    weights_of<W>(wk, at, has, w[1]);
+    const int ato = (my.other & (LANES - 1)) * W;
+    weights_of<W>(wq, ato, has && my.first >= 0, wo[0]);
+    weights_of<W>(wk, ato, has && my.first >= 0, wo[1]);
+    for (int token0 = blockIdx.x * c.group; token0 < c.tokens; token0 += gridDim.x * c.group) {
+        const int count = min(c.group, c.tokens - token0);
+        if (c.rot) {
+            __syncthreads();   // the table has been read
+            make_table(c, table, token0, count);
+            __syncthreads();
+        }
+        for (int r0 = 0; r0 < count * heads; r0 += ROWS) {   // (all threads take part in every turn: the sums want whole waves)
+            const int r = r0 + threadIdx.x / LANES;
+            const bool there = r < count * heads;
+            const int slot = there ? r / heads : 0, head = there ? r - slot * heads : 0;
+            const Row row = place(c, token0 + slot, slot, head);
+            const u32x4 v = gload<u32x4, STREAM>((row.key ? xk : xq) + row.x + at, 0);
+            float f[W], g[W], s = 0.0f;
+            P::unpack(v, f);
+#pragma unroll
+            for (int i = 0; i < W; ++i) s = __builtin_fmaf(f[i], f[i], s);
+            const float k = scale_of(c, row_sum<LANES>(has ? s : 0.0f));
+            P::unpack(my.partner(c, v), g);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                f[i] *= k * (row.key ? w[1][i] : w[0][i]);
+                g[i] *= k * (row.key ? wo[1][i] : wo[0][i]);
+            }
+            my.template turn<false>(c, table + row.table, f, g);
+            if (there && has) put<STREAM>((row.key ? yk : yq) + row.y + at, P::pack(f));
+        }
+    }
+}
+
+template <typename T, int LANES, bool STREAM>
+__global__ __launch_bounds__(kThreads) void k_qk_bwd(const T *__restrict__ xq, const T *__restrict__ xk, const float *__restrict__ wq,
+                                                     const float *__restrict__ wk, const T *__restrict__ dyq, const T *__restrict__ dyk,
+                                                     T *__restrict__ dxq, T *__restrict__ dxk, float *__restrict__ pq, float *__restrict__ pk, QkCall c) {
+    using P = Piece<T>;
+    constexpr int W = P::W, ROWS = kThreads / LANES;
+    __shared__ __attribute__((aligned(16))) float2 table[kTable];
+    __shared__ __attribute__((aligned(16))) float part[kThreads / 64][LANES * W];
+    const int lane = threadIdx.x % LANES, heads = c.H + c.Hk;
+    const bool has = lane * W < c.D, sums = pq || pk, reads = c.norm != 0 || sums;
+    const Turn<T, LANES> my(c, lane);
+    const int at = has ? my.at : 0;
+    float w[2][W], acc[2][W] = {};
+    weights_of<W>(wq, at, has, w[0]);
+    weights_of<W>(wk, at, has, w[1]);
+    for (int token0 = blockIdx.x * c.group; token0 < c.tokens; token0 += gridDim.x * c.group) {
+        const int count = min(c.group, c.tokens - token0);
+        if (c.rot) {
+            __syncthreads();
+            make_table(c, table, token0, count);
+            __syncthreads();
+        }
+        for (int r0 = 0; r0 < count * heads; r0 += ROWS) {
+            const int r = r0 + threadIdx.x / LANES;
+            const bool there = r < count * heads;
+            const int slot = there ? r / heads : 0, head = there ? r - slot * heads : 0;
+            const Row row = place(c, token0 + slot, slot, head);
+            const u32x4 vy = gload<u32x4, STREAM>((row.key ? dyk : dyq) + row.y + at, 0);
+            u32x4 vx{0, 0, 0, 0};
+            if (reads) vx = gload<u32x4, STREAM>((row.key ? xk : xq) + row.x + at, 0);
+            float f[W], d[W], o[W], s = 0.0f, t = 0.0f;
+            P::unpack(vy, d);
+            P::unpack(my.partner(c, vy), o);
+            P::unpack(vx, f);
+            my.template turn<true>(c, table + row.table, d, o);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                o[i] = d[i] * (row.key ? w[1][i] : w[0][i]);
+                s = __builtin_fmaf(f[i], f[i], s);
+                t = __builtin_fmaf(o[i], f[i], t);
+            }
+            float k = 1.0f, mean = 0.0f;
+            if (c.norm != 0) {
+                k = scale_of(c, row_sum<LANES>(has ? s : 0.0f));
+                mean = row_sum<LANES>(has ? t : 0.0f) * k * k;
+                if (c.norm == 1) mean /= (float)c.D;
+            }
+            if (there && has) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float n = d[i] * (f[i] * k);   // (one of the two sums: a select instead of a branch)
+                    acc[0][i] += row.key ? 0.0f : n;
+                    acc[1][i] += row.key ? n : 0.0f;
+                    o[i] = k * (o[i] - f[i] * mean);
+                }
+                put<STREAM>((row.key ? dxk : dxq) + row.x + at, P::pack(o));
+            }
+        }
+    }
+    // a partial row per workgroup: the rows of a wave by shuffles, the waves in LDS, in a fixed order
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        float *to = n ? pk : pq;
+        if (!to) continue;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int d = LANES; d < 64; d *= 2) acc[n][i] += __shfl_xor(acc[n][i], d);
+        __syncthreads();
+        if ((threadIdx.x & 63) < LANES) store_floats<W>(&part[threadIdx.x >> 6][lane * W], acc[n]);
+        __syncthreads();
+        for (int e = threadIdx.x; e < c.D; e += kThreads) to[(size_t)blockIdx.x * c.D + e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+    }
+}
+
+constexpr int kCus = 256;
+// Tokens of a group: as many as the table holds, and no more than leave four workgroups a CU something to do.
+int group_of(const QkPlan &p) {
+    const long long tokens = (long long)p.B * p.N;
+    const long long room = p.rot ? kTable / (p.rot / 2) : 8;
+    return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(room, 8), tokens / (4 * kCus)));
+}
+int workgroups(const QkPlan &p, int a_cu) {
+    const long long tokens = (long long)p.B * p.N, g = group_of(p);
+    return (int)std::min<long long>((tokens + g - 1) / g, (long long)a_cu * kCus);
+}
+constexpr int kForwardACu = 8, kBackwardACu = 4;
+QkCall call_of(const QkPlan &p, const QkArgs &a) {
+    return {p.B, p.N, p.H, p.Hk, p.D, p.rot, p.half, p.norm, p.B * p.N, group_of(p), p.ldq, p.ldk, a.eps, a.amplitude, a.freq, a.pos};
+}
+// f.template operator()<T, LANES, STREAM>()
+template <typename T, bool STREAM, typename F>
+void by_lanes(int n, F f) {
+    if (n <= 1) f.template operator()<T, 1, STREAM>();
+    else if (n <= 2) f.template operator()<T, 2, STREAM>();
+    else if (n <= 4) f.template operator()<T, 4, STREAM>();
+    else if (n <= 8) f.template operator()<T, 8, STREAM>();
+    else if (n <= 16) f.template operator()<T, 16, STREAM>();
+    else if (n <= 32) f.template operator()<T, 32, STREAM>();
+    else if constexpr (sizeof(T) == 4) f.template operator()<T, 64, STREAM>();   // (two-byte rows have 32 pieces at most)
+}
+template <typename F>
+hipError_t by_plan(const QkPlan &p, int tensors, F f) {
+    const size_t bytes = (size_t)tensors * p.B * p.N * (p.H + p.Hk) * p.D * (p.dtype == 0 ? 4 : 2);
+    if (p.dtype == 0) past_cache(bytes) ? by_lanes<float, true>(p.D / 4, f) : by_lanes<float, false>(p.D / 4, f);
+    else past_cache(bytes) ? by_lanes<bf16_t, true>(p.D / 8, f) : by_lanes<bf16_t, false>(p.D / 8, f);
+    return hipGetLastError();
+}
+struct QkFwd {
+    const QkPlan &p;
+    const QkArgs &a;
+    hipStream_t s;
+    template <typename T, int LANES, bool STREAM>
+    void operator()() const {
+        k_qk_fwd<T, LANES, STREAM><<<dim3(workgroups(p, kForwardACu)), dim3(kThreads), 0, s>>>(
+            (const T *)a.xq, (const T *)a.xk, a.wq, a.wk, (T *)a.q, (T *)a.k, call_of(p, a));
+    }
+};
+struct QkBwd {
+    const QkPlan &p;
+    const QkArgs &a;
+    hipStream_t s;
+    template <typename T, int LANES, bool STREAM>
+    void operator()() const {
+        const int n = workgroups(p, kBackwardACu);
+        k_qk_bwd<T, LANES, STREAM><<<dim3(n), dim3(kThreads), 0, s>>>(
+            (const T *)a.xq, (const T *)a.xk, a.wq, a.wk, (const T *)a.dq, (const T *)a.dk, (T *)a.dxq, (T *)a.dxk,
+            a.dwq ? a.scratch : nullptr, a.dwk ? a.scratch + (size_t)n * p.D : nullptr, call_of(p, a));
+    }
+};
+
+}  // namespace
+
+size_t qk_scratch(const QkPlan &p) { return 2 * (size_t)workgroups(p, kBackwardACu) * p.D * sizeof(float); }
+
+hipError_t launch_qk_fwd(const QkPlan &p, const QkArgs &a, hipStream_t s) { return by_plan(p, 2, QkFwd{p, a, s}); }
+hipError_t launch_qk_bwd(const QkPlan &p, const QkArgs &a, hipStream_t s) {
+    if (hipError_t e = by_plan(p, 3, QkBwd{p, a, s}); e != hipSuccess) return e;
+    const int n = workgroups(p, kBackwardACu);
+    return launch_column_sums(a.scratch, a.dwq, a.scratch + (size_t)n * p.D, a.dwk, n, p.D, s);
+}
+
+}  // namespace lasp

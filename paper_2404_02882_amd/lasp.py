@@ -45,6 +45,10 @@ class DeltaShape(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("Dv", ctypes.c_int32), ("key_heads", ctypes.c_int32)]
 
 
+class QkShape(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "N", "H", "key_heads", "D", "dtype", "norm", "rot", "layout", "ld")]
+
+
 class LaspError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -162,7 +166,18 @@ def _bind_delta(handle):
     return handle
 
 
-lib = _bind_delta(_bind_blocks(_bind_bidir_sequence(_bind(ctypes.CDLL(LIB_PATH)))))
+def _bind_qk(handle):
+    """The same for norms and rotation of queries and keys."""
+    qk, f, d = ctypes.POINTER(QkShape), ctypes.c_float, ctypes.c_double
+    handle.lasp_check_qk.argtypes = handle.lasp_qk_scratch_bytes.argtypes = [qk]
+    handle.lasp_qk_scratch_bytes.restype = _sz
+    handle.lasp_qk_fwd.argtypes = [qk] + [_vp] * 4 + [f] + [_vp] * 2 + [f] + [_vp] * 3
+    handle.lasp_qk_bwd.argtypes = [qk] + [_vp] * 4 + [f] + [_vp] * 2 + [f] + [_vp] * 7 + [_sz, _vp]
+    handle.lasp_rope_frequencies.argtypes = [ctypes.c_int32, d, ctypes.c_int32] + [d] * 4 + [_vp]
+    return handle
+
+
+lib = _bind_qk(_bind_delta(_bind_blocks(_bind_bidir_sequence(_bind(ctypes.CDLL(LIB_PATH))))))
 
 
 def profile_begin(max_calls: int) -> None:
@@ -622,6 +637,67 @@ def lasp_gatenorm_bwd(shape: GateShape, o, u, weight, eps, dy, do, du, dweight, 
           _addr_rows(u, "u", B, N, C, shape.ld, d, at), _addr(weight, "weight", C, f, at), eps, _addr(dy, "dy", n, d, at),
           _addr(do, "do", n, d, at), _addr_rows(du, "du", B, N, C, shape.ld, d, at), _addr(dweight, "dweight", C, f, at),
           *_room(scratch, at))
+
+
+# ---- Queries and keys: norm, rotation, heads first ----------------------------------
+NORMS = {"none": 0, "rms": 1, "l2": 2}
+ROTATIONS = {"half": 0, "interleaved": 1}
+ROPES = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+def make_qk_shape(B, N, H, key_heads, D, dtype, norm="rms", rot=0, layout="half", ld=0) -> QkShape:
+    """norm: one of NORMS, layout: one of ROTATIONS (unknown names are refused by the calls)."""
+    return QkShape(int(B), int(N), int(H), int(key_heads), int(D), _dtype_code(dtype), NORMS.get(norm, -1), int(rot), ROTATIONS.get(layout, -1),
+                   int(ld))
+
+
+def check_qk(shape: QkShape) -> int:
+    return int(lib.lasp_check_qk(ctypes.byref(shape)))
+
+
+def qk_scratch_bytes(shape: QkShape) -> int:
+    return int(lib.lasp_qk_scratch_bytes(ctypes.byref(shape)))
+
+
+def rope_frequencies(rot, base=10000.0, scaling="none", factor=1.0, trained=4096.0, few_turns=1.0, many_turns=32.0, device="cuda") -> torch.Tensor:
+    """float64 [rot/2], radians per position, for lasp_qk_fwd; scaling: one of ROPES, for a context `factor` times the `trained` one."""
+    freq = torch.empty(max(int(rot), 0) // 2, dtype=torch.float64)
+    rc = lib.lasp_rope_frequencies(int(rot), float(base), ROPES.get(scaling, -1), float(factor), float(trained), float(few_turns),
+                                   float(many_turns), freq.data_ptr() or None)
+    if rc != 0:
+        raise LaspError(rc, "rope_frequencies")
+    return freq.to(device)
+
+
+def _qk_args(shape: QkShape, xq, xk, wq, wk, freq, pos, at, d):
+    """Addresses of what both calls read."""
+    B, N, D, f = shape.B, shape.N, shape.D, torch.float32
+    keys = shape.key_heads > 0
+    return (_addr_rows(xq, "xq", B, N, shape.H * D, shape.ld, d, at),
+            _addr_rows(xk, "xk", B, N, shape.key_heads * D, shape.ld, d, at) if keys else None, _addr(wq, "wq", D, f, at),
+            _addr(wk, "wk", D, f, at) if keys else None, _addr(freq, "freq", shape.rot // 2, torch.float64, at) if shape.rot else None,
+            _addr(pos, "pos", B * N, torch.int32, at) if shape.rot else None)
+
+
+def lasp_qk_fwd(shape: QkShape, xq, xk, wq, wk, eps, freq, pos, amplitude, q, k, stream=None) -> None:
+    """Norm and rotation by head: xq [B,N,H*D], xk [B,N,key_heads*D] (rows shape.ld apart) to q [B,H,N,D], k [B,key_heads,N,D]; wq, wk float32
+    [D] or None, freq float64 [rot/2] (rope_frequencies), pos int32 [B,N] or None; raises LaspError on a non-zero status."""
+    (d, at), n = _home(xq, "lasp_qk_fwd", shape, check_qk), shape.B * shape.N * shape.D
+    xq, xk, wq, wk, freq, pos = _qk_args(shape, xq, xk, wq, wk, freq, pos, at, d)
+    _call(lib.lasp_qk_fwd, "lasp_qk_fwd", at, stream, ctypes.byref(shape), xq, xk, wq, wk, eps, freq, pos, amplitude,
+          _addr(q, "q", n * shape.H, d, at), _addr(k, "k", n * shape.key_heads, d, at) if shape.key_heads else None)
+
+
+def lasp_qk_bwd(shape: QkShape, xq, xk, wq, wk, eps, freq, pos, amplitude, dq, dk, dxq, dxk, dwq, dwk, scratch, stream=None) -> None:
+    """Gradients dxq, dxk (as xq, xk), dwq, dwk (may be None, scratch then too) of lasp_qk_fwd; raises LaspError on a non-zero status."""
+    (d, at), n, f = _home(dq, "lasp_qk_bwd", shape, check_qk), shape.B * shape.N * shape.D, torch.float32
+    B, N, D, keys = shape.B, shape.N, shape.D, shape.key_heads > 0
+    xq, xk, wq, wk, freq, pos = _qk_args(shape, xq, xk, wq, wk, freq, pos, at, d)
+    _call(lib.lasp_qk_bwd, "lasp_qk_bwd", at, stream, ctypes.byref(shape), xq, xk, wq, wk, eps, freq, pos, amplitude,
+          _addr(dq, "dq", n * shape.H, d, at), _addr(dk, "dk", n * shape.key_heads, d, at) if keys else None,
+          _addr_rows(dxq, "dxq", B, N, shape.H * D, shape.ld, d, at),
+          _addr_rows(dxk, "dxk", B, N, shape.key_heads * D, shape.ld, d, at) if keys else None, _addr(dwq, "dwq", D, f, at),
+          _addr(dwk, "dwk", D, f, at) if keys else None, *_room(scratch, at))
 
 
 # ---- The gated delta rule ---------------------------------------------------------
