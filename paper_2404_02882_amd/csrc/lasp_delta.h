@@ -9,12 +9,12 @@
 
 namespace lasp {
 
-constexpr int kDeltaCols = 64;      // value features that a workgroup carries the state of
+constexpr int kDeltaTile = 32;         // tokens of a walk's tile
 constexpr int kDeltaStepTokens = 16;   // forward calls up to this length, without a cache, run token by token
 
 struct DeltaPlan {
     int B, H, N, D, Dv, dtype, key_heads;
-    int tile, tiles;          // tokens of a tile; tiles of a sequence
+    int tiles, grad_tiles;    // tiles of a sequence; those that the gradients are computed in
     int segments, seg_tiles;  // segments a sequence is cut into, tiles of one
 };
 DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_heads);

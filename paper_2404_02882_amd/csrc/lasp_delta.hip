@@ -36,13 +36,15 @@ template <typename T>
 struct Parts;
 template <>
 struct Parts<bf16_t> {
-    static constexpr int DATA = 1, MADE = 2, C = 64;   // parts of an input and of what is computed; tokens of a tile
+    // parts of an input and of what is computed; tiles of the walks that k_delta_grad takes at a time
+    static constexpr int DATA = 1, MADE = 2, GRAD_TILES = 2;
 };
 template <>
 struct Parts<float> {
-    static constexpr int DATA = 3, MADE = 3, C = 32;
+    static constexpr int DATA = 3, MADE = 3, GRAD_TILES = 1;
 };
 constexpr int kThreads = 256, kWaves = 4;
+constexpr int kTile = kDeltaTile;   // tokens of a walk's tile: one block of an MFMA
 
 template <int NP>
 struct Frags {
@@ -60,6 +62,131 @@ DEVI f32x16 mm(const Frags<NA> &a, const Frags<NB> &b, f32x16 c) {
 }
 
 constexpr int ld_of(int width) { return width == 128 ? kSwzLd : width + E::PAD; }
+
+// Two transposing reads: lane i of 16 gets column i of the four rows that the lanes point to in pieces of four.
+DEVI bf16x8 transposed(const bf16_t *lo, const bf16_t *hi) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    union {
+        struct {
+            s16x4 a, b;
+        } s;
+        bf16x8 v;
+    } u;
+    u.s.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lo);
+    u.s.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)hi);
+    return u.v;
+}
+// Eight values in parts, by pairs: element by element the compiler converts every one of them twice.
+template <int NP>
+DEVI Frags<NP> split(const f32x8 &x) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    u32x4 d[NP];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f32x2 y{x[2 * e], x[2 * e + 1]};
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(y, bf16x2));
+            d[i][e] = u;
+            if (i + 1 < NP) y -= f32x2{__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)};
+        }
+    }
+    Frags<NP> f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) f.p[i] = __builtin_bit_cast(bf16x8, d[i]);
+    return f;
+}
+// Rows 16 m .. 16 m + 15 of an accumulator tile as the fragment of sub-step m (contraction along the rows).
+template <int NP>
+DEVI Frags<NP> split(const f32x16 &t, int m) {
+    f32x8 x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = t[8 * m + e];
+    return split<NP>(x);
+}
+// Four values in parts, to LDS or memory: part i at `at` + i PS.
+template <int NP, int PS>
+DEVI void store_parts(bf16_t *at, f32x4 v) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    f32x2 y[2] = {{v[0], v[1]}, {v[2], v[3]}};
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        u32x2 d;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            d[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(y[e], bf16x2));
+            if (i + 1 < NP) y[e] -= f32x2{__uint_as_float(d[e] << 16), __uint_as_float(d[e] & 0xffff0000u)};
+        }
+        *(u32x2 *)(at + i * PS) = d;
+    }
+}
+
+// What the lanes of a wave wrote to LDS is there for its other lanes.
+DEVI void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A square of 32 by 32: NP parts, PS elements apart.
+template <int NP, int PART = 1024>
+struct Block {
+    static constexpr int PS = PART, BYTES = NP * PS * 2;
+    bf16_t *p;
+    DEVI Frags<NP> kc(const Lane &ln, int k0) const {
+        Frags<NP> f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f.p[i] = E::ld_kc(ln, p + i * PS, kBlockLd, 0, k0);
+        return f;
+    }
+    DEVI Frags<NP> ks(const Lane &ln, int k0) const {
+        Frags<NP> f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f.p[i] = E::ld_ks(ln, p + i * PS, kBlockLd, k0, 0);
+        return f;
+    }
+    // contraction in the order in which an accumulator tile enumerates its rows, sub-step m
+    DEVI Frags<NP> kp(const Lane &ln, int m) const {
+        const bf16_t *at = p + ln.r * 32 + 4 * ln.h;
+        const int sw = swz4(ln.r);
+        Frags<NP> f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            union {
+                struct {
+                    bf16x4 a, b;
+                } s;
+                bf16x8 v;
+            } u;
+            u.s.a = *(const bf16x4 *)(at + i * PS + (((2 * m) ^ sw) << 3));
+            u.s.b = *(const bf16x4 *)(at + i * PS + (((2 * m + 1) ^ sw) << 3));
+            f.p[i] = u.v;
+        }
+        return f;
+    }
+    DEVI Frags<NP> ksp(const Lane &ln, int m) const {
+        const int l16 = ln.id & 15, row = 16 * m + 4 * ln.h + (l16 >> 2), col = (ln.id & 16) + 4 * (l16 & 3);
+        const bf16_t *lo = p + lds_off(kBlockLd, row, col), *hi = p + lds_off(kBlockLd, row + 8, col);
+        Frags<NP> f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f.p[i] = transposed(lo + i * PS, hi + i * PS);
+        return f;
+    }
+    DEVI void st4(int row, int col, f32x4 v) const { store_parts<NP, PS>(p + lds_off(kBlockLd, row, col), v); }
+    DEVI void st_acc(const Lane &ln, const f32x16 &t) const {   // (transposed, as Tile's)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) st4(ln.r, 8 * g + 4 * ln.h, f32x4{t[4 * g], t[4 * g + 1], t[4 * g + 2], t[4 * g + 3]});
+    }
+};
+// A lower triangular square of C tokens: its blocks (0,0), (1,0), (1,1).
+template <int NP, int C>
+struct Lower {
+    static constexpr int NB = C / 32, BLOCKS = NB * (NB + 1) / 2, PS = BLOCKS * 1024, BYTES = NP * PS * 2;
+    bf16_t *p;
+    DEVI Block<NP, PS> at(int it, int jt) const { return {p + (it * (it + 1) / 2 + jt) * 1024}; }
+};
 
 // A tile in LDS: NP parts of ROWS rows of WIDTH bfloat16.
 template <int NP, int ROWS, int WIDTH>
@@ -80,13 +207,7 @@ struct Tile {
         return f;
     }
     DEVI void st4(int row, int col, f32x4 v) const {
-        bf16_t *at = p + lds_off(LD, row, col);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const bf16x4 b = __builtin_convertvector(v, bf16x4);
-            *(bf16x4 *)(at + i * PS) = b;
-            if (i + 1 < NP) v -= __builtin_convertvector(b, f32x4);
-        }
+        store_parts<NP, PS>(p + lds_off(LD, row, col), v);
     }
     DEVI f32x4 get4(int row, int col) const {
         const bf16_t *at = p + lds_off(LD, row, col);
@@ -95,6 +216,21 @@ struct Tile {
         for (int i = NP - 1; i >= 0; --i) v += __builtin_convertvector(*(const bf16x4 *)(at + i * PS), f32x4);
         return v;
     }
+    // contraction in the order in which an accumulator tile enumerates its rows: sub-step m of the 32 from k0
+    DEVI Frags<NP> kp(const Lane &ln, int row0, int k0, int m) const {
+        Frags<NP> f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f.p[i] = E::ld_kp(ln, p + i * PS, LD, row0, k0, m);
+        return f;
+    }
+    DEVI Frags<NP> ksp(const Lane &ln, int k0, int col0, int m) const {
+        const int l16 = ln.id & 15, row = k0 + 16 * m + 4 * ln.h + (l16 >> 2), col = col0 + (ln.id & 16) + 4 * (l16 & 3);
+        const bf16_t *lo = p + lds_off(LD, row, col), *hi = p + lds_off(LD, row + 8, col);
+        Frags<NP> f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f.p[i] = transposed(lo + i * PS, hi + i * PS);
+        return f;
+    }
     // an accumulator tile, transposed: its column r is row row0 + r here, its rows are columns col0 ..
     DEVI void st_acc(const Lane &ln, int row0, int col0, const f32x16 &t) const {
 #pragma unroll
@@ -102,66 +238,52 @@ struct Tile {
     }
 };
 
-// Rows of a global tensor on their way to a tile: 16 bytes a thread and piece. Rows from `valid` on are zeros.
-template <typename T, int ROWS, int WIDTH>
+// Rows of a global tensor on their way to a tile: 16 bytes a thread (of NT) and piece. Rows from `valid` on are zeros.
+template <typename T, int ROWS, int WIDTH, int NT>
 struct Fetch {
-    static constexpr int EPC = 16 / sizeof(T), CPR = WIDTH / EPC, N = ROWS * CPR / kThreads;
-    static_assert(N * kThreads == ROWS * CPR, "whole pieces");
+    static constexpr int EPC = 16 / sizeof(T), CPR = WIDTH / EPC, PIECES = ROWS * CPR, N = (PIECES + NT - 1) / NT;
     u32x4 v[N];
     DEVI void load(const T *base, size_t ld, int valid) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int c = threadIdx.x + n * kThreads, row = c / CPR, col = (c % CPR) * EPC;
+            const int c = threadIdx.x + n * NT, row = c / CPR, col = (c % CPR) * EPC;
             v[n] = u32x4{0, 0, 0, 0};
-            if (row < valid) v[n] = *(const u32x4 *)(base + row * ld + col);
+            if (row < valid) v[n] = *(const u32x4 *)(base + row * ld + col);   // (valid <= ROWS)
         }
     }
     template <typename F>
     DEVI void each(F f) const {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int c = threadIdx.x + n * kThreads;
-            f(c / CPR, (c % CPR) * EPC, v[n]);
+            const int c = threadIdx.x + n * NT;
+            if (PIECES % NT == 0 || c < PIECES) f(n, c / CPR, (c % CPR) * EPC, v[n]);
         }
     }
     template <typename Tl>
     DEVI void store(const Tl &t) const {
-        each([&](int row, int col, u32x4 x) {
+        each([&](int, int row, int col, u32x4 x) {
             if constexpr (sizeof(T) == 2) *(u32x4 *)(t.p + lds_off(Tl::LD, row, col)) = x;
             else t.st4(row, col, __builtin_bit_cast(f32x4, x));
         });
     }
-    // every row times its weight
-    template <typename Tl>
-    DEVI void store_scaled(const Tl &t, const float *w) const {
-        each([&](int row, int col, u32x4 x) {
-            if constexpr (sizeof(T) == 2) {
-                const f32x8 f = __builtin_convertvector(__builtin_bit_cast(bf16x8, x), f32x8) * w[row];
-                t.st4(row, col, __builtin_shufflevector(f, f, 0, 1, 2, 3));
-                t.st4(row, col + 4, __builtin_shufflevector(f, f, 4, 5, 6, 7));
-            } else {
-                t.st4(row, col, __builtin_bit_cast(f32x4, x) * w[row]);
-            }
-        });
-    }
 };
-// N of a tile, as k_delta_prep leaves it: its parts one after the other.
-template <int NP, int C>
-struct FetchParts {
-    static constexpr int PIECES = NP * C * C / 8, N = (PIECES + kThreads - 1) / kThreads;
+// BYTES that lie in LDS as they do in global memory.
+template <int BYTES, int NT>
+struct Copy {
+    static constexpr int PIECES = BYTES / 16, N = (PIECES + NT - 1) / NT;
     u32x4 v[N];
-    DEVI void load(const bf16_t *base) {
+    DEVI void load(const void *base) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int c = threadIdx.x + n * kThreads;
-            if (c < PIECES) v[n] = *(const u32x4 *)(base + c * 8);
+            const int c = threadIdx.x + n * NT;
+            if (PIECES % NT == 0 || c < PIECES) v[n] = ((const u32x4 *)base)[c];
         }
     }
-    DEVI void store(const Tile<NP, C, C> &t) const {
+    DEVI void store(void *to) const {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int c = threadIdx.x + n * kThreads;
-            if (c < PIECES) *(u32x4 *)(t.p + c / (C * C / 8) * Tile<NP, C, C>::PS + c / (C / 8) % C * Tile<NP, C, C>::LD + c % (C / 8) * 8) = v[n];
+            const int c = threadIdx.x + n * NT;
+            if (PIECES % NT == 0 || c < PIECES) ((u32x4 *)to)[c] = v[n];
         }
     }
 };
@@ -191,47 +313,27 @@ DEVI void store_acc(T *p, const Lane &ln, const f32x16 &x) {
     }
 }
 
-// The gates of a tile. Logarithms are summed in 64 bits and to base 2: the sum over a tile may be large where a difference is small.
+// The gates of C tokens. Logarithms are summed in 64 bits and to base 2: the sum over a tile may be large where a difference is small.
 // From 2^-300 on (-infinity among them: the state starts anew) a gate counts as 2^-300, whose power is 0 as a float, so that
 // differences of sums stay numbers.
-template <int C>
-struct Gates {
-    double sum[C];
-    float start[C], rest[C], beta[C];   // exp(G_i), exp(G_C - G_i)
-    float whole;
-};
-struct GateIn {
-    float log_g, beta;
-    DEVI void load(const float *lg, const float *b, int valid, int lane) {
-        log_g = lg && lane < valid ? lg[lane] : 0.0f;
-        beta = lane < valid ? b[lane] : 0.0f;
-    }
-};
 DEVI double to_base2(float log_g) {
     const double x = (double)log_g * 1.4426950408889634;
     return x < -300.0 ? -300.0 : x;   // (NaN stays)
 }
+DEVI float power(double d) { return __builtin_amdgcn_exp2f((float)d); }
+// Sums over the lanes of C up to this one.
 template <int C>
-DEVI void make_gates(Gates<C> &g, const GateIn &in, int lane) {   // one wave
-    double x = to_base2(in.log_g);
+DEVI double sum_up(double x, int lane) {
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
         const double y = __shfl_up(x, d, C);
         if ((lane & (C - 1)) >= d) x += y;
     }
-    const double all = __shfl(x, C - 1, C);
-    if (lane < C) {
-        g.sum[lane] = x;
-        g.start[lane] = __builtin_amdgcn_exp2f((float)x);
-        g.rest[lane] = __builtin_amdgcn_exp2f((float)(all - x));
-        g.beta[lane] = in.beta;
-    }
-    if (lane == 0) g.whole = __builtin_amdgcn_exp2f((float)all);
+    return x;
 }
-DEVI float power(double d) { return __builtin_amdgcn_exp2f((float)d); }
 
 struct DeltaCall {
-    int B, H, Hk, N, Dv, tiles, segments, seg_tiles;
+    int B, H, Hk, N, Dv, tiles, segments, seg_tiles, grad_tiles;
     const float *log_g, *beta;
     const int *len;
     // tokens of sequence b from token0 on, 0 .. most
@@ -242,49 +344,84 @@ struct DeltaCall {
     DEVI size_t key_row(int b, int h) const { return ((size_t)b * Hk + h / (H / Hk)) * N; }   // first row of a head of q, k
 };
 
+// What k_delta_prep leaves of a tile: N, scores P (a row per query), and by token exp(G_i), exp(G_C - G_i), beta_i, and (every one the same) exp(G_C).
+template <typename T>
+struct Prepared {
+    typedef Block<Parts<T>::MADE> Square;
+    static constexpr int N = 0, P = Square::BYTES, START = 2 * Square::BYTES, REST = START + 4 * kTile, BETA = REST + 4 * kTile, WHOLE = BETA + 4 * kTile,
+                         BYTES = WHOLE + 4 * kTile;
+};
+
 // ---------------------------------------------------------------------------
-// k_delta_prep: N of a tile. Blocks of 16 by substitution, a thread per column; then joined to twice the size,
+// k_delta_prep: a wave per tile, keys and queries straight into operands. N in blocks of 16 by substitution, a lane per column; then joined,
 //     N21 = -(I + N22 beta) M21 (I + beta N11).
 // ---------------------------------------------------------------------------
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void k_delta_prep(const T *__restrict__ K, bf16_t *__restrict__ inv, DeltaCall a) {
-    using P = Parts<T>;
-    constexpr int C = P::C, LDM = C + 4;
-    typedef Tile<P::DATA, C, D> KTile;
-    __shared__ __attribute__((aligned(16))) unsigned char lds_k[KTile::BYTES];
-    __shared__ __attribute__((aligned(16))) float M[C * LDM], Nn[C * LDM];
-    __shared__ Gates<C> g;
-    const KTile kt{(bf16_t *)lds_k};
-    const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6, tile = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * C;
-    const int valid = a.valid(b, token0, C);
-    Fetch<T, C, D> fk;
-    fk.load(K + (a.key_row(b, h) + token0) * D, D, valid);
-    if (wave == 0) {
-        GateIn in;
-        in.load(a.log_g ? a.log_g + (size_t)bh * a.N + token0 : nullptr, a.beta + (size_t)bh * a.N + token0, valid, ln.id);
-        make_gates<C>(g, in, ln.id);
-    }
-    fk.store(kt);
-    __syncthreads();
-    constexpr int NT = C / 32;
-    if (wave < NT * NT && wave % NT <= wave / NT) {
-        const int it = wave / NT, jt = wave % NT;
-        f32x16 m = {};
+DEVI void operands(Frags<Parts<T>::DATA> (&f)[D / 16], const T *row, const Lane &ln, bool there) {
 #pragma unroll
-        for (int k0 = 0; k0 < D; k0 += 16) m = mm<P::MADE>(kt.kc(ln, 32 * it, k0), kt.kc(ln, 32 * jt, k0), m);
-        const int j = 32 * jt + ln.r;
-        const double gj = g.sum[j];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int i = 32 * it + ln.acc_row(e);
-            M[i * LDM + j] = i > j ? m[e] * power(g.sum[i] - gj) : 0.0f;
+    for (int k = 0; k < D / 16; ++k) {
+        if constexpr (sizeof(T) == 2) {
+            u32x4 x{0, 0, 0, 0};
+            if (there) x = *(const u32x4 *)(row + 16 * k + 8 * ln.h);
+            f[k].p[0] = __builtin_bit_cast(bf16x8, x);
+        } else {
+            f32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+            if (there) {
+                x = *(const f32x4 *)(row + 16 * k + 8 * ln.h);
+                y = *(const f32x4 *)(row + 16 * k + 8 * ln.h + 4);
+            }
+            f[k] = split<3>(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
-    for (int c = threadIdx.x; c < C * C; c += kThreads) Nn[c / C * LDM + c % C] = 0.0f;
-    __syncthreads();
-    if (threadIdx.x < C) {
-        const int j = threadIdx.x, b0 = j & ~15, jj = j & 15;
+}
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict__ Q, const T *__restrict__ K, char *__restrict__ prepared, DeltaCall a) {
+    using P = Parts<T>;
+    using Pr = Prepared<T>;
+    constexpr int LDM = kTile + 4;
+    __shared__ __attribute__((aligned(16))) float lds_m[kWaves][kTile * LDM], lds_n[kWaves][kTile * LDM], lds_beta[kWaves][kTile];
+    __shared__ double lds_sum[kWaves][kTile];
+    const Lane ln(threadIdx.x);
+    const int wave = threadIdx.x >> 6, tile = blockIdx.x * kWaves + wave, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * kTile;
+    float *M = lds_m[wave], *N = lds_n[wave], *beta = lds_beta[wave];
+    double *sum = lds_sum[wave];
+    const int valid = tile < a.tiles ? a.valid(b, token0, kTile) : 0;
+    if (valid == 0) return;   // (no walk reads it; the waves share nothing)
+    const size_t key_row = a.key_row(b, h) + token0 + ln.r, gate = (size_t)bh * a.N + token0 + ln.r;
+    const bool there = ln.r < valid;
+    Frags<P::DATA> fk[D / 16], fq[D / 16];
+    operands<T, D>(fk, K + key_row * D, ln, there);
+    operands<T, D>(fq, Q + key_row * D, ln, there);
+    const float bt = there ? a.beta[gate] : 0.0f;
+    const double x = sum_up<kTile>(a.log_g && there ? to_base2(a.log_g[gate]) : 0.0, ln.id), all = __shfl(x, kTile - 1, kTile);
+    char *to = prepared + ((size_t)bh * a.tiles + tile) * Pr::BYTES;
+    if (ln.h == 0) {
+        beta[ln.r] = bt;
+        sum[ln.r] = x;
+        ((float *)(to + Pr::START))[ln.r] = power(x);
+        ((float *)(to + Pr::REST))[ln.r] = power(all - x);
+        ((float *)(to + Pr::BETA))[ln.r] = bt;
+        ((float *)(to + Pr::WHOLE))[ln.r] = power(all);
+    }
+    f32x16 m = {}, p = {};   // k_i . k_j, a row per i;  q_i . k_j, a row per j
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        m = mm<P::MADE>(fk[k], fk[k], m);
+        p = mm<P::MADE>(fk[k], fq[k], p);
+    }
+    wave_sync();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int o = ln.acc_row(e);
+        const double d = x - sum[o];
+        M[o * LDM + ln.r] = o > ln.r ? m[e] * power(-d) : 0.0f;
+        p[e] = o <= ln.r ? p[e] * power(d) : 0.0f;
+    }
+    const typename Pr::Square pt{(bf16_t *)(to + Pr::P)}, nt{(bf16_t *)(to + Pr::N)};
+    pt.st_acc(ln, p);
+    wave_sync();
+    if (ln.h == 0) {
+        const int j = ln.r, b0 = j & ~15, jj = j & 15;
         float n[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -293,219 +430,200 @@ __global__ __launch_bounds__(kThreads) void k_delta_prep(const T *__restrict__ K
             for (int k = 0; k < 16; ++k)
                 if (k < i) s = __builtin_fmaf(M[(b0 + i) * LDM + b0 + k], n[k], s);
             s = i > jj ? -s : 0.0f;
-            Nn[(b0 + i) * LDM + j] = s;
-            n[i] = s * g.beta[b0 + i];
+            N[(b0 + i) * LDM + j] = s;
+            N[((b0 ^ 16) + i) * LDM + j] = 0.0f;   // (below the blocks: in place of what is joined next)
+            n[i] = s * beta[b0 + i];
         }
     }
-    __syncthreads();
+    wave_sync();
+    {
+        const int i = ln.id >> 2, j = 4 * (ln.id & 3);   // four columns of a row
+        f32x4 y = *(const f32x4 *)(M + (16 + i) * LDM + j);
 #pragma unroll
-    for (int s = 16; s < C; s *= 2) {
-        // pairs of blocks of s rows; 4 columns of a row a thread. First M21 (I + beta N11), in place of N21, then the other factor.
-        const int quads = s / 4, jobs = C / (2 * s) * s * quads;
-        const int job = threadIdx.x, pair = job / (s * quads), i = job / quads % s, j = 4 * (job % quads), r0 = 2 * s * pair;
-        static_assert(C / 2 * C / 8 <= kThreads, "a job a thread");
-        f32x4 y = {};
+        for (int k = 0; k < 16; ++k) y += (M[(16 + i) * LDM + k] * beta[k]) * *(const f32x4 *)(N + k * LDM + j);
+        *(f32x4 *)(N + (16 + i) * LDM + j) = y;
+        wave_sync();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (job < jobs) {
-                const float *m = half ? Nn + (r0 + s + i) * LDM + r0 + s : M + (r0 + s + i) * LDM + r0;
-                const float *n0 = half ? Nn + (r0 + s) * LDM + r0 + j : Nn + r0 * LDM + r0 + j;
-                const float *bt = g.beta + r0 + (half ? s : 0);
-                y = half ? *(const f32x4 *)(n0 + i * LDM) : *(const f32x4 *)(m + j);
-#pragma unroll 8
-                for (int k = 0; k < s; ++k) y += (m[k] * bt[k]) * *(const f32x4 *)(n0 + k * LDM);
-                if (half) y = -y;
-            }
-            __syncthreads();
-            if (job < jobs) *(f32x4 *)(Nn + (r0 + s + i) * LDM + r0 + j) = y;
-            __syncthreads();
-        }
+        for (int k = 0; k < 16; ++k) y += (N[(16 + i) * LDM + 16 + k] * beta[16 + k]) * *(const f32x4 *)(N + (16 + k) * LDM + j);
+        wave_sync();
+        *(f32x4 *)(N + (16 + i) * LDM + j) = -y;
+        wave_sync();
     }
-    bf16_t *to = inv + ((size_t)bh * a.tiles + tile) * (P::MADE * C * C);
-    for (int c = threadIdx.x; c < C * C / 4; c += kThreads) {
-        const int i = c / (C / 4), j = c % (C / 4) * 4;
-        f32x4 v = *(const f32x4 *)(Nn + i * LDM + j);
 #pragma unroll
-        for (int part = 0; part < P::MADE; ++part) {
-            const bf16x4 x = __builtin_convertvector(v, bf16x4);
-            *(bf16x4 *)(to + part * C * C + i * C + j) = x;
-            v -= __builtin_convertvector(x, f32x4);
-        }
-    }
+    for (int c = ln.id; c < kTile * kTile / 4; c += 64) nt.st4(c / 8, c % 8 * 4, *(const f32x4 *)(N + c / 8 * LDM + c % 8 * 4));
 }
 
-// Where a wave's accumulator tiles of the state lie: D / 32 by 2 tiles of 32 features of the key by 32 of the value.
-template <int D>
-struct StatePlace {
-    static constexpr int N = D == 128 ? 2 : 1;
-    int wave;
-    DEVI int key0(int s) const { return 32 * (N == 2 ? wave : wave >> 1); }
-    DEVI int col0(int s) const { return 32 * (N == 2 ? s : wave & 1); }
-};
-template <int D>
-DEVI void load_state(f32x16 (&S)[StatePlace<D>::N], const StatePlace<D> &at, const Lane &ln, const float *src, int ld) {
+// Waves a SIMD that a walk is compiled for: two, so that one computes while the other waits, where 256 registers are enough.
+template <typename T, int D, int DV>
+constexpr int waves_of() { return D == 128 && (sizeof(T) == 4 || DV == 64) ? 1 : 2; }
+
+// Values of a tile's rows in the order of an accumulator tile's rows, from LDS.
+DEVI f32x16 by_row(const float *w, const Lane &ln) {
+    f32x16 x;
 #pragma unroll
-    for (int s = 0; s < StatePlace<D>::N; ++s)
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *(const f32x4 *)(w + 8 * g + 4 * ln.h);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) S[s][e] = src ? src[(size_t)(at.key0(s) + ln.acc_row(e)) * ld + at.col0(s) + ln.r] : 0.0f;
+        for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
+    }
+    return x;
 }
-template <int D>
-DEVI void save_state(const f32x16 (&S)[StatePlace<D>::N], const StatePlace<D> &at, const Lane &ln, float *dst, int ld) {
+// Values of the lane's column in rows of LD elements, in the order of an accumulator tile's rows; `there`: rows that exist.
+template <int LD, typename T>
+DEVI f32x16 load_rows(const T *p, const Lane &ln, int there) {
+    f32x16 x;
+    p += 4 * ln.h * LD;
+    if (there >= 32)
 #pragma unroll
-    for (int s = 0; s < StatePlace<D>::N; ++s)
+        for (int e = 0; e < 16; ++e) x[e] = Elem<T>::ld1(p + (8 * (e >> 2) + (e & 3)) * LD);
+    else
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dst[(size_t)(at.key0(s) + ln.acc_row(e)) * ld + at.col0(s) + ln.r] = S[s][e];
+        for (int e = 0; e < 16; ++e) x[e] = ln.acc_row(e) < there ? Elem<T>::ld1(p + (8 * (e >> 2) + (e & 3)) * LD) : 0.0f;
+    return x;
+}
+template <int LD, typename T>
+DEVI void store_rows(T *p, const Lane &ln, int there, const f32x16 &x) {
+    p += 4 * ln.h * LD;
+    if (there >= 32)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) Elem<T>::st1(p + (8 * (e >> 2) + (e & 3)) * LD, x[e]);
+    else
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (ln.acc_row(e) < there) Elem<T>::st1(p + (8 * (e >> 2) + (e & 3)) * LD, x[e]);
+}
+// A wave's part of a state: KB blocks of 32 key features (rows) by its 32 columns (a lane each).
+template <int KB>
+DEVI void load_state(f32x16 (&S)[KB], const Lane &ln, const float *src, int ld) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) S[kb][e] = src ? src[(size_t)(32 * kb + ln.acc_row(e)) * ld + ln.r] : 0.0f;
+}
+template <int KB>
+DEVI void save_state(const f32x16 (&S)[KB], const Lane &ln, float *dst, int ld) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dst[(size_t)(32 * kb + ln.acc_row(e)) * ld + ln.r] = S[kb][e];
 }
 
 // ---------------------------------------------------------------------------
-// k_delta_walk. LOCAL: no outputs; the state a segment reaches from zero, and (column blocks behind those of the values) its
-// matrix T, which is the state reached from the identity without values.
+// k_delta_walk: a wave carries 32 columns of the state in its accumulators and meets no other wave's: what a product leaves in an
+// accumulator tile (a row per token or key feature, a lane per column) is the next one's operand as it lies there, with the contraction in the
+// order of the accumulator's rows; the waves share the tile's keys, queries, N and scores in LDS. LOCAL: no outputs; the state a segment reaches
+// from zero, and (waves behind those of the values) its matrix T, which is the state reached from the identity without values.
 // ---------------------------------------------------------------------------
-template <typename T, int D>
-struct WalkLds {
+template <typename T, int D, int DV, bool LOCAL>
+struct Walk {
     using P = Parts<T>;
-    static constexpr int C = P::C;
-    typedef Tile<P::DATA, C, D> Data;
-    typedef Tile<P::MADE, kDeltaCols, D> State;   // transposed: a row per column
-    typedef Tile<P::MADE, C, C> Square;
-    typedef Tile<P::MADE, C, kDeltaCols> Rows;
-    static constexpr int K = 0, S = K + Data::BYTES, NN = S + State::BYTES, X = NN + Square::BYTES, Z = X + Rows::BYTES, G = Z + Rows::BYTES,
-                         Q = G + (int)((sizeof(Gates<C>) + 15) / 16 * 16), PP = Q + Data::BYTES, Y = PP + Square::BYTES, ALL = Y + Rows::BYTES;
-    static constexpr int bytes(bool local) { return local ? Q : ALL; }
+    static constexpr int KB = D / 32, WAVES = (DV + (LOCAL ? D : 0)) / 32, NT = 64 * WAVES;
+    typedef Tile<P::DATA, kTile, D> Data;
+    static constexpr int PREP = 0, K = Prepared<T>::BYTES, Q = K + Data::BYTES, STAGE = LOCAL ? Q : Q + Data::BYTES, LDS = 2 * STAGE;
 };
 struct WalkStates {
     const float *first;   // states that segments start from ([head][segment], or kv_in where there is one segment); null = zeros
     float *last;          // kv_out
     float *local, *trans; // LOCAL
-    float *cache;         // the state in front of every tile; may be null
+    float *cache;         // the state in front of every tile that k_delta_grad takes; may be null
+    float *w;             // w of every token; goes with the cache
     int all_trans;        // T is wanted of the last segment too
 };
-template <typename T, int D, bool LOCAL>
-__global__ __launch_bounds__(kThreads, 1) void k_delta_walk(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
-                                                            const bf16_t *__restrict__ inv, T *__restrict__ O, WalkStates st, DeltaCall a) {
-    using P = Parts<T>;
-    using L = WalkLds<T, D>;
-    constexpr int C = P::C;
+template <typename T, int D, int DV, bool LOCAL>
+__global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())) void k_delta_walk(const T *__restrict__ Q, const T *__restrict__ K,
+                                                                              const T *__restrict__ V, const char *__restrict__ prepared,
+                                                                              T *__restrict__ O, WalkStates st, DeltaCall a) {
+    using L = Walk<T, D, DV, LOCAL>;
+    using P = typename L::P;
+    using Pr = Prepared<T>;
+    constexpr int KB = L::KB, MADE = P::MADE;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const typename L::Data kt{(bf16_t *)(lds + L::K)}, qt{(bf16_t *)(lds + L::Q)};
-    const typename L::State stt{(bf16_t *)(lds + L::S)};
-    const typename L::Square nt{(bf16_t *)(lds + L::NN)}, pt{(bf16_t *)(lds + L::PP)};
-    const typename L::Rows xt{(bf16_t *)(lds + L::X)}, yt{(bf16_t *)(lds + L::Y)}, zt{(bf16_t *)(lds + L::Z)};
-    Gates<C> &g = *(Gates<C> *)(lds + L::G);
     const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6;
-    const int blocks = a.Dv / kDeltaCols + (LOCAL ? D / kDeltaCols : 0);
-    const int cb = blockIdx.x % blocks, seg = blockIdx.x / blocks % a.segments, bh = blockIdx.x / (blocks * a.segments);
-    const int b = bh / a.H, h = bh - b * a.H;
-    const bool trans = LOCAL && cb >= a.Dv / kDeltaCols;
-    const int c0 = trans ? (cb - a.Dv / kDeltaCols) * kDeltaCols : cb * kDeltaCols;
-    if (LOCAL && seg == a.segments - 1 && !(trans && st.all_trans)) return;
-    const int t0 = seg * a.seg_tiles, t1 = min(a.tiles, t0 + a.seg_tiles);
+    const int wave = threadIdx.x >> 6, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
+    if (LOCAL && seg == a.segments - 1 && !st.all_trans) return;
+    const bool trans = LOCAL && wave >= DV / 32;
+    const int c0 = 32 * (trans ? wave - DV / 32 : wave);
+    const int tokens = a.valid(b, 0, a.N), end = min(a.tiles, (seg + 1) * a.seg_tiles);
+    const int t0 = seg * a.seg_tiles, t1 = min(end, (tokens + kTile - 1) / kTile);   // (tiles behind a sequence's end leave the state as it is)
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N;
-    const int ct = wave & 1, tt = wave >> 1;          // this wave's block of 32 columns and 32 tokens
-    const bool active = tt < C / 32;
-    const StatePlace<D> at{wave};
-    f32x16 S[StatePlace<D>::N];
+    f32x16 S[KB];
     if (trans) {
 #pragma unroll
-        for (int s = 0; s < StatePlace<D>::N; ++s)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[s][e] = at.key0(s) + ln.acc_row(e) == c0 + at.col0(s) + ln.r ? 1.0f : 0.0f;
+            for (int e = 0; e < 16; ++e) S[kb][e] = 32 * kb + ln.acc_row(e) == c0 + ln.r ? 1.0f : 0.0f;
     } else {
-        const float *from = LOCAL || !st.first ? nullptr : st.first + ((size_t)bh * a.segments + seg) * D * a.Dv + c0;
-        load_state<D>(S, at, ln, from, a.Dv);
+        load_state<KB>(S, ln, LOCAL || !st.first ? nullptr : st.first + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
     }
-#pragma unroll
-    for (int s = 0; s < StatePlace<D>::N; ++s) stt.st_acc(ln, at.col0(s), at.key0(s), S[s]);
-
-    Fetch<T, C, D> fk, fq;
-    FetchParts<P::MADE, C> fn;
+    Fetch<T, kTile, D, L::NT> fk, fq;
+    Copy<Pr::BYTES, L::NT> fp;
     f32x16 v = {};
-    GateIn gi{0.0f, 0.0f};
     auto fetch = [&](int t) {
-        const int token0 = t * C, valid = a.valid(b, token0, C);
+        const int token0 = t * kTile, valid = min(tokens - token0, kTile);
+        fp.load(prepared + ((size_t)bh * a.tiles + t) * Pr::BYTES);
         fk.load(K + (key_row + token0) * D, D, valid);
         if constexpr (!LOCAL) fq.load(Q + (key_row + token0) * D, D, valid);
-        fn.load(inv + ((size_t)bh * a.tiles + t) * (P::MADE * C * C));
-        const int i = 32 * tt + ln.r;
-        if (active && !trans) v = load_acc(V + (row + token0 + i) * a.Dv + c0 + 32 * ct, ln, i < valid);
-        if (wave == 0) gi.load(a.log_g ? a.log_g + row + token0 : nullptr, a.beta + row + token0, valid, ln.id);
+        if (!trans) v = load_rows<DV>(V + (row + token0) * DV + c0 + ln.r, ln, valid);
     };
-    fetch(t0);
+    if (t0 < t1) fetch(t0);
     for (int t = t0; t < t1; ++t) {
-        const int token0 = t * C, i = 32 * tt + ln.r;
+        const int token0 = t * kTile, there = min(a.N - token0, kTile);
+        unsigned char *at = lds + (t & 1) * L::STAGE;   // (the waves that still read the tile before have the other half)
+        const typename L::Data kt{(bf16_t *)(at + L::K)}, qt{(bf16_t *)(at + L::Q)};
+        const typename Pr::Square nt{(bf16_t *)(at + Pr::N)}, pt{(bf16_t *)(at + Pr::P)};
+        fp.store(at);
         fk.store(kt);
         if constexpr (!LOCAL) fq.store(qt);
-        fn.store(nt);
-        if (wave == 0) make_gates<C>(g, gi, ln.id);
-        const f32x16 vt = v;
+        f32x16 r = v;
         __syncthreads();
         if (t + 1 < t1) fetch(t + 1);
-        if (!LOCAL && st.cache) save_state<D>(S, at, ln, st.cache + ((size_t)bh * a.tiles + t) * D * a.Dv + c0, a.Dv);
-        f32x16 r = {}, o = {};
-        float beta = 0.0f, start = 0.0f, rest = 0.0f;
-        if (active) {
-            beta = g.beta[i];
-            start = g.start[i];
-            rest = g.rest[i];
-#pragma unroll
-            for (int k0 = 0; k0 < D; k0 += 16) {
-                const auto s = stt.kc(ln, 32 * ct, k0);
-                r = mm<P::MADE>(s, kt.kc(ln, 32 * tt, k0), r);
-                if constexpr (!LOCAL) o = mm<P::MADE>(s, qt.kc(ln, 32 * tt, k0), o);
-            }
-            f32x16 x;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                r[e] = vt[e] - start * r[e];
-                x[e] = beta * r[e];
-            }
-            xt.st_acc(ln, 32 * tt, 32 * ct, x);
-            if constexpr (!LOCAL) {
-                o *= start;
-                if (ct <= tt) {   // scores of the tokens of block ct with this one's
-                    f32x16 p = {};
-#pragma unroll
-                    for (int k0 = 0; k0 < D; k0 += 16) p = mm<P::MADE>(kt.kc(ln, 32 * ct, k0), qt.kc(ln, 32 * tt, k0), p);
-                    const double gs = g.sum[i];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = 32 * ct + ln.acc_row(e);
-                        p[e] = j <= i ? p[e] * power(gs - g.sum[j]) : 0.0f;
-                    }
-                    pt.st_acc(ln, 32 * tt, 32 * ct, p);
-                }
-            }
-        }
-        __syncthreads();
-        if (active) {
-            for (int k0 = 0; k0 < 32 * (tt + 1); k0 += 16) r = mm<P::MADE>(xt.ks(ln, k0, 32 * ct), nt.kc(ln, 32 * tt, k0), r);
-            r *= beta;
-            if constexpr (!LOCAL) yt.st_acc(ln, 32 * tt, 32 * ct, r);
-            r *= rest;
-            zt.st_acc(ln, 32 * tt, 32 * ct, r);
-        }
-        __syncthreads();
         if constexpr (!LOCAL)
-            if (active) {
-                for (int k0 = 0; k0 < 32 * (tt + 1); k0 += 16) o = mm<P::MADE>(yt.ks(ln, k0, 32 * ct), pt.kc(ln, 32 * tt, k0), o);
-                if (token0 + i < a.N) store_acc(O + (row + token0 + i) * a.Dv + c0 + 32 * ct, ln, o);
-            }
-        const float whole = g.whole;
+            if (st.cache && t % P::GRAD_TILES == 0)
+                save_state<KB>(S, ln, st.cache + ((size_t)bh * a.grad_tiles + t / P::GRAD_TILES) * D * DV + c0, DV);
+        const f32x16 beta = by_row((const float *)(at + Pr::BETA), ln);
+        f32x16 o = {};   // r: a row per token;  o: a lane per token, a row per column
+        {
+            f32x16 x = {};
 #pragma unroll
-        for (int s = 0; s < StatePlace<D>::N; ++s) {
-            S[s] *= whole;
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int k0 = 0; k0 < C; k0 += 16) S[s] = mm<P::MADE>(kt.ks(ln, k0, at.key0(s)), zt.ks(ln, k0, at.col0(s)), S[s]);
-            stt.st_acc(ln, at.col0(s), at.key0(s), S[s]);
+                for (int m = 0; m < 2; ++m) {
+                    const auto s = split<MADE>(S[kb], m);
+                    x = mm<MADE>(kt.kp(ln, 0, 32 * kb, m), s, x);
+                    if constexpr (!LOCAL) o = mm<MADE>(s, qt.kp(ln, 0, 32 * kb, m), o);
+                }
+            r -= by_row((const float *)(at + Pr::START), ln) * x;
+            x = beta * r;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) r = mm<MADE>(nt.kp(ln, m), split<MADE>(x, m), r);
         }
-        __syncthreads();
+        if constexpr (!LOCAL)
+            if (st.cache) store_rows<DV>(st.w + (row + token0) * DV + c0 + ln.r, ln, there, r);
+        r *= beta;
+        if constexpr (!LOCAL) {
+            o *= ((const float *)(at + Pr::START))[ln.r];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) o = mm<MADE>(split<MADE>(r, m), pt.kp(ln, m), o);
+            if (ln.r < there) store_acc(O + (row + token0 + ln.r) * DV + c0, ln, o);
+        }
+        r *= by_row((const float *)(at + Pr::REST), ln);
+        const float whole = *(const float *)(at + Pr::WHOLE);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) S[kb] *= whole;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const auto f = split<MADE>(r, m);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, 32 * kb, m), f, S[kb]);
+        }
     }
     if constexpr (LOCAL) {
-        if (trans) save_state<D>(S, at, ln, st.trans + ((size_t)bh * a.segments + seg) * D * D + c0, D);
-        else save_state<D>(S, at, ln, st.local + ((size_t)bh * a.segments + seg) * D * a.Dv + c0, a.Dv);
-    } else if (seg == a.segments - 1) {
-        save_state<D>(S, at, ln, st.last + (size_t)bh * D * a.Dv + c0, a.Dv);
+        if (trans) save_state<KB>(S, ln, st.trans + ((size_t)bh * a.segments + seg) * D * D + c0, D);
+        else save_state<KB>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
+    } else {
+        for (int t = max(t0, t1); t < end; ++t)
+            store_rows<DV>(O + (row + t * kTile) * DV + c0 + ln.r, ln, min(a.N - t * kTile, kTile), f32x16{});
+        if (seg == a.segments - 1) save_state<KB>(S, ln, st.last + (size_t)bh * D * DV + c0, DV);
     }
 }
 
@@ -513,36 +631,62 @@ __global__ __launch_bounds__(kThreads, 1) void k_delta_walk(const T *__restrict_
 // k_delta_scan: first[0] = in, first[p + 1] = T_p first[p] + local[p]; BACK: last[P - 1] = in, last[p - 1] = T_p^T last[p] + local[p].
 // 16 columns a workgroup, in float.
 // ---------------------------------------------------------------------------
+// (v_mfma_f32_16x16x4_f32: lane l supplies row or column l & 15 and contraction index l >> 4; accumulator rows 4 (l >> 4) .. + 3, column l & 15.)
 constexpr int kScanCols = 16;
 template <int D, bool BACK>
 __global__ __launch_bounds__(kThreads) void k_delta_scan(const float *__restrict__ in, const float *__restrict__ trans, const float *__restrict__ local,
                                                          float *__restrict__ states, int Dv, int segments) {
-    __shared__ __attribute__((aligned(16))) float S[D][kScanCols];
-    constexpr int PER = D * kScanCols / kThreads, TPR = kScanCols / PER;   // columns a thread takes of one row
-    const int bh = blockIdx.y, c0 = blockIdx.x * kScanCols, d = threadIdx.x / TPR, c = threadIdx.x % TPR * PER;
-    float x[PER];
+    __shared__ float S[2][D][kScanCols + 1];
+    constexpr int TILES = D / 16 / kWaves;   // 16 rows each, a wave
+    const int bh = blockIdx.x, c = blockIdx.y * kScanCols + (threadIdx.x & 15), wave = threadIdx.x >> 6, l16 = threadIdx.x & 15, l4 = threadIdx.x >> 4 & 3;
+    f32x4 x[TILES], add[TILES];
+    float m[TILES][D / 4];   // contraction 16 s + 4 l4 + i at 4 s + i
+    auto at = [&](size_t segment, int tl, int i) { return (segment * D + 16 * (wave * TILES + tl) + 4 * l4 + i) * Dv + c; };
+    auto fetch = [&](int p) {
+        const float *t = trans + ((size_t)bh * segments + p) * D * D;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) x[e] = in ? in[((size_t)bh * D + d) * Dv + c0 + c + e] : 0.0f;
+        for (int tl = 0; tl < TILES; ++tl) {
+            const int d = 16 * (wave * TILES + tl) + l16;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                if constexpr (BACK) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m[tl][4 * s + i] = t[(size_t)(16 * s + 4 * l4 + i) * D + d];
+                } else {
+                    const f32x4 y = *(const f32x4 *)(t + (size_t)d * D + 16 * s + 4 * l4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m[tl][4 * s + i] = y[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add[tl][i] = local[at((size_t)bh * segments + p, tl, i)];
+        }
+    };
+#pragma unroll
+    for (int tl = 0; tl < TILES; ++tl)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[tl][i] = in ? in[at(bh, tl, i)] : 0.0f;
     for (int step = 0; step < segments; ++step) {
         const int p = BACK ? segments - 1 - step : step;
-        const size_t at = (((size_t)bh * segments + p) * D + d) * Dv + c0 + c;
+        if (step + 1 < segments) fetch(p);
+        auto &lds = S[step & 1];   // (read by the other waves until the barrier of the next step)
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            states[at + e] = x[e];
-            S[d][c + e] = x[e];
-        }
+        for (int tl = 0; tl < TILES; ++tl)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                states[at((size_t)bh * segments + p, tl, i)] = x[tl][i];
+                lds[16 * (wave * TILES + tl) + 4 * l4 + i][l16] = x[tl][i];
+            }
         if (step + 1 == segments) break;
         __syncthreads();
-        const float *m = trans + ((size_t)bh * segments + p) * D * D;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = local[at + e];
-#pragma unroll 8
-        for (int k = 0; k < D; ++k) {
-            const float w = BACK ? m[(size_t)k * D + d] : m[(size_t)d * D + k];
+        for (int tl = 0; tl < TILES; ++tl) x[tl] = add[tl];
 #pragma unroll
-            for (int e = 0; e < PER; ++e) x[e] = __builtin_fmaf(w, S[k][c + e], x[e]);
+        for (int s = 0; s < D / 4; ++s) {
+            const float y = lds[16 * (s / 4) + 4 * l4 + s % 4][l16];
+#pragma unroll
+            for (int tl = 0; tl < TILES; ++tl) x[tl] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[tl][s], y, x[tl], 0, 0, 0);
         }
-        __syncthreads();
     }
 }
 
@@ -621,300 +765,302 @@ __global__ __launch_bounds__(kThreads) void k_delta_step(const T *__restrict__ Q
 // ---------------------------------------------------------------------------
 // k_delta_back: the walk in reverse. LOCAL: the gradient that reaches a segment's front from its own tokens.
 // ---------------------------------------------------------------------------
-template <typename T, int D>
-struct BackLds {
+template <typename T, int D, int DV>
+struct Back {
     using P = Parts<T>;
-    static constexpr int C = P::C;
-    typedef Tile<P::DATA, C, D> Data;
-    typedef Tile<P::MADE, kDeltaCols, D> State;   // transposed
-    typedef Tile<P::MADE, C, C> Square;
-    typedef Tile<P::MADE, C, kDeltaCols> Rows;
-    typedef Tile<P::DATA, C, kDeltaCols> Grad;
-    static constexpr int GATES = (int)((sizeof(Gates<C>) + 15) / 16 * 16);
-    static constexpr int K = 0, Q = K + Data::BYTES, S = Q + Data::BYTES, DO = S + State::BYTES, GO = DO + Grad::BYTES, NN = GO + Rows::BYTES,
-                         X = NN + Square::BYTES, PP = X + Rows::BYTES, G = PP + (Rows::BYTES > Square::BYTES ? Rows::BYTES : Square::BYTES),
-                         ALL = G + 2 * GATES;
-    static_assert(ALL <= 163840, "LDS of a CU");
+    static constexpr int KB = D / 32, WAVES = DV / 32, NT = 64 * WAVES;
+    typedef Tile<P::DATA, kTile, D> Data;
+    typedef Tile<P::DATA, kTile, DV> Grad;
+    static constexpr int PREP = 0, K = Prepared<T>::BYTES, Q = K + Data::BYTES, DO = Q + Data::BYTES, STAGE = DO + Grad::BYTES,
+                         STAGES = 2 * STAGE <= 163840 ? 2 : 1, LDS = STAGES * STAGE;
 };
 struct BackStates {
     const float *last;   // gradients of the states segments end with ([head][segment], or dkv_out where there is one segment); null = zeros
     float *first;        // dkv_in
     float *local;        // LOCAL
-    float *grads;        // the gradient of the state behind every tile
+    float *grads;        // the gradient of the state behind every tile that k_delta_grad takes
     float *dr;           // [B][H][N][Dv]
 };
-template <typename T, int D, bool LOCAL>
-__global__ __launch_bounds__(kThreads, 1) void k_delta_back(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ dO,
-                                                            const bf16_t *__restrict__ inv, T *__restrict__ dV, BackStates st, DeltaCall a) {
-    using P = Parts<T>;
-    using L = BackLds<T, D>;
-    constexpr int C = P::C;
+template <typename T, int D, int DV, bool LOCAL>
+__global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void k_delta_back(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ dO,
+                                                                       const char *__restrict__ prepared, T *__restrict__ dV, BackStates st,
+                                                                       DeltaCall a) {
+    using L = Back<T, D, DV>;
+    using P = typename L::P;
+    using Pr = Prepared<T>;
+    constexpr int KB = L::KB, MADE = P::MADE, GT = P::GRAD_TILES;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const typename L::Data kt{(bf16_t *)(lds + L::K)}, qt{(bf16_t *)(lds + L::Q)};
-    const typename L::State stt{(bf16_t *)(lds + L::S)};
-    const typename L::Square nt{(bf16_t *)(lds + L::NN)}, pt{(bf16_t *)(lds + L::PP)};   // pt: [key token][query token]
-    const typename L::Rows xt{(bf16_t *)(lds + L::X)}, gt{(bf16_t *)(lds + L::GO)}, zt{(bf16_t *)(lds + L::PP)};
-    const typename L::Grad dot{(bf16_t *)(lds + L::DO)};
-    auto gates = [&](int t) -> Gates<C> & { return *(Gates<C> *)(lds + L::G + (t & 1) * L::GATES); };
     const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6;
-    const int blocks = a.Dv / kDeltaCols, c0 = blockIdx.x % blocks * kDeltaCols, seg = blockIdx.x / blocks % a.segments;
-    const int bh = blockIdx.x / (blocks * a.segments), b = bh / a.H, h = bh - b * a.H;
+    const int wave = threadIdx.x >> 6, c0 = 32 * wave, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
     if (LOCAL && seg == 0) return;
-    const int t0 = seg * a.seg_tiles, t1 = min(a.tiles, t0 + a.seg_tiles);
+    const int tokens = a.valid(b, 0, a.N), end = min(a.tiles, (seg + 1) * a.seg_tiles);
+    const int t0 = seg * a.seg_tiles, t1 = min(end, (tokens + kTile - 1) / kTile);
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N;
-    const int ct = wave & 1, jt = wave >> 1;   // this wave's block of 32 columns and 32 tokens
-    const bool active = jt < C / 32;
-    const StatePlace<D> at{wave};
-    f32x16 S[StatePlace<D>::N];
-    load_state<D>(S, at, ln, LOCAL || !st.last ? nullptr : st.last + ((size_t)bh * a.segments + seg) * D * a.Dv + c0, a.Dv);
-#pragma unroll
-    for (int s = 0; s < StatePlace<D>::N; ++s) stt.st_acc(ln, at.col0(s), at.key0(s), S[s]);
-
-    Fetch<T, C, D> fk, fq;
-    Fetch<T, C, kDeltaCols> fo;
-    FetchParts<P::MADE, C> fn;
-    GateIn gi{0.0f, 0.0f};
+    f32x16 S[KB];
+    load_state<KB>(S, ln, LOCAL || !st.last ? nullptr : st.last + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
+    if constexpr (!LOCAL)
+        for (int t = max(t0, t1); t < end; ++t)
+            store_rows<DV>(dV + (row + t * kTile) * DV + c0 + ln.r, ln, min(a.N - t * kTile, kTile), f32x16{});
+    Fetch<T, kTile, D, L::NT> fk, fq;
+    Fetch<T, kTile, DV, L::NT> fo;
+    Copy<Pr::BYTES, L::NT> fp;
     auto fetch = [&](int t) {
-        const int token0 = t * C, valid = a.valid(b, token0, C);
+        const int token0 = t * kTile, valid = min(tokens - token0, kTile);
+        fp.load(prepared + ((size_t)bh * a.tiles + t) * Pr::BYTES);
         fk.load(K + (key_row + token0) * D, D, valid);
         fq.load(Q + (key_row + token0) * D, D, valid);
-        fo.load(dO + (row + token0) * a.Dv + c0, a.Dv, valid);
-        fn.load(inv + ((size_t)bh * a.tiles + t) * (P::MADE * C * C));
-        if (wave == 0) gi.load(a.log_g ? a.log_g + row + token0 : nullptr, a.beta + row + token0, valid, ln.id);
+        fo.load(dO + (row + token0) * DV, DV, valid);
     };
-    fetch(t1 - 1);
-    if (wave == 0) make_gates<C>(gates(t1 - 1), gi, ln.id);
-    __syncthreads();
+    if (t0 < t1) fetch(t1 - 1);
     for (int t = t1 - 1; t >= t0; --t) {
-        const int token0 = t * C, j = 32 * jt + ln.r;
-        const Gates<C> &g = gates(t);
+        const int token0 = t * kTile, there = min(a.N - token0, kTile);
+        unsigned char *at = lds + t % L::STAGES * L::STAGE;
+        const typename L::Data kt{(bf16_t *)(at + L::K)}, qt{(bf16_t *)(at + L::Q)};
+        const typename L::Grad dot{(bf16_t *)(at + L::DO)};
+        const typename Pr::Square nt{(bf16_t *)(at + Pr::N)}, pt{(bf16_t *)(at + Pr::P)};
+        if (L::STAGES == 1) __syncthreads();
+        fp.store(at);
         fk.store(kt);
         fq.store(qt);
         fo.store(dot);
-        fo.store_scaled(gt, g.start);
-        fn.store(nt);
         __syncthreads();
         if (t > t0) fetch(t - 1);
-        if (!LOCAL) save_state<D>(S, at, ln, st.grads + ((size_t)bh * a.tiles + t) * D * a.Dv + c0, a.Dv);
-        f32x16 du = {};
-        float beta = 0.0f, start = 0.0f;
-        if (active) {
-            beta = g.beta[j];
-            start = g.start[j];
+        if constexpr (!LOCAL)
+            if (t % GT == GT - 1 || t == t1 - 1) save_state<KB>(S, ln, st.grads + ((size_t)bh * a.grad_tiles + t / GT) * D * DV + c0, DV);
+        f32x16 du = {};   // a row per token
 #pragma unroll
-            for (int k0 = 0; k0 < D; k0 += 16) du = mm<P::MADE>(stt.kc(ln, 32 * ct, k0), kt.kc(ln, 32 * jt, k0), du);
-            du *= g.rest[j];
-            // scores of block `qb` of queries with this block of keys: the two waves of a block of keys take one each
-            const int qb = C == 32 ? 0 : ct;
-            if (qb >= jt && (C > 32 || ct == 0)) {
-                f32x16 p = {};
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int k0 = 0; k0 < D; k0 += 16) p = mm<P::MADE>(qt.kc(ln, 32 * qb, k0), kt.kc(ln, 32 * jt, k0), p);
-                const double gj = g.sum[j];
+            for (int m = 0; m < 2; ++m) du = mm<MADE>(kt.kp(ln, 0, 32 * kb, m), split<MADE>(S[kb], m), du);
+        du *= by_row((const float *)(at + Pr::REST), ln);
+        const float whole = *(const float *)(at + Pr::WHOLE);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int i = 32 * qb + ln.acc_row(e);
-                    p[e] = i >= j ? p[e] * power(g.sum[i] - gj) : 0.0f;
-                }
-                pt.st_acc(ln, 32 * jt, 32 * qb, p);
-            }
+        for (int kb = 0; kb < KB; ++kb) S[kb] *= whole;
+#pragma unroll
+        for (int f = 0; f < kTile / 16; ++f) {
+            const auto go = dot.ks(ln, 16 * f, c0);
+            du = mm<MADE>(pt.ks(ln, 16 * f), go, du);
+            f32x8 y = {};   // Q^T (exp(G) dO)
+#pragma unroll
+            for (int i = P::DATA - 1; i >= 0; --i) y += __builtin_convertvector(go.p[i], f32x8);
+            const float *start = (const float *)(at + Pr::START) + 16 * f + 8 * ln.h;
+            y *= __builtin_shufflevector(*(const f32x4 *)start, *(const f32x4 *)(start + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+            const auto s = split<MADE>(y);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(qt.ks(ln, 16 * f, 32 * kb), s, S[kb]);
         }
-        __syncthreads();
-        if (active) {
-            for (int k0 = 32 * jt; k0 < C; k0 += 16) du = mm<P::MADE>(dot.ks(ln, k0, 32 * ct), pt.kc(ln, 32 * jt, k0), du);
-            xt.st_acc(ln, 32 * jt, 32 * ct, du * beta);
-        }
-        __syncthreads();
-        if (active) {
-            for (int k0 = 32 * jt; k0 < C; k0 += 16) du = mm<P::MADE>(xt.ks(ln, k0, 32 * ct), nt.ks(ln, k0, 32 * jt), du);
-            const f32x16 dv = du * beta;
-            if (!LOCAL && token0 + j < a.N) {
-                store_acc(st.dr + (row + token0 + j) * a.Dv + c0 + 32 * ct, ln, du);
-                store_acc(dV + (row + token0 + j) * a.Dv + c0 + 32 * ct, ln, dv);
-            }
-            zt.st_acc(ln, 32 * jt, 32 * ct, dv * -start);   // (in the scores' place: every wave is past them)
-        }
-        const float whole = g.whole;
-        if (t > t0 && wave == 0) make_gates<C>(gates(t - 1), gi, ln.id);
-        __syncthreads();
+        const f32x16 beta = by_row((const float *)(at + Pr::BETA), ln);
+        {
+            const f32x16 x = beta * du;
 #pragma unroll
-        for (int s = 0; s < StatePlace<D>::N; ++s) {
-            S[s] *= whole;
-#pragma unroll
-            for (int k0 = 0; k0 < C; k0 += 16) {
-                S[s] = mm<P::MADE>(qt.ks(ln, k0, at.key0(s)), gt.ks(ln, k0, at.col0(s)), S[s]);
-                S[s] = mm<P::MADE>(kt.ks(ln, k0, at.key0(s)), zt.ks(ln, k0, at.col0(s)), S[s]);
-            }
-            stt.st_acc(ln, at.col0(s), at.key0(s), S[s]);
+            for (int m = 0; m < 2; ++m) du = mm<MADE>(nt.ksp(ln, m), split<MADE>(x, m), du);
         }
-        __syncthreads();
+        const f32x16 dv = beta * du;
+        if constexpr (!LOCAL) {
+            const size_t to = (row + token0) * DV + c0 + ln.r;
+            store_rows<DV>(st.dr + to, ln, there, du);
+            store_rows<DV>(dV + to, ln, there, dv);
+        }
+        const f32x16 z = -dv * by_row((const float *)(at + Pr::START), ln);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const auto f = split<MADE>(z, m);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, 32 * kb, m), f, S[kb]);
+        }
     }
-    if (LOCAL) save_state<D>(S, at, ln, st.local + ((size_t)bh * a.segments + seg) * D * a.Dv + c0, a.Dv);
-    else if (seg == 0) save_state<D>(S, at, ln, st.first + (size_t)bh * D * a.Dv + c0, a.Dv);
+    if (LOCAL) save_state<KB>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
+    else if (seg == 0) save_state<KB>(S, ln, st.first + (size_t)bh * D * DV + c0, DV);
 }
 
 // ---------------------------------------------------------------------------
-// k_delta_grad: a tile's gradients, from the state in front of it and the gradient of the one behind it, 64 value features at a time.
+// k_delta_grad: a tile's gradients, from the state in front of it, the gradient of the one behind it, w and dR, 64 value features at a time. A wave
+// has 32 key features of dQ and dK; its rows of both states come from memory straight into its registers, as they are read once.
 // ---------------------------------------------------------------------------
+template <int C>
+struct Gates {
+    double sum[C];
+    float start[C], rest[C], beta[C];   // exp(G_i), exp(G_C - G_i)
+    float whole;
+};
 template <typename T, int D>
-struct GradLds {
+struct Grad {
     using P = Parts<T>;
-    static constexpr int C = P::C;
+    static constexpr int NB = P::GRAD_TILES, C = NB * kTile, COLS = 64, SLICES = D / 32, PER = SLICES == kWaves ? NB : 1;   // PER: token blocks of a wave
     typedef Tile<P::DATA, C, D> Data;
-    typedef Tile<P::MADE, D, kDeltaCols> State;
-    typedef Tile<P::MADE, C, C> Square;
-    typedef Tile<P::MADE, C, kDeltaCols> Rows;
-    typedef Tile<P::DATA, C, kDeltaCols> Grad;
-    static_assert(Square::BYTES <= Rows::BYTES, "Ep and Em take the places of rows");
-    static constexpr int K = 0, Q = K + Data::BYTES, S = Q + Data::BYTES, DO = S + State::BYTES, NN = DO + Grad::BYTES, X = NN + Square::BYTES,
-                         Y = X + Rows::BYTES, G = Y + Rows::BYTES, RED = G + (int)((sizeof(Gates<C>) + 15) / 16 * 16),
-                         ALL = RED + kWaves * (3 * C + 4) * 4;
-    static_assert(ALL <= 163840, "LDS of a CU");
+    typedef Lower<P::MADE, C> Square;
+    typedef Tile<P::MADE, C, COLS> Rows;
+    typedef Tile<P::DATA, C, COLS> Out;
+    static_assert(Square::BYTES <= Rows::BYTES && kWaves * (C + 1) * 4 + 2 * C * 4 <= Out::BYTES, "what comes later takes the places of rows");
+    static constexpr int K = 0, Q = K + Data::BYTES, U = Q + Data::BYTES, DV = U + Rows::BYTES, DO = DV + Rows::BYTES, G = DO + Out::BYTES,
+                         LDS = G + (int)((sizeof(Gates<C>) + 15) / 16 * 16);
 };
 template <typename T, int D, typename TO>
 __global__ __launch_bounds__(kThreads, 1) void k_delta_grad(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
-                                                            const T *__restrict__ dO, const bf16_t *__restrict__ inv, const float *__restrict__ states,
-                                                            const float *__restrict__ grads, const float *__restrict__ dR, TO *__restrict__ dQ,
+                                                            const T *__restrict__ dO, const float *__restrict__ states, const float *__restrict__ grads,
+                                                            const float *__restrict__ w, const float *__restrict__ dR, TO *__restrict__ dQ,
                                                             TO *__restrict__ dK, float *__restrict__ dbeta, float *__restrict__ dlog_g, DeltaCall a) {
-    using P = Parts<T>;
-    using L = GradLds<T, D>;
-    constexpr int C = P::C, KEY_BLOCKS = D / 32, BLOCKS = KEY_BLOCKS * (C / 32), PER = BLOCKS > kWaves ? BLOCKS / kWaves : 1;
+    using L = Grad<T, D>;
+    using P = typename L::P;
+    constexpr int C = L::C, NB = L::NB, PER = L::PER, COLS = L::COLS, MADE = P::MADE;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const typename L::Data kt{(bf16_t *)(lds + L::K)}, qt{(bf16_t *)(lds + L::Q)};
-    const typename L::State stt{(bf16_t *)(lds + L::S)};
-    const typename L::Square nt{(bf16_t *)(lds + L::NN)}, ep{(bf16_t *)(lds + L::X)}, em{(bf16_t *)(lds + L::Y)};
-    const typename L::Rows xt{(bf16_t *)(lds + L::X)}, yt{(bf16_t *)(lds + L::Y)};
-    const typename L::Grad dot{(bf16_t *)(lds + L::DO)};
+    const typename L::Rows ut{(bf16_t *)(lds + L::U)}, vt{(bf16_t *)(lds + L::DV)};
+    const typename L::Out dot{(bf16_t *)(lds + L::DO)};
+    const typename L::Square ep{ut.p}, em{vt.p};
     Gates<C> &g = *(Gates<C> *)(lds + L::G);
-    float(*red)[3 * C + 4] = (float(*)[3 * C + 4])(lds + L::RED);
+    float *red = (float *)(lds + L::DO);   // [wave][C] q . dq, [wave] <dS, S'>, [C] dbeta, [C] v . dv
     const Lane ln(threadIdx.x);
     const int wave = threadIdx.x >> 6, tile = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * C;
-    const int valid = a.valid(b, token0, C);
-    const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N;
-    const int ct = wave & 1, tt = wave >> 1, i = 32 * tt + ln.r;     // block of 32 columns and 32 tokens
-    const bool active = tt < C / 32;
-    const int tk = wave * PER / KEY_BLOCKS, m = 32 * tk + ln.r;      // token block of the accumulators of dQ and dK
-    auto key0 = [&](int s) { return (wave * PER + s) % KEY_BLOCKS * 32; };
-    const bool active_k = wave * PER < BLOCKS;
+    const int valid = a.valid(b, token0, C), there = min(a.N - token0, C);
+    const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N + token0;
+    if (valid == 0) {
+        for (int e = threadIdx.x; e < there * D; e += kThreads) {
+            Elem<TO>::st1(dQ + row * D + e, 0.0f);
+            Elem<TO>::st1(dK + row * D + e, 0.0f);
+        }
+        if ((int)threadIdx.x < there) {
+            dbeta[row + threadIdx.x] = 0.0f;
+            if (dlog_g) dlog_g[row + threadIdx.x] = 0.0f;
+        }
+        return;
+    }
+    const int d0 = 32 * (L::SLICES == kWaves ? wave : wave & 1), tk0 = L::SLICES == kWaves ? 0 : wave >> 1;
+    const bool active = tk0 < NB;
 
-    Fetch<T, C, D> fk, fq;
+    Fetch<T, C, D, kThreads> fk, fq;
+    Fetch<float, C, COLS, kThreads> fw, fr;
+    Fetch<T, C, COLS, kThreads> fo;
+    constexpr int ROWS = Fetch<float, C, COLS, kThreads>::N;
+    typedef typename std::conditional<sizeof(T) == 2, bf16x4, f32x4>::type Four;
+    Four fv[ROWS];
+    auto fetch = [&](int c0) {
+        fw.load(w + row * a.Dv + c0, a.Dv, valid);
+        fr.load(dR + row * a.Dv + c0, a.Dv, valid);
+        fo.load(dO + row * a.Dv + c0, a.Dv, valid);
+#pragma unroll
+        for (int n = 0; n < ROWS; ++n) {
+            const int c = threadIdx.x + n * kThreads, r = c / (COLS / 4);
+            fv[n] = Four{0, 0, 0, 0};
+            if (r < valid) fv[n] = *(const Four *)(V + (row + r) * a.Dv + c0 + c % (COLS / 4) * 4);
+        }
+    };
     fk.load(K + (key_row + token0) * D, D, valid);
     fq.load(Q + (key_row + token0) * D, D, valid);
+    fetch(0);
     if (wave == 0) {
-        GateIn gi;
-        gi.load(a.log_g ? a.log_g + row + token0 : nullptr, a.beta + row + token0, valid, ln.id);
-        make_gates<C>(g, gi, ln.id);
+        const bool in = ln.id < valid;
+        const double x = sum_up<C>(a.log_g && in ? to_base2(a.log_g[row + ln.id]) : 0.0, ln.id), all = __shfl(x, C - 1, C);
+        if (ln.id < C) {
+            g.sum[ln.id] = x;
+            g.start[ln.id] = power(x);
+            g.rest[ln.id] = power(all - x);
+            g.beta[ln.id] = in ? a.beta[row + ln.id] : 0.0f;
+        }
+        if (ln.id == 0) g.whole = power(all);
     }
     fk.store(kt);
     fq.store(qt);
-    for (int e = threadIdx.x; e < kWaves * (3 * C + 4); e += kThreads) ((float *)red)[e] = 0.0f;
 
-    f32x16 ap = {}, am = {};                          // dO U^T, dV U^T
-    f32x16 aq[PER] = {}, a1[PER] = {}, a2[PER] = {};  // S dO, S dV, dS U (a row per key feature)
-    float sum_b = 0.0f, sum_v = 0.0f, both = 0.0f;    // dR . w and V . dV of the lane's token, <dS, S>
-    for (int c0 = 0; c0 < a.Dv; c0 += kDeltaCols) {
-        const size_t state = ((size_t)bh * a.tiles + tile) * D * a.Dv + c0;
-        Fetch<float, D, kDeltaCols> fs, fd;
-        Fetch<T, C, kDeltaCols> fo;
-        FetchParts<P::MADE, C> fn;
-        fs.load(states + state, a.Dv, D);
-        fo.load(dO + (row + token0) * a.Dv + c0, a.Dv, valid);
-        fn.load(inv + ((size_t)bh * a.tiles + tile) * (P::MADE * C * C));
-        f32x16 v = {}, dr = {};
-        if (active) {
-            v = load_acc(V + (row + token0 + i) * a.Dv + c0 + 32 * ct, ln, i < valid);
-            dr = load_acc(dR + (row + token0 + i) * a.Dv + c0 + 32 * ct, ln, i < valid);
-        }
-        if (c0 > 0) __syncthreads();
-        fs.store(stt);
+    f32x16 ap = {}, am = {};                          // U dO^T, U dV^T, a row per key token
+    f32x16 aq[PER] = {}, a1[PER] = {}, a2[PER] = {};  // S dO^T, S dV^T, dS U^T, a row per key feature
+    float sum_b[ROWS] = {}, sum_v[ROWS] = {}, both = 0.0f;   // dR . w and v . dv of the rows this thread stages, <dS, S>
+    for (int c0 = 0; c0 < a.Dv; c0 += COLS) {
+        f32x4 s4[COLS / 16][2], d4[COLS / 16][2];
+        const size_t state = (((size_t)bh * a.grad_tiles + tile) * D + d0 + ln.r) * a.Dv + c0 + 8 * ln.h;
+#pragma unroll
+        for (int k = 0; k < COLS / 16; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s4[k][i] = *(const f32x4 *)(states + state + 16 * k + 4 * i);
+                d4[k][i] = *(const f32x4 *)(grads + state + 16 * k + 4 * i);
+            }
+        __syncthreads();   // the gates are there; the tiles have been read
         fo.store(dot);
-        fn.store(nt);
-        __syncthreads();
-        fd.load(grads + state, a.Dv, D);
-        f32x16 r = {};
-        float beta = 0.0f;
-        if (active) {
-            beta = g.beta[i];
-            const float start = g.start[i];
+        fw.each([&](int n, int r, int col, u32x4 x) {
+            const f32x4 w4 = __builtin_bit_cast(f32x4, x), r4 = __builtin_bit_cast(f32x4, fr.v[n]), v4 = __builtin_convertvector(fv[n], f32x4);
+            const float beta = g.beta[r];
+            const f32x4 dv4 = beta * r4;
+            ut.st4(r, col, beta * w4);
+            vt.st4(r, col, dv4);
 #pragma unroll
-            for (int k0 = 0; k0 < D; k0 += 16) r = mm<P::MADE>(stt.ks(ln, k0, 32 * ct), kt.kc(ln, 32 * tt, k0), r);
-            r = v - start * r;
-            xt.st_acc(ln, 32 * tt, 32 * ct, r * beta);
-        }
+            for (int e = 0; e < 4; ++e) {
+                sum_b[n] = __builtin_fmaf(r4[e], w4[e], sum_b[n]);
+                sum_v[n] = __builtin_fmaf(dv4[e], v4[e], sum_v[n]);
+            }
+        });
         __syncthreads();
-        f32x16 dv = {};
-        if (active) {
-            for (int k0 = 0; k0 < 32 * (tt + 1); k0 += 16) r = mm<P::MADE>(xt.ks(ln, k0, 32 * ct), nt.kc(ln, 32 * tt, k0), r);
-            dv = dr * beta;
+        if (c0 + COLS < a.Dv) fetch(c0 + COLS);
+        if (wave < L::Square::BLOCKS) {
+            const int tb = wave > 0, jb = wave == 2;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                sum_b = __builtin_fmaf(dr[e], r[e], sum_b);
-                sum_v = __builtin_fmaf(dv[e], v[e], sum_v);
+            for (int k0 = 0; k0 < COLS; k0 += 16) {
+                const auto u = ut.kc(ln, 32 * jb, k0);
+                ap = mm<MADE>(u, dot.kc(ln, 32 * tb, k0), ap);
+                am = mm<MADE>(u, vt.kc(ln, 32 * tb, k0), am);
             }
         }
-        __syncthreads();
-        if (active) {
-            xt.st_acc(ln, 32 * tt, 32 * ct, dv);
-            yt.st_acc(ln, 32 * tt, 32 * ct, r * beta);
-        }
-        __syncthreads();
-        if (active && ct <= tt && ct < C / 32)   // (as block of key tokens here)
+        if (active)
 #pragma unroll
-            for (int k0 = 0; k0 < kDeltaCols; k0 += 16) {
-                const auto u = yt.kc(ln, 32 * ct, k0);
-                ap = mm<P::MADE>(u, dot.kc(ln, 32 * tt, k0), ap);
-                am = mm<P::MADE>(u, xt.kc(ln, 32 * tt, k0), am);
-            }
-        if (active_k)
+            for (int k = 0; k < COLS / 16; ++k) {
+                const f32x8 x = __builtin_shufflevector(s4[k][0], s4[k][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                const f32x8 y = __builtin_shufflevector(d4[k][0], d4[k][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                if (tk0 == 0)
 #pragma unroll
-            for (int s = 0; s < PER; ++s)
+                    for (int e = 0; e < 8; ++e) both = __builtin_fmaf(x[e], y[e], both);
+                const auto fs = split<MADE>(x), fd = split<MADE>(y);
 #pragma unroll
-                for (int k0 = 0; k0 < kDeltaCols; k0 += 16) {
-                    const auto x = stt.kc(ln, key0(s), k0);
-                    aq[s] = mm<P::MADE>(x, dot.kc(ln, 32 * tk, k0), aq[s]);
-                    a1[s] = mm<P::MADE>(x, xt.kc(ln, 32 * tk, k0), a1[s]);
+                for (int n = 0; n < PER; ++n) {
+                    const int at = 32 * (tk0 + n);
+                    aq[n] = mm<MADE>(fs, dot.kc(ln, at, 16 * k), aq[n]);
+                    a1[n] = mm<MADE>(fs, vt.kc(ln, at, 16 * k), a1[n]);
+                    a2[n] = mm<MADE>(fd, ut.kc(ln, at, 16 * k), a2[n]);
                 }
-        __syncthreads();
-        fd.store(stt);
-#pragma unroll
-        for (int n = 0; n < Fetch<float, D, kDeltaCols>::N; ++n) {
-            const f32x4 x = __builtin_bit_cast(f32x4, fs.v[n]), y = __builtin_bit_cast(f32x4, fd.v[n]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) both = __builtin_fmaf(x[e], y[e], both);
-        }
-        __syncthreads();
-        if (active_k)
-#pragma unroll
-            for (int s = 0; s < PER; ++s)
-#pragma unroll
-                for (int k0 = 0; k0 < kDeltaCols; k0 += 16) a2[s] = mm<P::MADE>(stt.kc(ln, key0(s), k0), yt.kc(ln, 32 * tk, k0), a2[s]);
+            }
     }
     __syncthreads();
-    if (active && ct <= tt && ct < C / 32) {
+    if (wave < L::Square::BLOCKS) {
+        const int tb = wave > 0, jb = wave == 2, i = 32 * tb + ln.r;
         const double gi = g.sum[i];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int j = 32 * ct + ln.acc_row(e);
-            const float w = j <= i ? power(gi - g.sum[j]) : 0.0f;
-            ap[e] *= w;
-            am[e] *= j < i ? -w : 0.0f;
+            const int j = 32 * jb + ln.acc_row(e);
+            const float x = j <= i ? power(gi - g.sum[j]) : 0.0f;
+            ap[e] *= x;
+            am[e] *= j < i ? -x : 0.0f;
         }
-        ep.st_acc(ln, 32 * tt, 32 * ct, ap);
-        em.st_acc(ln, 32 * tt, 32 * ct, am);
+        ep.at(tb, jb).st_acc(ln, ap);
+        em.at(tb, jb).st_acc(ln, am);
     }
-    __syncthreads();
-    float sum_q = 0.0f, phi = g.whole * both;
-    if (active_k) {
-        const float start = g.start[m], rest = g.rest[m];
-        const bool there = token0 + m < a.N;
-        const size_t to = (row + token0 + m) * D;   // (shared heads: a partial sum for every state, in float)
+    float *red_phi = red + kWaves * C, *red_b = red_phi + kWaves, *red_v = red_b + C;
 #pragma unroll
-        for (int s = 0; s < PER; ++s) {
-            const int d0 = key0(s);
-            f32x16 x = aq[s] * start;
-            for (int k0 = 0; k0 < 32 * (tk + 1); k0 += 16) x = mm<P::MADE>(kt.ks(ln, k0, d0), ep.kc(ln, 32 * tk, k0), x);
-            f32x16 y = a2[s] * rest;
+    for (int n = 0; n < ROWS; ++n) {
+#pragma unroll
+        for (int d = 1; d < COLS / 4; d *= 2) {
+            sum_b[n] += __shfl_xor(sum_b[n], d);
+            sum_v[n] += __shfl_xor(sum_v[n], d);
+        }
+        const int c = threadIdx.x + n * kThreads;
+        if (c % (COLS / 4) == 0) {
+            red_b[c / (COLS / 4)] = sum_b[n];
+            red_v[c / (COLS / 4)] = sum_v[n];
+        }
+    }
+    for (int e = threadIdx.x; e < kWaves * C; e += kThreads) red[e] = 0.0f;
+    __syncthreads();
+    float phi = g.whole * both;
+    if (active)
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+            const int tk = tk0 + n, m = 32 * tk + ln.r;
+            const float start = g.start[m], rest = g.rest[m];
+            const size_t to = (row + m) * D + d0;   // (shared heads: a partial sum for every state, in float)
+            f32x16 x = aq[n] * start;
+            for (int jb = 0; jb <= tk; ++jb)
+#pragma unroll
+                for (int k0 = 0; k0 < 32; k0 += 16) x = mm<MADE>(kt.ks(ln, 32 * jb + k0, d0), ep.at(tk, jb).kc(ln, k0), x);
+            f32x16 y = a2[n] * rest;
+            float sum_q = 0.0f;
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
                 const f32x4 q4 = qt.get4(m, d0 + 8 * f + 4 * ln.h), k4 = kt.get4(m, d0 + 8 * f + 4 * ln.h);
@@ -924,51 +1070,44 @@ __global__ __launch_bounds__(kThreads, 1) void k_delta_grad(const T *__restrict_
                     phi = __builtin_fmaf(k4[e], y[4 * f + e], phi);
                 }
             }
-            if (there) store_acc(dQ + to + d0, ln, x);
-            y -= a1[s] * start;
-            for (int k0 = 32 * tk; k0 < C; k0 += 16) {
-                y = mm<P::MADE>(qt.ks(ln, k0, d0), ep.ks(ln, k0, 32 * tk), y);
-                y = mm<P::MADE>(kt.ks(ln, k0, d0), em.ks(ln, k0, 32 * tk), y);
-            }
-            for (int k0 = 0; k0 < 32 * (tk + 1); k0 += 16) y = mm<P::MADE>(kt.ks(ln, k0, d0), em.kc(ln, 32 * tk, k0), y);
-            if (there) store_acc(dK + to + d0, ln, y);
+            if (m < there) store_acc(dQ + to, ln, x);
+            y -= a1[n] * start;
+            for (int it = tk; it < NB; ++it)
+#pragma unroll
+                for (int k0 = 0; k0 < 32; k0 += 16) {
+                    y = mm<MADE>(qt.ks(ln, 32 * it + k0, d0), ep.at(it, tk).ks(ln, k0), y);
+                    y = mm<MADE>(kt.ks(ln, 32 * it + k0, d0), em.at(it, tk).ks(ln, k0), y);
+                }
+            for (int jb = 0; jb <= tk; ++jb)
+#pragma unroll
+                for (int k0 = 0; k0 < 32; k0 += 16) y = mm<MADE>(kt.ks(ln, 32 * jb + k0, d0), em.at(tk, jb).kc(ln, k0), y);
+            if (m < there) store_acc(dK + to, ln, y);
+            sum_q += __shfl_xor(sum_q, 32);
+            if (ln.h == 0) red[wave * C + m] = sum_q;
         }
-    }
-    sum_b += __shfl_xor(sum_b, 32);
-    sum_v += __shfl_xor(sum_v, 32);
-    sum_q += __shfl_xor(sum_q, 32);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) phi += __shfl_xor(phi, d);
-    if (ln.h == 0) {
-        if (active) {
-            red[wave][i] = sum_b;
-            red[wave][C + i] = sum_v;
-        }
-        if (active_k) red[wave][2 * C + m] = sum_q;
-    }
-    if (ln.id == 0) red[wave][3 * C] = phi;
+    if (ln.id == 0) red_phi[wave] = phi;
     __syncthreads();
     if (wave != 0) return;
     double x = 0.0, all = 0.0;
-    float db = 0.0f;
-    if (ln.id < C)
+    if (ln.id < C) {
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            db += red[w][ln.id];
-            x += (double)red[w][2 * C + ln.id] - (double)red[w][C + ln.id];
-        }
+        for (int v = 0; v < kWaves; ++v) x += red[v * C + ln.id];
+        x -= red_v[ln.id];
+    }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) all += red[w][3 * C];
+    for (int v = 0; v < kWaves; ++v) all += red_phi[v];
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
         const double y = __shfl_down(x, d, C);
         if ((ln.id & (C - 1)) + d < C) x += y;
     }
-    if (ln.id < C && token0 + ln.id < a.N) {
-        dbeta[row + token0 + ln.id] = db;
+    if (ln.id < there) {
+        dbeta[row + ln.id] = red_b[ln.id];
         if (dlog_g) {
-            const bool none = ln.id >= valid || to_base2(a.log_g[row + token0 + ln.id]) <= -150.0;   // (a gate of 0 has no slope)
-            dlog_g[row + token0 + ln.id] = none ? 0.0f : (float)(all + x);
+            const bool none = ln.id >= valid || to_base2(a.log_g[row + ln.id]) <= -150.0;   // (a gate of 0 has no slope)
+            dlog_g[row + ln.id] = none ? 0.0f : (float)(all + x);
         }
     }
 }
@@ -996,38 +1135,41 @@ constexpr int kCus = 256;
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 struct Layout {   // byte offsets
-    size_t states, inv, trans, cache;                               // cache
-    size_t own_inv, own_trans, local, first, scratch;               // forward scratch
-    size_t grads, dr, back_local, last, part, back_scratch;         // backward scratch
+    size_t states, inv, trans, w, cache;                      // cache
+    size_t own_inv, own_trans, local, first, scratch;         // forward scratch
+    size_t grads, dr, back_local, last, part, back_scratch;   // backward scratch
 };
 Layout layout(const DeltaPlan &p) {
     Layout l{};
-    const size_t bh = (size_t)p.B * p.H, state = (size_t)p.D * p.Dv * 4, made = p.dtype == 0 ? Parts<float>::MADE : Parts<bf16_t>::MADE;
-    const size_t inv = bh * p.tiles * made * p.tile * p.tile * 2, between = p.segments > 1 ? bh * p.segments * state : 0;
+    const size_t bh = (size_t)p.B * p.H, state = (size_t)p.D * p.Dv * 4, rows = bh * p.N * p.Dv * 4;
+    const size_t inv = bh * p.tiles * (p.dtype == 0 ? Prepared<float>::BYTES : Prepared<bf16_t>::BYTES), between = p.segments > 1 ? bh * p.segments * state : 0;
     const size_t trans = p.segments > 1 ? bh * p.segments * p.D * p.D * 4 : 0;
-    l.inv = up(bh * p.tiles * state);
+    l.inv = up(bh * p.grad_tiles * state);
     l.trans = l.inv + up(inv);
-    l.cache = l.trans + up(trans);
+    l.w = l.trans + up(trans);
+    l.cache = l.w + up(rows);
     l.own_trans = up(inv);
     l.local = l.own_trans + up(trans);
     l.first = l.local + up(between);
     l.scratch = l.first + up(between);
-    l.dr = up(bh * p.tiles * state);
-    l.back_local = l.dr + up(bh * p.N * p.Dv * 4);
+    l.dr = up(bh * p.grad_tiles * state);
+    l.back_local = l.dr + up(rows);
     l.last = l.back_local + up(between);
     l.part = l.last + up(between);
     l.back_scratch = l.part + (p.key_heads < p.H ? 2 * up(bh * p.N * p.D * 4) : 0);
     return l;
 }
 DeltaCall call_of(const DeltaPlan &p, const DeltaArgs &a) {
-    return {p.B, p.H, p.key_heads, p.N, p.Dv, p.tiles, p.segments, p.seg_tiles, a.log_g, a.beta, a.len};
+    return {p.B, p.H, p.key_heads, p.N, p.Dv, p.tiles, p.segments, p.seg_tiles, p.grad_tiles, a.log_g, a.beta, a.len};
 }
-// f.template operator()<T, D>()
+// f.template operator()<T, D, DV>()
+template <typename T, typename F>
+hipError_t by_dims(const DeltaPlan &p, F f) {
+    if (p.D == 128) return p.Dv == 128 ? f.template operator()<T, 128, 128>() : f.template operator()<T, 128, 64>();
+    return p.Dv == 128 ? f.template operator()<T, 64, 128>() : f.template operator()<T, 64, 64>();
+}
 template <typename F>
-hipError_t by_type(const DeltaPlan &p, F f) {
-    if (p.dtype == 0) return p.D == 128 ? f.template operator()<float, 128>() : f.template operator()<float, 64>();
-    return p.D == 128 ? f.template operator()<bf16_t, 128>() : f.template operator()<bf16_t, 64>();
-}
+hipError_t by_type(const DeltaPlan &p, F f) { return p.dtype == 0 ? by_dims<float>(p, f) : by_dims<bf16_t>(p, f); }
 template <typename K>
 hipError_t room(K kernel, size_t bytes) { return allow_dynamic_lds((const void *)kernel, bytes); }
 
@@ -1035,36 +1177,36 @@ struct Forward {
     const DeltaPlan &p;
     const DeltaArgs &a;
     hipStream_t s;
-    template <typename T, int D>
+    template <typename T, int D, int DV>
     hipError_t operator()() const {
         const DeltaCall c = call_of(p, a);
         const int bh = p.B * p.H;
         const T *q = (const T *)a.q, *k = (const T *)a.k, *v = (const T *)a.v;
         if (!a.cache && p.N <= kDeltaStepTokens) {
             // narrower blocks of columns where 32 would not give every CU two workgroups
-            if (bh * (p.Dv / 32) >= 2 * kCus)
-                k_delta_step<T, D, 32><<<dim3(bh * (p.Dv / 32)), dim3(kThreads), 0, s>>>(q, k, v, a.kv_in, (T *)a.out, a.kv_out, c);
+            if (bh * (DV / 32) >= 2 * kCus)
+                k_delta_step<T, D, 32><<<dim3(bh * (DV / 32)), dim3(kThreads), 0, s>>>(q, k, v, a.kv_in, (T *)a.out, a.kv_out, c);
             else
-                k_delta_step<T, D, 16><<<dim3(bh * (p.Dv / 16)), dim3(kThreads), 0, s>>>(q, k, v, a.kv_in, (T *)a.out, a.kv_out, c);
+                k_delta_step<T, D, 16><<<dim3(bh * (DV / 16)), dim3(kThreads), 0, s>>>(q, k, v, a.kv_in, (T *)a.out, a.kv_out, c);
             return hipGetLastError();
         }
         const Layout l = layout(p);
         char *sc = (char *)a.scratch, *ca = (char *)a.cache;
-        bf16_t *inv = (bf16_t *)(ca ? ca + l.inv : sc);
+        char *inv = ca ? ca + l.inv : sc;
         float *trans = (float *)(ca ? ca + l.trans : sc + l.own_trans), *local = (float *)(sc + l.local), *first = (float *)(sc + l.first);
-        k_delta_prep<T, D><<<dim3(p.tiles, bh), dim3(kThreads), 0, s>>>(k, inv, c);
-        const int blocks = p.Dv / kDeltaCols;
-        typedef WalkLds<T, D> L;
-        WalkStates st{a.kv_in, a.kv_out, local, trans, (float *)ca, ca != nullptr};
+        k_delta_prep<T, D><<<dim3((p.tiles + kWaves - 1) / kWaves, bh), dim3(kThreads), 0, s>>>(q, k, inv, c);
+        WalkStates st{a.kv_in, a.kv_out, local, trans, (float *)ca, (float *)(ca ? ca + l.w : nullptr), ca != nullptr};
+        const dim3 grid(p.segments * bh);
         if (p.segments > 1) {
-            if (hipError_t e = room(k_delta_walk<T, D, true>, L::bytes(true)); e != hipSuccess) return e;
-            k_delta_walk<T, D, true><<<dim3((blocks + D / kDeltaCols) * p.segments * bh), dim3(kThreads), L::bytes(true), s>>>(
-                nullptr, k, v, inv, nullptr, st, c);
-            k_delta_scan<D, false><<<dim3(p.Dv / kScanCols, bh), dim3(kThreads), 0, s>>>(a.kv_in, trans, local, first, p.Dv, p.segments);
+            typedef Walk<T, D, DV, true> L;
+            if (hipError_t e = room(k_delta_walk<T, D, DV, true>, L::LDS); e != hipSuccess) return e;
+            k_delta_walk<T, D, DV, true><<<grid, dim3(L::NT), L::LDS, s>>>(nullptr, k, v, inv, nullptr, st, c);
+            k_delta_scan<D, false><<<dim3(bh, DV / kScanCols), dim3(kThreads), 0, s>>>(a.kv_in, trans, local, first, DV, p.segments);
             st.first = first;
         }
-        if (hipError_t e = room(k_delta_walk<T, D, false>, L::bytes(false)); e != hipSuccess) return e;
-        k_delta_walk<T, D, false><<<dim3(blocks * p.segments * bh), dim3(kThreads), L::bytes(false), s>>>(q, k, v, inv, (T *)a.out, st, c);
+        typedef Walk<T, D, DV, false> L;
+        if (hipError_t e = room(k_delta_walk<T, D, DV, false>, L::LDS); e != hipSuccess) return e;
+        k_delta_walk<T, D, DV, false><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, v, inv, (T *)a.out, st, c);
         return hipGetLastError();
     }
 };
@@ -1073,42 +1215,42 @@ struct Backward {
     const DeltaPlan &p;
     const DeltaArgs &a;
     hipStream_t s;
-    template <typename T, int D>
+    template <typename T, int D, int DV>
     hipError_t operator()() const {
         const DeltaCall c = call_of(p, a);
-        const int bh = p.B * p.H, blocks = p.Dv / kDeltaCols;
+        const int bh = p.B * p.H;
         const T *q = (const T *)a.q, *k = (const T *)a.k, *v = (const T *)a.v, *dout = (const T *)a.dout;
         const Layout l = layout(p);
         char *sc = (char *)a.scratch, *ca = (char *)a.cache;
-        const bf16_t *inv = (const bf16_t *)(ca + l.inv);
-        typedef BackLds<T, D> L;
+        const char *inv = ca + l.inv;
+        typedef Back<T, D, DV> L;
         float *last = (float *)(sc + l.last);
         BackStates st{a.dkv_out, a.dkv_in, (float *)(sc + l.back_local), (float *)sc, (float *)(sc + l.dr)};
-        const dim3 grid(blocks * p.segments * bh);
+        const dim3 grid(p.segments * bh);
         if (p.segments > 1) {
-            if (hipError_t e = room(k_delta_back<T, D, true>, L::ALL); e != hipSuccess) return e;
-            k_delta_back<T, D, true><<<grid, dim3(kThreads), L::ALL, s>>>(q, k, dout, inv, nullptr, st, c);
-            k_delta_scan<D, true><<<dim3(p.Dv / kScanCols, bh), dim3(kThreads), 0, s>>>(a.dkv_out, (const float *)(ca + l.trans), st.local, last, p.Dv,
-                                                                                     p.segments);
+            if (hipError_t e = room(k_delta_back<T, D, DV, true>, L::LDS); e != hipSuccess) return e;
+            k_delta_back<T, D, DV, true><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, dout, inv, nullptr, st, c);
+            k_delta_scan<D, true><<<dim3(bh, DV / kScanCols), dim3(kThreads), 0, s>>>(a.dkv_out, (const float *)(ca + l.trans), st.local, last, DV,
+                                                                                   p.segments);
             st.last = last;
         }
-        if (hipError_t e = room(k_delta_back<T, D, false>, L::ALL); e != hipSuccess) return e;
-        k_delta_back<T, D, false><<<grid, dim3(kThreads), L::ALL, s>>>(q, k, dout, inv, (T *)a.dv, st, c);
-        const dim3 tiles(p.tiles, bh);
-        if (p.key_heads == p.H) {
-            if (hipError_t e = room(k_delta_grad<T, D, T>, GradLds<T, D>::ALL); e != hipSuccess) return e;
-            k_delta_grad<T, D, T><<<tiles, dim3(kThreads), GradLds<T, D>::ALL, s>>>(q, k, v, dout, inv, (const float *)ca, st.grads, st.dr, (T *)a.dq,
-                                                                                 (T *)a.dk, a.dbeta, a.dlog_g, c);
-        } else {
-            const size_t n = (size_t)bh * p.N * D;
-            float *part = (float *)(sc + l.part);
-            if (hipError_t e = room(k_delta_grad<T, D, float>, GradLds<T, D>::ALL); e != hipSuccess) return e;
-            k_delta_grad<T, D, float><<<tiles, dim3(kThreads), GradLds<T, D>::ALL, s>>>(q, k, v, dout, inv, (const float *)ca, st.grads, st.dr, part,
-                                                                                     part + n, a.dbeta, a.dlog_g, c);
-            const int share = p.H / p.key_heads;
-            k_delta_group<T, D><<<dim3((unsigned)((n / share / 4 + kThreads - 1) / kThreads), 2), dim3(kThreads), 0, s>>>(part, (T *)a.dq, (T *)a.dk, n,
-                                                                                                                 share, p.N);
-        }
+        if (hipError_t e = room(k_delta_back<T, D, DV, false>, L::LDS); e != hipSuccess) return e;
+        k_delta_back<T, D, DV, false><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, dout, inv, (T *)a.dv, st, c);
+        if (p.key_heads == p.H) return grad<T, D>(c, (T *)a.dq, (T *)a.dk, st, l);
+        const size_t n = (size_t)bh * p.N * D;
+        float *part = (float *)(sc + l.part);
+        if (hipError_t e = grad<T, D>(c, part, part + n, st, l); e != hipSuccess) return e;
+        const int share = p.H / p.key_heads;
+        k_delta_group<T, D><<<dim3((unsigned)((n / share / 4 + kThreads - 1) / kThreads), 2), dim3(kThreads), 0, s>>>(part, (T *)a.dq, (T *)a.dk, n, share,
+                                                                                                             p.N);
+        return hipGetLastError();
+    }
+    template <typename T, int D, typename TO>
+    hipError_t grad(const DeltaCall &c, TO *dq, TO *dk, const BackStates &st, const Layout &l) const {
+        if (hipError_t e = room(k_delta_grad<T, D, TO>, Grad<T, D>::LDS); e != hipSuccess) return e;
+        k_delta_grad<T, D, TO><<<dim3(p.grad_tiles, p.B * p.H), dim3(kThreads), Grad<T, D>::LDS, s>>>(
+            (const T *)a.q, (const T *)a.k, (const T *)a.v, (const T *)a.dout, (const float *)a.cache, st.grads,
+            (const float *)((const char *)a.cache + l.w), st.dr, dq, dk, a.dbeta, a.dlog_g, c);
         return hipGetLastError();
     }
 };
@@ -1119,13 +1261,14 @@ struct Backward {
 // columns) and a chain of one step a segment, so it is cut where that leaves a third of the tiles or less.
 DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_heads) {
     DeltaPlan p{B, H, N, D, Dv, dtype, key_heads};
-    p.tile = dtype == 0 ? Parts<float>::C : Parts<bf16_t>::C;
-    p.tiles = (int)(((long long)N + p.tile - 1) / p.tile);
-    const long long walks = (long long)B * H * (Dv / kDeltaCols);
-    int cut = (int)std::min<long long>(kCus / std::min<long long>(walks, kCus), p.tiles / 4);
+    p.tiles = (int)(((long long)N + kTile - 1) / kTile);
+    const int together = dtype == 0 ? Parts<float>::GRAD_TILES : Parts<bf16_t>::GRAD_TILES;
+    p.grad_tiles = (p.tiles + together - 1) / together;
+    const long long walks = (long long)B * H;
+    int cut = (int)std::min<long long>(2 * kCus / std::min<long long>(walks, 2 * kCus), p.tiles / 8);
     while (cut > 1 && (long long)cut * cut > 2LL * p.tiles) --cut;
     if (cut < 3) cut = 1;
-    p.seg_tiles = (p.tiles + cut - 1) / cut;
+    p.seg_tiles = ((p.tiles + cut - 1) / cut + together - 1) / together * together;
     p.segments = (p.tiles + p.seg_tiles - 1) / p.seg_tiles;
     return p;
 }
