@@ -14,7 +14,7 @@
 //     dS' = exp(G_C) dS + Q^T (exp(G) dO) - K^T (exp(G) dV),   P_ij = W_ij q_i . k_j
 //     dQ = exp(G) dO S^T + Ep K,   dK = Ep^T Q + Em K + Em^T K - exp(G) dV S^T + exp(G_C - G) U dS^T,
 //     Ep = W (dO U^T),   Em = -W (dV U^T) below the diagonal,
-//     dlog_a_i = <dS, S'> + sum_{t >= i} (q_t . dq_t - v_t . dv_t)   (sums within the tile, so that they stay short).
+//     and dlog_a_i = a_i <dS_i - beta_i k_i (dS_i^T k_i)^T, S_{i-1}>, by what goes through gate i (k_delta_grad).
 //   k_delta_back : the walk in reverse: dV, and dS and dR of every tile
 //   k_delta_grad : dQ, dK, dbeta, dlog_a of every tile (tiles are independent)
 //   k_delta_group: sums over the states that share a head of q and k
@@ -36,12 +36,12 @@ template <typename T>
 struct Parts;
 template <>
 struct Parts<bf16_t> {
-    // parts of an input and of what is computed; tiles of the walks that k_delta_grad takes at a time
-    static constexpr int DATA = 1, MADE = 2, GRAD_TILES = 2;
+    // parts of an input, of what is computed, and of what only ends in outputs of the data's type; tiles of the walks that k_delta_grad takes at a time
+    static constexpr int DATA = 1, MADE = 3, ROUNDED = 2, GRAD_TILES = 2;
 };
 template <>
 struct Parts<float> {
-    static constexpr int DATA = 3, MADE = 3, GRAD_TILES = 1;
+    static constexpr int DATA = 3, MADE = 3, ROUNDED = 3, GRAD_TILES = 1;
 };
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTile = kDeltaTile;   // tokens of a walk's tile: one block of an MFMA
@@ -590,7 +590,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
                 for (int m = 0; m < 2; ++m) {
                     const auto s = split<MADE>(S[kb], m);
                     x = mm<MADE>(kt.kp(ln, 0, 32 * kb, m), s, x);
-                    if constexpr (!LOCAL) o = mm<MADE>(s, qt.kp(ln, 0, 32 * kb, m), o);
+                    if constexpr (!LOCAL) o = mm<P::ROUNDED>(s, qt.kp(ln, 0, 32 * kb, m), o);
                 }
             r -= by_row((const float *)(at + Pr::START), ln) * x;
             x = beta * r;
@@ -603,7 +603,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
         if constexpr (!LOCAL) {
             o *= ((const float *)(at + Pr::START))[ln.r];
 #pragma unroll
-            for (int m = 0; m < 2; ++m) o = mm<MADE>(split<MADE>(r, m), pt.kp(ln, m), o);
+            for (int m = 0; m < 2; ++m) o = mm<P::ROUNDED>(split<P::ROUNDED>(r, m), pt.kp(ln, m), o);
             if (ln.r < there) store_acc(O + (row + token0 + ln.r) * DV + c0, ln, o);
         }
         r *= by_row((const float *)(at + Pr::REST), ln);
@@ -634,15 +634,20 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
 // (v_mfma_f32_16x16x4_f32: lane l supplies row or column l & 15 and contraction index l >> 4; accumulator rows 4 (l >> 4) .. + 3, column l & 15.)
 constexpr int kScanCols = 16;
 template <int D, bool BACK>
-__global__ __launch_bounds__(kThreads) void k_delta_scan(const float *__restrict__ in, const float *__restrict__ trans, const float *__restrict__ local,
+__global__ __launch_bounds__(4 * D) void k_delta_scan(const float *__restrict__ in, const float *__restrict__ trans, const float *__restrict__ local,
                                                          float *__restrict__ states, int Dv, int segments) {
-    __shared__ float S[2][D][kScanCols + 1];
-    constexpr int TILES = D / 16 / kWaves;   // 16 rows each, a wave
+    __shared__ __attribute__((aligned(16))) float S[2][kScanCols][D + 4];   // a row per column
+    constexpr int TILES = 1;   // 16 rows a wave
     const int bh = blockIdx.x, c = blockIdx.y * kScanCols + (threadIdx.x & 15), wave = threadIdx.x >> 6, l16 = threadIdx.x & 15, l4 = threadIdx.x >> 4 & 3;
-    f32x4 x[TILES], add[TILES];
-    float m[TILES][D / 4];   // contraction 16 s + 4 l4 + i at 4 s + i
+    struct Step {
+        f32x4 add[TILES];
+        float m[TILES][D / 4];   // contraction 16 s + 4 l4 + i at 4 s + i
+    };
+    f32x4 x[TILES];
     auto at = [&](size_t segment, int tl, int i) { return (segment * D + 16 * (wave * TILES + tl) + 4 * l4 + i) * Dv + c; };
-    auto fetch = [&](int p) {
+    auto fetch = [&](Step &to, int step) {
+        if (step + 1 >= segments) return;
+        const int p = BACK ? segments - 1 - step : step;
         const float *t = trans + ((size_t)bh * segments + p) * D * D;
 #pragma unroll
         for (int tl = 0; tl < TILES; ++tl) {
@@ -651,42 +656,58 @@ __global__ __launch_bounds__(kThreads) void k_delta_scan(const float *__restrict
             for (int s = 0; s < D / 16; ++s) {
                 if constexpr (BACK) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) m[tl][4 * s + i] = t[(size_t)(16 * s + 4 * l4 + i) * D + d];
+                    for (int i = 0; i < 4; ++i) to.m[tl][4 * s + i] = t[(size_t)(16 * s + 4 * l4 + i) * D + d];
                 } else {
                     const f32x4 y = *(const f32x4 *)(t + (size_t)d * D + 16 * s + 4 * l4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) m[tl][4 * s + i] = y[i];
+                    for (int i = 0; i < 4; ++i) to.m[tl][4 * s + i] = y[i];
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) add[tl][i] = local[at((size_t)bh * segments + p, tl, i)];
+            for (int i = 0; i < 4; ++i) to.add[tl][i] = local[at((size_t)bh * segments + p, tl, i)];
         }
+    };
+    auto go = [&](const Step &now, int step) {   // the state in front of this step's segment is written, and taken through it
+        const int p = BACK ? segments - 1 - step : step;
+        auto &lds = S[step & 1];   // (read by the other waves until the barrier of the next step)
+#pragma unroll
+        for (int tl = 0; tl < TILES; ++tl) {
+            *(f32x4 *)(&lds[l16][16 * (wave * TILES + tl) + 4 * l4]) = x[tl];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) states[at((size_t)bh * segments + p, tl, i)] = x[tl][i];
+        }
+        if (step + 1 == segments) return;
+        __syncthreads();
+        f32x4 y[D / 16], z[TILES] = {};
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) y[s] = *(const f32x4 *)(&lds[l16][16 * s + 4 * l4]);
+#pragma unroll
+        for (int tl = 0; tl < TILES; ++tl) x[tl] = now.add[tl];
+        __builtin_amdgcn_sched_barrier(0);   // (all reads are on their way before the first product waits for one)
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int tl = 0; tl < TILES; ++tl) {   // (two chains a tile)
+                    auto &sum = i & 1 ? z[tl] : x[tl];
+                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(now.m[tl][4 * s + i], y[s][i], sum, 0, 0, 0);
+                }
+#pragma unroll
+        for (int tl = 0; tl < TILES; ++tl) x[tl] += z[tl];
     };
 #pragma unroll
     for (int tl = 0; tl < TILES; ++tl)
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[tl][i] = in ? in[at(bh, tl, i)] : 0.0f;
-    for (int step = 0; step < segments; ++step) {
-        const int p = BACK ? segments - 1 - step : step;
-        if (step + 1 < segments) fetch(p);
-        auto &lds = S[step & 1];   // (read by the other waves until the barrier of the next step)
-#pragma unroll
-        for (int tl = 0; tl < TILES; ++tl)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                states[at((size_t)bh * segments + p, tl, i)] = x[tl][i];
-                lds[16 * (wave * TILES + tl) + 4 * l4 + i][l16] = x[tl][i];
-            }
+    Step even, odd;   // (the next segment's matrix is on its way while one is used)
+    fetch(even, 0);
+    for (int step = 0; step < segments; step += 2) {
+        fetch(odd, step + 1);
+        go(even, step);
         if (step + 1 == segments) break;
-        __syncthreads();
-#pragma unroll
-        for (int tl = 0; tl < TILES; ++tl) x[tl] = add[tl];
-#pragma unroll
-        for (int s = 0; s < D / 4; ++s) {
-            const float y = lds[16 * (s / 4) + 4 * l4 + s % 4][l16];
-#pragma unroll
-            for (int tl = 0; tl < TILES; ++tl) x[tl] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[tl][s], y, x[tl], 0, 0, 0);
-        }
+        fetch(even, step + 2);
+        go(odd, step + 1);
     }
 }
 
@@ -886,36 +907,58 @@ struct Gates {
 template <typename T, int D>
 struct Grad {
     using P = Parts<T>;
-    static constexpr int NB = P::GRAD_TILES, C = NB * kTile, COLS = 64, SLICES = D / 32, PER = SLICES == kWaves ? NB : 1;   // PER: token blocks of a wave
+    static constexpr int NB = P::GRAD_TILES, C = NB * kTile, COLS = NB == 2 ? 32 : 64, SLICES = D / 32, WAVES = SLICES * NB, NT = 64 * WAVES;
     typedef Tile<P::DATA, C, D> Data;
-    typedef Lower<P::MADE, C> Square;
+    typedef Lower<P::ROUNDED, C> Square;
     typedef Tile<P::MADE, C, COLS> Rows;
     typedef Tile<P::DATA, C, COLS> Out;
-    static_assert(Square::BYTES <= Rows::BYTES && kWaves * (C + 1) * 4 + 2 * C * 4 <= Out::BYTES, "what comes later takes the places of rows");
-    static constexpr int K = 0, Q = K + Data::BYTES, U = Q + Data::BYTES, DV = U + Rows::BYTES, DO = DV + Rows::BYTES, G = DO + Out::BYTES,
+    static constexpr int JOBS = 2 * Square::BLOCKS, MINE = (JOBS + WAVES - 1) / WAVES;   // blocks of Ep and of Em; of a wave
+    struct Sums {   // by token: dbeta, row and column sums of Z (of a block), x and y (of a wave's key features); <dS, S>
+        float beta[C], row[JOBS][32], col[JOBS][32], up[SLICES][C], on[SLICES][C], both[SLICES];
+    };
+    static constexpr int PAIR = Rows::BYTES > Square::BYTES ? Rows::BYTES : Square::BYTES;   // (Ep and Em take the places of w and dR)
+    static constexpr int K = 0, Q = K + Data::BYTES, W = Q + Data::BYTES, DR = W + PAIR, DO = DR + PAIR, G = DO + Out::BYTES,
                          LDS = G + (int)((sizeof(Gates<C>) + 15) / 16 * 16);
+    static_assert(sizeof(Sums) <= Out::BYTES, "the sums take the place of dO");
+    // waves a SIMD: as many workgroups a CU as LDS has room for
+    static constexpr int PER_SIMD = NB == 2 ? (163840 / LDS * WAVES) / 4 : 1;
 };
+// Sums over the 32 lanes of a half wave of 16 values: lane r gets that of value r / 2 (two lanes each). By halves: 16 exchanges.
+DEVI float sum_lanes(const f32x16 &z, const Lane &ln) {
+    float v[8];
+    const bool b4 = ln.r & 16, b3 = ln.r & 8, b2 = ln.r & 4, b1 = ln.r & 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (b4 ? z[8 + i] : z[i]) + __shfl_xor(b4 ? z[i] : z[8 + i], 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (b3 ? v[4 + i] : v[i]) + __shfl_xor(b3 ? v[i] : v[4 + i], 8);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = (b2 ? v[2 + i] : v[i]) + __shfl_xor(b2 ? v[i] : v[2 + i], 4);
+    v[0] = (b1 ? v[1] : v[0]) + __shfl_xor(b1 ? v[0] : v[1], 2);
+    return v[0] + __shfl_xor(v[0], 1);
+}
 template <typename T, int D, typename TO>
-__global__ __launch_bounds__(kThreads, 1) void k_delta_grad(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ V,
-                                                            const T *__restrict__ dO, const float *__restrict__ states, const float *__restrict__ grads,
-                                                            const float *__restrict__ w, const float *__restrict__ dR, TO *__restrict__ dQ,
-                                                            TO *__restrict__ dK, float *__restrict__ dbeta, float *__restrict__ dlog_g, DeltaCall a) {
+__global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_delta_grad(const T *__restrict__ Q, const T *__restrict__ K,
+                                                                                   const T *__restrict__ dO, const float *__restrict__ states,
+                                                                                   const float *__restrict__ grads, const float *__restrict__ w,
+                                                                                   const float *__restrict__ dR, TO *__restrict__ dQ,
+                                                                                   TO *__restrict__ dK, float *__restrict__ dbeta,
+                                                                                   float *__restrict__ dlog_g, DeltaCall a) {
     using L = Grad<T, D>;
     using P = typename L::P;
-    constexpr int C = L::C, NB = L::NB, PER = L::PER, COLS = L::COLS, MADE = P::MADE;
+    constexpr int C = L::C, NB = L::NB, COLS = L::COLS, MADE = P::MADE, NT = L::NT, MINE = L::MINE;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const typename L::Data kt{(bf16_t *)(lds + L::K)}, qt{(bf16_t *)(lds + L::Q)};
-    const typename L::Rows ut{(bf16_t *)(lds + L::U)}, vt{(bf16_t *)(lds + L::DV)};
+    const typename L::Rows wt{(bf16_t *)(lds + L::W)}, rt{(bf16_t *)(lds + L::DR)};
     const typename L::Out dot{(bf16_t *)(lds + L::DO)};
-    const typename L::Square ep{ut.p}, em{vt.p};
+    const typename L::Square ep{wt.p}, em{rt.p};
     Gates<C> &g = *(Gates<C> *)(lds + L::G);
-    float *red = (float *)(lds + L::DO);   // [wave][C] q . dq, [wave] <dS, S'>, [C] dbeta, [C] v . dv
+    typename L::Sums &red = *(typename L::Sums *)(lds + L::DO);
     const Lane ln(threadIdx.x);
     const int wave = threadIdx.x >> 6, tile = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * C;
     const int valid = a.valid(b, token0, C), there = min(a.N - token0, C);
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N + token0;
     if (valid == 0) {
-        for (int e = threadIdx.x; e < there * D; e += kThreads) {
+        for (int e = threadIdx.x; e < there * D; e += NT) {
             Elem<TO>::st1(dQ + row * D + e, 0.0f);
             Elem<TO>::st1(dK + row * D + e, 0.0f);
         }
@@ -925,48 +968,39 @@ __global__ __launch_bounds__(kThreads, 1) void k_delta_grad(const T *__restrict_
         }
         return;
     }
-    const int d0 = 32 * (L::SLICES == kWaves ? wave : wave & 1), tk0 = L::SLICES == kWaves ? 0 : wave >> 1;
-    const bool active = tk0 < NB;
-
-    Fetch<T, C, D, kThreads> fk, fq;
-    Fetch<float, C, COLS, kThreads> fw, fr;
-    Fetch<T, C, COLS, kThreads> fo;
-    constexpr int ROWS = Fetch<float, C, COLS, kThreads>::N;
-    typedef typename std::conditional<sizeof(T) == 2, bf16x4, f32x4>::type Four;
-    Four fv[ROWS];
-    auto fetch = [&](int c0) {
+    const int slice = wave % L::SLICES, d0 = 32 * slice, tk = wave / L::SLICES;   // a wave's 32 key features and 32 tokens
+    // a wave's blocks of Ep (even) and Em (odd)
+    auto job = [&](int n) { return wave + n * L::WAVES; };
+    auto token_block = [](int j) { return j >= 2 ? 1 : 0; };
+    auto key_block = [](int j) { return j >= 4 ? 1 : 0; };
+    {
+        Fetch<T, C, D, NT> fk, fq;
+        fk.load(K + (key_row + token0) * D, D, valid);
+        fq.load(Q + (key_row + token0) * D, D, valid);
+        if (wave == 0) {
+            const bool in = ln.id < valid;
+            const double x = sum_up<C>(a.log_g && in ? to_base2(a.log_g[row + ln.id]) : 0.0, ln.id), all = __shfl(x, C - 1, C);
+            if (ln.id < C) {
+                g.sum[ln.id] = x;
+                g.start[ln.id] = power(x);
+                g.rest[ln.id] = power(all - x);
+                g.beta[ln.id] = in ? a.beta[row + ln.id] : 0.0f;
+            }
+            if (ln.id == 0) g.whole = power(all);
+        }
+        fk.store(kt);
+        fq.store(qt);
+    }
+    f32x16 pr[MINE] = {};                     // w dO^T or w dR^T, a row per key token
+    f32x16 aq = {}, a1 = {}, a2 = {};         // S dO^T, S dR^T, dS w^T, a row per key feature
+    float both = 0.0f;                        // <dS, S>
+    for (int c0 = 0; c0 < a.Dv; c0 += COLS) {
+        Fetch<float, C, COLS, NT> fw, fr;   // everything is on its way before the first of it is waited for
+        Fetch<T, C, COLS, NT> fo;
+        f32x4 s4[COLS / 16][2], d4[COLS / 16][2];
         fw.load(w + row * a.Dv + c0, a.Dv, valid);
         fr.load(dR + row * a.Dv + c0, a.Dv, valid);
         fo.load(dO + row * a.Dv + c0, a.Dv, valid);
-#pragma unroll
-        for (int n = 0; n < ROWS; ++n) {
-            const int c = threadIdx.x + n * kThreads, r = c / (COLS / 4);
-            fv[n] = Four{0, 0, 0, 0};
-            if (r < valid) fv[n] = *(const Four *)(V + (row + r) * a.Dv + c0 + c % (COLS / 4) * 4);
-        }
-    };
-    fk.load(K + (key_row + token0) * D, D, valid);
-    fq.load(Q + (key_row + token0) * D, D, valid);
-    fetch(0);
-    if (wave == 0) {
-        const bool in = ln.id < valid;
-        const double x = sum_up<C>(a.log_g && in ? to_base2(a.log_g[row + ln.id]) : 0.0, ln.id), all = __shfl(x, C - 1, C);
-        if (ln.id < C) {
-            g.sum[ln.id] = x;
-            g.start[ln.id] = power(x);
-            g.rest[ln.id] = power(all - x);
-            g.beta[ln.id] = in ? a.beta[row + ln.id] : 0.0f;
-        }
-        if (ln.id == 0) g.whole = power(all);
-    }
-    fk.store(kt);
-    fq.store(qt);
-
-    f32x16 ap = {}, am = {};                          // U dO^T, U dV^T, a row per key token
-    f32x16 aq[PER] = {}, a1[PER] = {}, a2[PER] = {};  // S dO^T, S dV^T, dS U^T, a row per key feature
-    float sum_b[ROWS] = {}, sum_v[ROWS] = {}, both = 0.0f;   // dR . w and v . dv of the rows this thread stages, <dS, S>
-    for (int c0 = 0; c0 < a.Dv; c0 += COLS) {
-        f32x4 s4[COLS / 16][2], d4[COLS / 16][2];
         const size_t state = (((size_t)bh * a.grad_tiles + tile) * D + d0 + ln.r) * a.Dv + c0 + 8 * ln.h;
 #pragma unroll
         for (int k = 0; k < COLS / 16; ++k)
@@ -975,140 +1009,146 @@ __global__ __launch_bounds__(kThreads, 1) void k_delta_grad(const T *__restrict_
                 s4[k][i] = *(const f32x4 *)(states + state + 16 * k + 4 * i);
                 d4[k][i] = *(const f32x4 *)(grads + state + 16 * k + 4 * i);
             }
-        __syncthreads();   // the gates are there; the tiles have been read
+        __builtin_amdgcn_sched_barrier(0);
+        if (c0 > 0) __syncthreads();   // the tiles have been read
         fo.store(dot);
-        fw.each([&](int n, int r, int col, u32x4 x) {
-            const f32x4 w4 = __builtin_bit_cast(f32x4, x), r4 = __builtin_bit_cast(f32x4, fr.v[n]), v4 = __builtin_convertvector(fv[n], f32x4);
-            const float beta = g.beta[r];
-            const f32x4 dv4 = beta * r4;
-            ut.st4(r, col, beta * w4);
-            vt.st4(r, col, dv4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sum_b[n] = __builtin_fmaf(r4[e], w4[e], sum_b[n]);
-                sum_v[n] = __builtin_fmaf(dv4[e], v4[e], sum_v[n]);
-            }
-        });
+        fw.store(wt);
+        fr.store(rt);
         __syncthreads();
-        if (c0 + COLS < a.Dv) fetch(c0 + COLS);
-        if (wave < L::Square::BLOCKS) {
-            const int tb = wave > 0, jb = wave == 2;
 #pragma unroll
-            for (int k0 = 0; k0 < COLS; k0 += 16) {
-                const auto u = ut.kc(ln, 32 * jb, k0);
-                ap = mm<MADE>(u, dot.kc(ln, 32 * tb, k0), ap);
-                am = mm<MADE>(u, vt.kc(ln, 32 * tb, k0), am);
-            }
+        for (int k = 0; k < COLS / 16; ++k) {
+            const auto fs = split<MADE>(__builtin_shufflevector(s4[k][0], s4[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
+            aq = mm<MADE>(fs, dot.kc(ln, 32 * tk, 16 * k), aq);
+            a1 = mm<MADE>(fs, rt.kc(ln, 32 * tk, 16 * k), a1);
+            if (tk == 0)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) both = __builtin_fmaf(s4[k][i][e], d4[k][i][e], both);
+            const auto fd = split<MADE>(__builtin_shufflevector(d4[k][0], d4[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
+            a2 = mm<MADE>(fd, wt.kc(ln, 32 * tk, 16 * k), a2);
         }
-        if (active)
 #pragma unroll
-            for (int k = 0; k < COLS / 16; ++k) {
-                const f32x8 x = __builtin_shufflevector(s4[k][0], s4[k][1], 0, 1, 2, 3, 4, 5, 6, 7);
-                const f32x8 y = __builtin_shufflevector(d4[k][0], d4[k][1], 0, 1, 2, 3, 4, 5, 6, 7);
-                if (tk0 == 0)
+        for (int n = 0; n < MINE; ++n)
+            if (job(n) < L::JOBS) {
+                const int j = job(n), tb = token_block(j), jb = key_block(j);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) both = __builtin_fmaf(x[e], y[e], both);
-                const auto fs = split<MADE>(x), fd = split<MADE>(y);
-#pragma unroll
-                for (int n = 0; n < PER; ++n) {
-                    const int at = 32 * (tk0 + n);
-                    aq[n] = mm<MADE>(fs, dot.kc(ln, at, 16 * k), aq[n]);
-                    a1[n] = mm<MADE>(fs, vt.kc(ln, at, 16 * k), a1[n]);
-                    a2[n] = mm<MADE>(fd, ut.kc(ln, at, 16 * k), a2[n]);
+                for (int k0 = 0; k0 < COLS; k0 += 16) {
+                    const auto u = wt.kc(ln, 32 * jb, k0);
+                    if (j & 1) pr[n] = mm<MADE>(u, rt.kc(ln, 32 * tb, k0), pr[n]);
+                    else pr[n] = mm<MADE>(u, dot.kc(ln, 32 * tb, k0), pr[n]);
                 }
             }
     }
     __syncthreads();
-    if (wave < L::Square::BLOCKS) {
-        const int tb = wave > 0, jb = wave == 2, i = 32 * tb + ln.r;
-        const double gi = g.sum[i];
+    // dlog_a_i = exp(G_C) <dS, S> + sum_{t >= i} x_t + sum_{j < i} y_j + sum_{t >= i > j} Z_tj: what goes through gate i and nothing else, with
+    // x_t = exp(G_t) (q_t . S dO_t - k_t . S dV_t), y_j = exp(G_C - G_j) k_j . dS u_j and Z = Ep q.k + Em k.k. Row and column sums of Z give the last one.
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int j = 32 * jb + ln.acc_row(e);
-            const float x = j <= i ? power(gi - g.sum[j]) : 0.0f;
-            ap[e] *= x;
-            am[e] *= j < i ? -x : 0.0f;
-        }
-        ep.at(tb, jb).st_acc(ln, ap);
-        em.at(tb, jb).st_acc(ln, am);
-    }
-    float *red_phi = red + kWaves * C, *red_b = red_phi + kWaves, *red_v = red_b + C;
+    for (int n = 0; n < MINE; ++n)
+        if (job(n) < L::JOBS) {
+            const int jo = job(n), tb = token_block(jo), jb = key_block(jo), i = 32 * tb + ln.r;
+            const bool is_em = jo & 1;
+            const double gi = g.sum[i];
+            f32x16 z = {};   // k_j . q_i or k_j . k_i
+            if (dlog_g)
 #pragma unroll
-    for (int n = 0; n < ROWS; ++n) {
+                for (int k0 = 0; k0 < D; k0 += 16) {
+                    const auto x = kt.kc(ln, 32 * jb, k0);
+                    z = is_em ? mm<MADE>(x, kt.kc(ln, 32 * tb, k0), z) : mm<MADE>(x, qt.kc(ln, 32 * tb, k0), z);
+                }
+            float along = 0.0f;
+            const float bi = is_em ? g.beta[i] : 1.0f;
 #pragma unroll
-        for (int d = 1; d < COLS / 4; d *= 2) {
-            sum_b[n] += __shfl_xor(sum_b[n], d);
-            sum_v[n] += __shfl_xor(sum_v[n], d);
+            for (int e = 0; e < 16; ++e) {
+                const int j = 32 * jb + ln.acc_row(e);
+                if (is_em && j == i) red.beta[i] = pr[n][e];   // dbeta_i = w_i . dR_i
+                const float x = j <= i ? g.beta[j] * bi * power(gi - g.sum[j]) : 0.0f;
+                pr[n][e] *= is_em ? (j < i ? -x : 0.0f) : x;
+                z[e] = j < i ? pr[n][e] * z[e] : 0.0f;
+                along += z[e];
+            }
+            if (dlog_g) {
+                along += __shfl_xor(along, 32);
+                const float down = sum_lanes(z, ln);
+                if (ln.h == 0) red.row[jo][ln.r] = along;
+                if ((ln.r & 1) == 0) red.col[jo][ln.acc_row(ln.r >> 1)] = down;
+            }
+            const auto to = is_em ? em.at(tb, jb) : ep.at(tb, jb);
+            to.st_acc(ln, pr[n]);
         }
-        const int c = threadIdx.x + n * kThreads;
-        if (c % (COLS / 4) == 0) {
-            red_b[c / (COLS / 4)] = sum_b[n];
-            red_v[c / (COLS / 4)] = sum_v[n];
-        }
-    }
-    for (int e = threadIdx.x; e < kWaves * C; e += kThreads) red[e] = 0.0f;
     __syncthreads();
-    float phi = g.whole * both;
-    if (active)
-#pragma unroll
-        for (int n = 0; n < PER; ++n) {
-            const int tk = tk0 + n, m = 32 * tk + ln.r;
-            const float start = g.start[m], rest = g.rest[m];
-            const size_t to = (row + m) * D + d0;   // (shared heads: a partial sum for every state, in float)
-            f32x16 x = aq[n] * start;
-            for (int jb = 0; jb <= tk; ++jb)
-#pragma unroll
-                for (int k0 = 0; k0 < 32; k0 += 16) x = mm<MADE>(kt.ks(ln, 32 * jb + k0, d0), ep.at(tk, jb).kc(ln, k0), x);
-            f32x16 y = a2[n] * rest;
-            float sum_q = 0.0f;
+    const int m = 32 * tk + ln.r;
+    {
+        const float start = g.start[m], rest = g.rest[m];
+        const size_t to = (row + m) * D + d0;   // (shared heads: a partial sum for every state, in float)
+        aq *= start;
+        a1 *= start * g.beta[m];
+        a2 *= rest * g.beta[m];
+        if (dlog_g) {
+            float up = 0.0f, on = 0.0f;
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
                 const f32x4 q4 = qt.get4(m, d0 + 8 * f + 4 * ln.h), k4 = kt.get4(m, d0 + 8 * f + 4 * ln.h);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sum_q = __builtin_fmaf(q4[e], x[4 * f + e], sum_q);
-                    phi = __builtin_fmaf(k4[e], y[4 * f + e], phi);
+                    up = __builtin_fmaf(q4[e], aq[4 * f + e], __builtin_fmaf(-k4[e], a1[4 * f + e], up));
+                    on = __builtin_fmaf(k4[e], a2[4 * f + e], on);
                 }
             }
-            if (m < there) store_acc(dQ + to, ln, x);
-            y -= a1[n] * start;
-            for (int it = tk; it < NB; ++it)
-#pragma unroll
-                for (int k0 = 0; k0 < 32; k0 += 16) {
-                    y = mm<MADE>(qt.ks(ln, 32 * it + k0, d0), ep.at(it, tk).ks(ln, k0), y);
-                    y = mm<MADE>(kt.ks(ln, 32 * it + k0, d0), em.at(it, tk).ks(ln, k0), y);
-                }
-            for (int jb = 0; jb <= tk; ++jb)
-#pragma unroll
-                for (int k0 = 0; k0 < 32; k0 += 16) y = mm<MADE>(kt.ks(ln, 32 * jb + k0, d0), em.at(tk, jb).kc(ln, k0), y);
-            if (m < there) store_acc(dK + to, ln, y);
-            sum_q += __shfl_xor(sum_q, 32);
-            if (ln.h == 0) red[wave * C + m] = sum_q;
+            up += __shfl_xor(up, 32);
+            on += __shfl_xor(on, 32);
+            if (ln.h == 0) {
+                red.up[slice][m] = up;
+                red.on[slice][m] = on;
+            }
         }
+        for (int jb = 0; jb <= tk; ++jb)
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) phi += __shfl_xor(phi, d);
-    if (ln.id == 0) red_phi[wave] = phi;
+            for (int k0 = 0; k0 < 32; k0 += 16) aq = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), ep.at(tk, jb).kc(ln, k0), aq);
+        if (m < there) store_acc(dQ + to, ln, aq);
+        a2 -= a1;
+        for (int it = tk; it < NB; ++it)
+#pragma unroll
+            for (int k0 = 0; k0 < 32; k0 += 16) {
+                a2 = mm<P::ROUNDED>(qt.ks(ln, 32 * it + k0, d0), ep.at(it, tk).ks(ln, k0), a2);
+                a2 = mm<P::ROUNDED>(kt.ks(ln, 32 * it + k0, d0), em.at(it, tk).ks(ln, k0), a2);
+            }
+        for (int jb = 0; jb <= tk; ++jb)
+#pragma unroll
+            for (int k0 = 0; k0 < 32; k0 += 16) a2 = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), em.at(tk, jb).kc(ln, k0), a2);
+        if (m < there) store_acc(dK + to, ln, a2);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) both += __shfl_xor(both, d);
+    if (ln.id == 0 && tk == 0) red.both[slice] = both;
     __syncthreads();
     if (wave != 0) return;
-    double x = 0.0, all = 0.0;
+    if (ln.id < there) dbeta[row + ln.id] = red.beta[ln.id];
+    if (!dlog_g) return;
+    double up = 0.0, on = 0.0, all = 0.0;   // x_t;  y_j + column j - row j of Z
     if (ln.id < C) {
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) x += red[v * C + ln.id];
-        x -= red_v[ln.id];
+        for (int v = 0; v < L::SLICES; ++v) {
+            up += red.up[v][ln.id];
+            on += red.on[v][ln.id];
+        }
+#pragma unroll
+        for (int v = 0; v < L::JOBS; ++v) {
+            if (key_block(v) == ln.id / 32) on += red.col[v][ln.id & 31];
+            if (token_block(v) == ln.id / 32) on -= red.row[v][ln.id & 31];
+        }
     }
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) all += red_phi[v];
+    for (int v = 0; v < L::SLICES; ++v) all += red.both[v];
+    on = sum_up<C>(on, ln.id) - on;         // over the tokens before this one
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
-        const double y = __shfl_down(x, d, C);
-        if ((ln.id & (C - 1)) + d < C) x += y;
+        const double y = __shfl_down(up, d, C);
+        if ((ln.id & (C - 1)) + d < C) up += y;
     }
     if (ln.id < there) {
-        dbeta[row + ln.id] = red_b[ln.id];
-        if (dlog_g) {
-            const bool none = ln.id >= valid || to_base2(a.log_g[row + ln.id]) <= -150.0;   // (a gate of 0 has no slope)
-            dlog_g[row + ln.id] = none ? 0.0f : (float)(all + x);
-        }
+        const bool none = ln.id >= valid || to_base2(a.log_g[row + ln.id]) <= -150.0;   // (a gate of 0 has no slope)
+        dlog_g[row + ln.id] = none ? 0.0f : (float)(g.whole * all + up + on);
     }
 }
 
@@ -1201,7 +1241,7 @@ struct Forward {
             typedef Walk<T, D, DV, true> L;
             if (hipError_t e = room(k_delta_walk<T, D, DV, true>, L::LDS); e != hipSuccess) return e;
             k_delta_walk<T, D, DV, true><<<grid, dim3(L::NT), L::LDS, s>>>(nullptr, k, v, inv, nullptr, st, c);
-            k_delta_scan<D, false><<<dim3(bh, DV / kScanCols), dim3(kThreads), 0, s>>>(a.kv_in, trans, local, first, DV, p.segments);
+            k_delta_scan<D, false><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.kv_in, trans, local, first, DV, p.segments);
             st.first = first;
         }
         typedef Walk<T, D, DV, false> L;
@@ -1230,7 +1270,7 @@ struct Backward {
         if (p.segments > 1) {
             if (hipError_t e = room(k_delta_back<T, D, DV, true>, L::LDS); e != hipSuccess) return e;
             k_delta_back<T, D, DV, true><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, dout, inv, nullptr, st, c);
-            k_delta_scan<D, true><<<dim3(bh, DV / kScanCols), dim3(kThreads), 0, s>>>(a.dkv_out, (const float *)(ca + l.trans), st.local, last, DV,
+            k_delta_scan<D, true><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.dkv_out, (const float *)(ca + l.trans), st.local, last, DV,
                                                                                    p.segments);
             st.last = last;
         }
@@ -1248,8 +1288,8 @@ struct Backward {
     template <typename T, int D, typename TO>
     hipError_t grad(const DeltaCall &c, TO *dq, TO *dk, const BackStates &st, const Layout &l) const {
         if (hipError_t e = room(k_delta_grad<T, D, TO>, Grad<T, D>::LDS); e != hipSuccess) return e;
-        k_delta_grad<T, D, TO><<<dim3(p.grad_tiles, p.B * p.H), dim3(kThreads), Grad<T, D>::LDS, s>>>(
-            (const T *)a.q, (const T *)a.k, (const T *)a.v, (const T *)a.dout, (const float *)a.cache, st.grads,
+        k_delta_grad<T, D, TO><<<dim3(p.grad_tiles, p.B * p.H), dim3(Grad<T, D>::NT), Grad<T, D>::LDS, s>>>(
+            (const T *)a.q, (const T *)a.k, (const T *)a.dout, (const float *)a.cache, st.grads,
             (const float *)((const char *)a.cache + l.w), st.dr, dq, dk, a.dbeta, a.dlog_g, c);
         return hipGetLastError();
     }
