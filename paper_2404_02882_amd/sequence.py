@@ -246,3 +246,62 @@ class RecurrenceSequence:
                               lens[t] if lens else None, dout[t], self.dh[t + 1] if t + 1 < self.T or dh_out is not None else None, dx[t],
                               dlog_a[t], self.dh[t], self.scratch)
         return self.dh[0]
+
+
+class DeltaSequence:
+    """Gated delta rule (lasp_delta_*) over T sub-sequences: kv_out of one is kv_in of the next, dkv_in of one the dkv_out of the one
+    before, as LaspSequence hands its states on.
+
+    q, k, dq, dk are lists of T tensors [B,key_heads,N/T,D], v, out, dout, dv of [B,H,N/T,Dv], log_g (None: no decay), beta and their gradients of
+    float32 [B,H,N/T]. All buffers are allocated once, up front; the calls only enqueue kernels and can be captured
+    (GraphedStep).
+    """
+
+    def __init__(self, B, H, N, D, dtype: torch.dtype, T=1, Dv=0, key_heads=0, device="cuda", need_backward=True):
+        if N % T != 0:
+            raise ValueError("N must be a multiple of T")
+        self.T = T
+        self.shape = lasp.make_delta_shape(B, H, N // T, D, dtype, Dv, key_heads)
+        rc = lasp.check_delta(self.shape)
+        if rc != 0:
+            raise lasp.LaspError(rc, "DeltaSequence")
+        need = lasp.delta_scratch_bytes(self.shape)
+        if need_backward:
+            need = max(need, lasp.delta_bwd_scratch_bytes(self.shape))
+        room = dict(dtype=torch.uint8, device=device)
+        self.scratch = torch.empty(need, **room)
+        self.caches = [torch.empty(lasp.delta_cache_bytes(self.shape), **room) if need_backward else None for _ in range(T)]
+        # kv[t] = state entering sub-sequence t (kv[T] = final); dkv[t] = gradient w.r.t. kv[t]
+        state = dict(dtype=torch.float32, device=device)
+        self.kv = [torch.zeros(B, H, D, Dv or D, **state) for _ in range(T + 1)]
+        self.dkv = [torch.zeros(B, H, D, Dv or D, **state) for _ in range(T + 1)] if need_backward else None
+
+    def _check(self, **lists) -> None:
+        """A list that is too short is refused before the first sub-sequence runs."""
+        for name, tensors in lists.items():
+            if tensors is not None and len(tensors) < self.T:
+                raise ValueError(f"{name}: {len(tensors)} tensors for {self.T} sub-sequences")
+
+    def forward(self, q: List[torch.Tensor], k, v, log_g, beta, out: List[torch.Tensor], kv_in: Optional[torch.Tensor] = None,
+                lens: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
+        """lens: per sub-sequence the int32 [B] tokens that each sequence has in it (None: all)."""
+        self._check(q=q, k=k, v=v, log_g=log_g, beta=beta, out=out, lens=lens)
+        if kv_in is not None:
+            self.kv[0].copy_(kv_in)
+        for t in range(self.T):
+            lasp.lasp_delta_fwd(self.shape, q[t], k[t], v[t], log_g[t] if log_g else None, beta[t],
+                                self.kv[t] if t or kv_in is not None else None, lens[t] if lens else None, out[t], self.kv[t + 1],
+                                self.caches[t], self.scratch)
+        return self.kv[self.T]
+
+    def backward(self, q, k, v, log_g, beta, dout, dq, dk, dv, dlog_g, dbeta, dkv_out: Optional[torch.Tensor] = None,
+                 lens: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
+        """After forward over the same tensors."""
+        self._check(q=q, k=k, v=v, log_g=log_g, beta=beta, dout=dout, dq=dq, dk=dk, dv=dv, dlog_g=dlog_g, dbeta=dbeta, lens=lens)
+        if dkv_out is not None:
+            self.dkv[self.T].copy_(dkv_out)
+        for t in reversed(range(self.T)):
+            lasp.lasp_delta_bwd(self.shape, q[t], k[t], v[t], log_g[t] if log_g else None, beta[t], lens[t] if lens else None, dout[t],
+                                self.dkv[t + 1] if t + 1 < self.T or dkv_out is not None else None, self.caches[t], dq[t], dk[t], dv[t],
+                                dlog_g[t] if log_g else None, dbeta[t], self.dkv[t], self.scratch)
+        return self.dkv[0]
