@@ -61,6 +61,9 @@ DEVI f32x16 mm(const Frags<NA> &a, const Frags<NB> &b, f32x16 c) {
     return c;
 }
 
+// The wave's number, as the scalar that it is: what is addressed by it then takes scalar registers.
+DEVI int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 constexpr int ld_of(int width) { return width == 128 ? kSwzLd : width + E::PAD; }
 
 // Two transposing reads: lane i of 16 gets column i of the four rows that the lanes point to in pieces of four.
@@ -231,6 +234,17 @@ struct Tile {
         for (int i = 0; i < NP; ++i) f.p[i] = transposed(lo + i * PS, hi + i * PS);
         return f;
     }
+    // the 32 rows of a tile in the order of an accumulator's, a lane per column (one part)
+    DEVI f32x16 rows(const Lane &ln, int col0) const {
+        f32x16 x;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f32x8 y = __builtin_convertvector(ksp(ln, 0, col0, m).p[0], f32x8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[8 * m + e] = y[e];
+        }
+        return x;
+    }
     // an accumulator tile, transposed: its column r is row row0 + r here, its rows are columns col0 ..
     DEVI void st_acc(const Lane &ln, int row0, int col0, const f32x16 &t) const {
 #pragma unroll
@@ -382,7 +396,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
     __shared__ __attribute__((aligned(16))) float lds_m[kWaves][kTile * LDM], lds_n[kWaves][kTile * LDM], lds_beta[kWaves][kTile];
     __shared__ double lds_sum[kWaves][kTile];
     const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6, tile = blockIdx.x * kWaves + wave, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * kTile;
+    const int wave = wave_id(), tile = blockIdx.x * kWaves + wave, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * kTile;
     float *M = lds_m[wave], *N = lds_n[wave], *beta = lds_beta[wave];
     double *sum = lds_sum[wave];
     const int valid = tile < a.tiles ? a.valid(b, token0, kTile) : 0;
@@ -468,44 +482,43 @@ DEVI f32x16 by_row(const float *w, const Lane &ln) {
     }
     return x;
 }
-// Values of the lane's column in rows of LD elements, in the order of an accumulator tile's rows; `there`: rows that exist.
+// Values of the lane's column in rows of LD elements, in the order of an accumulator tile's rows; `there`: rows that exist. A scalar base every
+// eight rows, so that a row is at most an instruction's own offset away from it.
 template <int LD, typename T>
 DEVI f32x16 load_rows(const T *p, const Lane &ln, int there) {
-    f32x16 x;
-    p += 4 * ln.h * LD;
-    if (there >= 32)
+    f32x16 x = {};
+    const unsigned at = (4 * ln.h * LD + ln.r) * sizeof(T);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = Elem<T>::ld1(p + (8 * (e >> 2) + (e & 3)) * LD);
-    else
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = ln.acc_row(e) < there ? Elem<T>::ld1(p + (8 * (e >> 2) + (e & 3)) * LD) : 0.0f;
+    for (int e = 0; e < 16; ++e) {
+        const T *row = p + (8 * (e >> 2)) * LD;
+        if (there >= 32 || ln.acc_row(e) < there) {
+            const T v = gload<T>(row, at + (e & 3) * LD * sizeof(T));
+            x[e] = Elem<T>::ld1(&v);
+        }
+    }
     return x;
 }
 template <int LD, typename T>
 DEVI void store_rows(T *p, const Lane &ln, int there, const f32x16 &x) {
-    p += 4 * ln.h * LD;
+    const unsigned at = (4 * ln.h * LD + ln.r) * sizeof(T);
     if (there >= 32)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) Elem<T>::st1(p + (8 * (e >> 2) + (e & 3)) * LD, x[e]);
+        for (int e = 0; e < 16; ++e) Elem<T>::gst1(p + (8 * (e >> 2)) * LD, at + (e & 3) * LD * sizeof(T), x[e]);
     else
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-            if (ln.acc_row(e) < there) Elem<T>::st1(p + (8 * (e >> 2) + (e & 3)) * LD, x[e]);
+            if (ln.acc_row(e) < there) Elem<T>::gst1(p + (8 * (e >> 2)) * LD, at + (e & 3) * LD * sizeof(T), x[e]);
 }
 // A wave's part of a state: KB blocks of 32 key features (rows) by its 32 columns (a lane each).
-template <int KB>
-DEVI void load_state(f32x16 (&S)[KB], const Lane &ln, const float *src, int ld) {
+template <int KB, int LD>
+DEVI void load_state(f32x16 (&S)[KB], const Lane &ln, const float *src) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) S[kb][e] = src ? src[(size_t)(32 * kb + ln.acc_row(e)) * ld + ln.r] : 0.0f;
+    for (int kb = 0; kb < KB; ++kb) S[kb] = src ? load_rows<LD>(src + 32 * kb * LD, ln, 32) : f32x16{};
 }
-template <int KB>
-DEVI void save_state(const f32x16 (&S)[KB], const Lane &ln, float *dst, int ld) {
+template <int KB, int LD>
+DEVI void save_state(const f32x16 (&S)[KB], const Lane &ln, float *dst) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) dst[(size_t)(32 * kb + ln.acc_row(e)) * ld + ln.r] = S[kb][e];
+    for (int kb = 0; kb < KB; ++kb) store_rows<LD>(dst + 32 * kb * LD, ln, 32, S[kb]);
 }
 
 // ---------------------------------------------------------------------------
@@ -519,7 +532,10 @@ struct Walk {
     using P = Parts<T>;
     static constexpr int KB = D / 32, WAVES = (DV + (LOCAL ? D : 0)) / 32, NT = 64 * WAVES;
     typedef Tile<P::DATA, kTile, D> Data;
-    static constexpr int PREP = 0, K = Prepared<T>::BYTES, Q = K + Data::BYTES, STAGE = LOCAL ? Q : Q + Data::BYTES, LDS = 2 * STAGE;
+    typedef Tile<1, kTile, DV> Value;
+    static constexpr bool STAGED = sizeof(T) == 2;   // two-byte values go through LDS, which hands a lane four tokens of its column at a time
+    static constexpr int PREP = 0, K = Prepared<T>::BYTES, V = K + Data::BYTES, Q = V + (STAGED ? Value::BYTES : 0),
+                         STAGE = LOCAL ? Q : Q + Data::BYTES, LDS = 2 * STAGE;
 };
 struct WalkStates {
     const float *first;   // states that segments start from ([head][segment], or kv_in where there is one segment); null = zeros
@@ -539,7 +555,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
     constexpr int KB = L::KB, MADE = P::MADE;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
+    const int wave = wave_id(), seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
     if (LOCAL && seg == a.segments - 1 && !st.all_trans) return;
     const bool trans = LOCAL && wave >= DV / 32;
     const int c0 = 32 * (trans ? wave - DV / 32 : wave);
@@ -553,17 +569,19 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
 #pragma unroll
             for (int e = 0; e < 16; ++e) S[kb][e] = 32 * kb + ln.acc_row(e) == c0 + ln.r ? 1.0f : 0.0f;
     } else {
-        load_state<KB>(S, ln, LOCAL || !st.first ? nullptr : st.first + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
+        load_state<KB, DV>(S, ln, LOCAL || !st.first ? nullptr : st.first + ((size_t)bh * a.segments + seg) * D * DV + c0);
     }
     Fetch<T, kTile, D, L::NT> fk, fq;
     Copy<Pr::BYTES, L::NT> fp;
-    f32x16 v = {};
+    Fetch<T, kTile, DV, L::NT> fv;   // (STAGED)
+    f32x16 v = {};                   // (else)
     auto fetch = [&](int t) {
         const int token0 = t * kTile, valid = min(tokens - token0, kTile);
         fp.load(prepared + ((size_t)bh * a.tiles + t) * Pr::BYTES);
         fk.load(K + (key_row + token0) * D, D, valid);
         if constexpr (!LOCAL) fq.load(Q + (key_row + token0) * D, D, valid);
-        if (!trans) v = load_rows<DV>(V + (row + token0) * DV + c0 + ln.r, ln, valid);
+        if constexpr (L::STAGED) fv.load(V + (row + token0) * DV, DV, valid);
+        else if (!trans) v = load_rows<DV>(V + (row + token0) * DV + c0, ln, valid);
     };
     if (t0 < t1) fetch(t0);
     for (int t = t0; t < t1; ++t) {
@@ -574,13 +592,14 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
         fp.store(at);
         fk.store(kt);
         if constexpr (!LOCAL) fq.store(qt);
+        const typename L::Value vt{(bf16_t *)(at + L::V)};
+        if constexpr (L::STAGED) fv.store(vt);
         f32x16 r = v;
         __syncthreads();
         if (t + 1 < t1) fetch(t + 1);
         if constexpr (!LOCAL)
             if (st.cache && t % P::GRAD_TILES == 0)
-                save_state<KB>(S, ln, st.cache + ((size_t)bh * a.grad_tiles + t / P::GRAD_TILES) * D * DV + c0, DV);
-        const f32x16 beta = by_row((const float *)(at + Pr::BETA), ln);
+                save_state<KB, DV>(S, ln, st.cache + ((size_t)bh * a.grad_tiles + t / P::GRAD_TILES) * D * DV + c0);
         f32x16 o = {};   // r: a row per token;  o: a lane per token, a row per column
         {
             f32x16 x = {};
@@ -592,14 +611,16 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
                     x = mm<MADE>(kt.kp(ln, 0, 32 * kb, m), s, x);
                     if constexpr (!LOCAL) o = mm<P::ROUNDED>(s, qt.kp(ln, 0, 32 * kb, m), o);
                 }
+            if constexpr (L::STAGED)
+                if (!trans) r = vt.rows(ln, c0);
             r -= by_row((const float *)(at + Pr::START), ln) * x;
-            x = beta * r;
+            x = by_row((const float *)(at + Pr::BETA), ln) * r;
 #pragma unroll
             for (int m = 0; m < 2; ++m) r = mm<MADE>(nt.kp(ln, m), split<MADE>(x, m), r);
         }
         if constexpr (!LOCAL)
-            if (st.cache) store_rows<DV>(st.w + (row + token0) * DV + c0 + ln.r, ln, there, r);
-        r *= beta;
+            if (st.cache) store_rows<DV>(st.w + (row + token0) * DV + c0, ln, there, r);
+        r *= by_row((const float *)(at + Pr::BETA), ln);
         if constexpr (!LOCAL) {
             o *= ((const float *)(at + Pr::START))[ln.r];
 #pragma unroll
@@ -618,12 +639,12 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
         }
     }
     if constexpr (LOCAL) {
-        if (trans) save_state<KB>(S, ln, st.trans + ((size_t)bh * a.segments + seg) * D * D + c0, D);
-        else save_state<KB>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
+        if (trans) save_state<KB, D>(S, ln, st.trans + ((size_t)bh * a.segments + seg) * D * D + c0);
+        else save_state<KB, DV>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0);
     } else {
         for (int t = max(t0, t1); t < end; ++t)
-            store_rows<DV>(O + (row + t * kTile) * DV + c0 + ln.r, ln, min(a.N - t * kTile, kTile), f32x16{});
-        if (seg == a.segments - 1) save_state<KB>(S, ln, st.last + (size_t)bh * D * DV + c0, DV);
+            store_rows<DV>(O + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
+        if (seg == a.segments - 1) save_state<KB, DV>(S, ln, st.last + (size_t)bh * D * DV + c0);
     }
 }
 
@@ -812,16 +833,16 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
     constexpr int KB = L::KB, MADE = P::MADE, GT = P::GRAD_TILES;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6, c0 = 32 * wave, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
+    const int wave = wave_id(), c0 = 32 * wave, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
     if (LOCAL && seg == 0) return;
     const int tokens = a.valid(b, 0, a.N), end = min(a.tiles, (seg + 1) * a.seg_tiles);
     const int t0 = seg * a.seg_tiles, t1 = min(end, (tokens + kTile - 1) / kTile);
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N;
     f32x16 S[KB];
-    load_state<KB>(S, ln, LOCAL || !st.last ? nullptr : st.last + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
+    load_state<KB, DV>(S, ln, LOCAL || !st.last ? nullptr : st.last + ((size_t)bh * a.segments + seg) * D * DV + c0);
     if constexpr (!LOCAL)
         for (int t = max(t0, t1); t < end; ++t)
-            store_rows<DV>(dV + (row + t * kTile) * DV + c0 + ln.r, ln, min(a.N - t * kTile, kTile), f32x16{});
+            store_rows<DV>(dV + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
     Fetch<T, kTile, D, L::NT> fk, fq;
     Fetch<T, kTile, DV, L::NT> fo;
     Copy<Pr::BYTES, L::NT> fp;
@@ -847,7 +868,7 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
         __syncthreads();
         if (t > t0) fetch(t - 1);
         if constexpr (!LOCAL)
-            if (t % GT == GT - 1 || t == t1 - 1) save_state<KB>(S, ln, st.grads + ((size_t)bh * a.grad_tiles + t / GT) * D * DV + c0, DV);
+            if (t % GT == GT - 1 || t == t1 - 1) save_state<KB, DV>(S, ln, st.grads + ((size_t)bh * a.grad_tiles + t / GT) * D * DV + c0);
         f32x16 du = {};   // a row per token
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -878,7 +899,7 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
         }
         const f32x16 dv = beta * du;
         if constexpr (!LOCAL) {
-            const size_t to = (row + token0) * DV + c0 + ln.r;
+            const size_t to = (row + token0) * DV + c0;
             store_rows<DV>(st.dr + to, ln, there, du);
             store_rows<DV>(dV + to, ln, there, dv);
         }
@@ -890,8 +911,8 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
             for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, 32 * kb, m), f, S[kb]);
         }
     }
-    if (LOCAL) save_state<KB>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0, DV);
-    else if (seg == 0) save_state<KB>(S, ln, st.first + (size_t)bh * D * DV + c0, DV);
+    if (LOCAL) save_state<KB, DV>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0);
+    else if (seg == 0) save_state<KB, DV>(S, ln, st.first + (size_t)bh * D * DV + c0);
 }
 
 // ---------------------------------------------------------------------------
@@ -954,7 +975,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
     Gates<C> &g = *(Gates<C> *)(lds + L::G);
     typename L::Sums &red = *(typename L::Sums *)(lds + L::DO);
     const Lane ln(threadIdx.x);
-    const int wave = threadIdx.x >> 6, tile = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * C;
+    const int wave = wave_id(), tile = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * C;
     const int valid = a.valid(b, token0, C), there = min(a.N - token0, C);
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N + token0;
     if (valid == 0) {
