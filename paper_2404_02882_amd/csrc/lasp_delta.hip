@@ -346,6 +346,33 @@ DEVI double sum_up(double x, int lane) {
     return x;
 }
 
+// Values of a tile's rows in the order of an accumulator tile's rows, from LDS.
+DEVI f32x16 by_row(const float *w, const Lane &ln) {
+    f32x16 x;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *(const f32x4 *)(w + 8 * g + 4 * ln.h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
+    }
+    return x;
+}
+// exp(G_i - G_j) for this lane's token and an accumulator's rows (of the one as i, or with NEGATIVE as j), whatever their order. Computed for all: a choice in front
+// of it would be compiled as sixteen branches, each with its own wait.
+template <bool NEGATIVE>
+DEVI f32x16 weights_by_row(const double *sums, double own, const Lane &ln) {
+    typedef __attribute__((ext_vector_type(2))) double f64x2;
+    f64x2 s[8];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s[2 * g + i] = *(const f64x2 *)(sums + 8 * g + 4 * ln.h + 2 * i);
+    f32x16 x;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = power(NEGATIVE ? s[e / 2][e & 1] - own : own - s[e / 2][e & 1]);
+    return x;
+}
+
 struct DeltaCall {
     int B, H, Hk, N, Dv, tiles, segments, seg_tiles, grad_tiles;
     const float *log_g, *beta;
@@ -394,7 +421,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
     using Pr = Prepared<T>;
     constexpr int LDM = kTile + 4;
     __shared__ __attribute__((aligned(16))) float lds_m[kWaves][kTile * LDM], lds_n[kWaves][kTile * LDM], lds_beta[kWaves][kTile];
-    __shared__ double lds_sum[kWaves][kTile];
+    __shared__ __attribute__((aligned(16))) double lds_sum[kWaves][kTile];
     const Lane ln(threadIdx.x);
     const int wave = wave_id(), tile = blockIdx.x * kWaves + wave, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, token0 = tile * kTile;
     float *M = lds_m[wave], *N = lds_n[wave], *beta = lds_beta[wave];
@@ -424,12 +451,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
         p = mm<P::MADE>(fk[k], fq[k], p);
     }
     wave_sync();
+    const f32x16 below = weights_by_row<true>(sum, x, ln), above = weights_by_row<false>(sum, x, ln);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const int o = ln.acc_row(e);
-        const double d = x - sum[o];
-        M[o * LDM + ln.r] = o > ln.r ? m[e] * power(-d) : 0.0f;
-        p[e] = o <= ln.r ? p[e] * power(d) : 0.0f;
+        const float v = m[e] * below[e], y = p[e] * above[e];
+        M[o * LDM + ln.r] = o > ln.r ? v : 0.0f;
+        p[e] = o <= ln.r ? y : 0.0f;
     }
     const typename Pr::Square pt{(bf16_t *)(to + Pr::P)}, nt{(bf16_t *)(to + Pr::N)};
     pt.st_acc(ln, p);
@@ -471,17 +499,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
 template <typename T, int D, int DV>
 constexpr int waves_of() { return D == 128 && (sizeof(T) == 4 || DV == 64) ? 1 : 2; }
 
-// Values of a tile's rows in the order of an accumulator tile's rows, from LDS.
-DEVI f32x16 by_row(const float *w, const Lane &ln) {
-    f32x16 x;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const f32x4 v = *(const f32x4 *)(w + 8 * g + 4 * ln.h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
-    }
-    return x;
-}
 // Values of the lane's column in rows of LD elements, in the order of an accumulator tile's rows; `there`: rows that exist. A scalar base every
 // eight rows, so that a row is at most an instruction's own offset away from it.
 template <int LD, typename T>
@@ -928,7 +945,8 @@ struct Gates {
 template <typename T, int D>
 struct Grad {
     using P = Parts<T>;
-    static constexpr int NB = P::GRAD_TILES, C = NB * kTile, COLS = NB == 2 ? 32 : 64, SLICES = D / 32, WAVES = SLICES * NB, NT = 64 * WAVES;
+    static constexpr int NB = P::GRAD_TILES, C = NB * kTile, COLS = NB == 2 ? 32 : 64, SLICES = D / 32;
+    static constexpr int PER = SLICES * NB > 4 ? NB : 1, WAVES = SLICES * NB / PER, NT = 64 * WAVES;   // PER: token blocks of a wave
     typedef Tile<P::DATA, C, D> Data;
     typedef Lower<P::ROUNDED, C> Square;
     typedef Tile<P::MADE, C, COLS> Rows;
@@ -944,17 +962,19 @@ struct Grad {
     // waves a SIMD: as many workgroups a CU as LDS has room for
     static constexpr int PER_SIMD = NB == 2 ? (163840 / LDS * WAVES) / 4 : 1;
 };
-// Sums over the 32 lanes of a half wave of 16 values: lane r gets that of value r / 2 (two lanes each). By halves: 16 exchanges.
+// Sums over the 32 lanes of a half wave of 16 values: lane r gets that of value r / 2 (two lanes each). By halves: 16 exchanges. (By masks: a
+// choice between elements of a vector would be compiled as an index into it.)
+DEVI float choose(unsigned mask, float a, float b) { return __uint_as_float((__float_as_uint(a) & mask) | (__float_as_uint(b) & ~mask)); }
 DEVI float sum_lanes(const f32x16 &z, const Lane &ln) {
-    float v[8];
-    const bool b4 = ln.r & 16, b3 = ln.r & 8, b2 = ln.r & 4, b1 = ln.r & 2;
+    float v[16];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (b4 ? z[8 + i] : z[i]) + __shfl_xor(b4 ? z[i] : z[8 + i], 16);
+    for (int i = 0; i < 16; ++i) v[i] = z[i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (b3 ? v[4 + i] : v[i]) + __shfl_xor(b3 ? v[i] : v[4 + i], 8);
+    for (int n = 8; n > 0; n /= 2) {   // lanes 2 n apart keep n values each
+        const unsigned up = ln.r & 2 * n ? ~0u : 0u;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = (b2 ? v[2 + i] : v[i]) + __shfl_xor(b2 ? v[i] : v[2 + i], 4);
-    v[0] = (b1 ? v[1] : v[0]) + __shfl_xor(b1 ? v[0] : v[1], 2);
+        for (int i = 0; i < n; ++i) v[i] = choose(up, v[n + i], v[i]) + __shfl_xor(choose(up, v[i], v[n + i]), 2 * n);
+    }
     return v[0] + __shfl_xor(v[0], 1);
 }
 template <typename T, int D, typename TO>
@@ -966,7 +986,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
                                                                                    float *__restrict__ dlog_g, DeltaCall a) {
     using L = Grad<T, D>;
     using P = typename L::P;
-    constexpr int C = L::C, NB = L::NB, COLS = L::COLS, MADE = P::MADE, NT = L::NT, MINE = L::MINE;
+    constexpr int C = L::C, NB = L::NB, COLS = L::COLS, MADE = P::MADE, NT = L::NT, MINE = L::MINE, PER = L::PER;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const typename L::Data kt{(bf16_t *)(lds + L::K)}, qt{(bf16_t *)(lds + L::Q)};
     const typename L::Rows wt{(bf16_t *)(lds + L::W)}, rt{(bf16_t *)(lds + L::DR)};
@@ -989,76 +1009,90 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         }
         return;
     }
-    const int slice = wave % L::SLICES, d0 = 32 * slice, tk = wave / L::SLICES;   // a wave's 32 key features and 32 tokens
+    const int slice = wave % L::SLICES, d0 = 32 * slice, tk0 = wave / L::SLICES * PER;   // a wave's 32 key features and first block of tokens
     // a wave's blocks of Ep (even) and Em (odd)
     auto job = [&](int n) { return wave + n * L::WAVES; };
     auto token_block = [](int j) { return j >= 2 ? 1 : 0; };
     auto key_block = [](int j) { return j >= 4 ? 1 : 0; };
+    // What is read once is on its way before it is needed: the next columns' rows while these are used, a state's next piece as soon as the one
+    // before has been split.
+    Fetch<float, C, COLS, NT> fw, fr;
+    Fetch<T, C, COLS, NT> fo;
+    f32x4 s4[COLS / 16][2], d4[COLS / 16][2];
+    auto fetch_rows = [&](int c0) {
+        fw.load(w + row * a.Dv + c0, a.Dv, valid);
+        fr.load(dR + row * a.Dv + c0, a.Dv, valid);
+        fo.load(dO + row * a.Dv + c0, a.Dv, valid);
+    };
+    const size_t state = (((size_t)bh * a.grad_tiles + tile) * D + d0) * a.Dv;
+    const unsigned piece = (ln.r * a.Dv + 8 * ln.h) * 4;
+    auto fetch_states = [&](int c0, int k) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s4[k][i] = gload<f32x4>(states + state + c0, piece + 64 * k + 16 * i);
+            d4[k][i] = gload<f32x4>(grads + state + c0, piece + 64 * k + 16 * i);
+        }
+    };
     {
         Fetch<T, C, D, NT> fk, fq;
         fk.load(K + (key_row + token0) * D, D, valid);
         fq.load(Q + (key_row + token0) * D, D, valid);
+        const bool in = wave == 0 && ln.id < valid;
+        const float lg = a.log_g && in ? a.log_g[row + ln.id] : 0.0f, bt = in ? a.beta[row + ln.id] : 0.0f;
+        fetch_rows(0);
+#pragma unroll
+        for (int k = 0; k < COLS / 16; ++k) fetch_states(0, k);
         if (wave == 0) {
-            const bool in = ln.id < valid;
-            const double x = sum_up<C>(a.log_g && in ? to_base2(a.log_g[row + ln.id]) : 0.0, ln.id), all = __shfl(x, C - 1, C);
+            const double x = sum_up<C>(to_base2(lg), ln.id), all = __shfl(x, C - 1, C);
             if (ln.id < C) {
                 g.sum[ln.id] = x;
                 g.start[ln.id] = power(x);
                 g.rest[ln.id] = power(all - x);
-                g.beta[ln.id] = in ? a.beta[row + ln.id] : 0.0f;
+                g.beta[ln.id] = bt;
             }
             if (ln.id == 0) g.whole = power(all);
         }
         fk.store(kt);
         fq.store(qt);
     }
-    f32x16 pr[MINE] = {};                     // w dO^T or w dR^T, a row per key token
-    f32x16 aq = {}, a1 = {}, a2 = {};         // S dO^T, S dR^T, dS w^T, a row per key feature
-    float both = 0.0f;                        // <dS, S>
+    f32x16 pr[MINE] = {};                              // w dO^T or w dR^T, a row per key token
+    f32x16 aq[PER] = {}, a1[PER] = {}, a2[PER] = {};   // S dO^T, S dR^T, dS w^T, a row per key feature
+    float both = 0.0f;                                 // <dS, S>
     for (int c0 = 0; c0 < a.Dv; c0 += COLS) {
-        Fetch<float, C, COLS, NT> fw, fr;   // everything is on its way before the first of it is waited for
-        Fetch<T, C, COLS, NT> fo;
-        f32x4 s4[COLS / 16][2], d4[COLS / 16][2];
-        fw.load(w + row * a.Dv + c0, a.Dv, valid);
-        fr.load(dR + row * a.Dv + c0, a.Dv, valid);
-        fo.load(dO + row * a.Dv + c0, a.Dv, valid);
-        const size_t state = (((size_t)bh * a.grad_tiles + tile) * D + d0 + ln.r) * a.Dv + c0 + 8 * ln.h;
-#pragma unroll
-        for (int k = 0; k < COLS / 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                s4[k][i] = *(const f32x4 *)(states + state + 16 * k + 4 * i);
-                d4[k][i] = *(const f32x4 *)(grads + state + 16 * k + 4 * i);
-            }
-        __builtin_amdgcn_sched_barrier(0);
+        const bool more = c0 + COLS < a.Dv;
         if (c0 > 0) __syncthreads();   // the tiles have been read
         fo.store(dot);
         fw.store(wt);
         fr.store(rt);
         __syncthreads();
+        if (more) fetch_rows(c0 + COLS);
 #pragma unroll
         for (int k = 0; k < COLS / 16; ++k) {
             const auto fs = split<MADE>(__builtin_shufflevector(s4[k][0], s4[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
-            aq = mm<MADE>(fs, dot.kc(ln, 32 * tk, 16 * k), aq);
-            a1 = mm<MADE>(fs, rt.kc(ln, 32 * tk, 16 * k), a1);
-            if (tk == 0)
+            const auto fd = split<MADE>(__builtin_shufflevector(d4[k][0], d4[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
+            if (tk0 == 0)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) both = __builtin_fmaf(s4[k][i][e], d4[k][i][e], both);
-            const auto fd = split<MADE>(__builtin_shufflevector(d4[k][0], d4[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
-            a2 = mm<MADE>(fd, wt.kc(ln, 32 * tk, 16 * k), a2);
+            if (more) fetch_states(c0 + COLS, k);
+#pragma unroll
+            for (int n = 0; n < PER; ++n) {
+                aq[n] = mm<MADE>(fs, dot.kc(ln, 32 * (tk0 + n), 16 * k), aq[n]);
+                a1[n] = mm<MADE>(fs, rt.kc(ln, 32 * (tk0 + n), 16 * k), a1[n]);
+                a2[n] = mm<MADE>(fd, wt.kc(ln, 32 * (tk0 + n), 16 * k), a2[n]);
+            }
         }
 #pragma unroll
         for (int n = 0; n < MINE; ++n)
             if (job(n) < L::JOBS) {
                 const int j = job(n), tb = token_block(j), jb = key_block(j);
+                if (j & 1)
 #pragma unroll
-                for (int k0 = 0; k0 < COLS; k0 += 16) {
-                    const auto u = wt.kc(ln, 32 * jb, k0);
-                    if (j & 1) pr[n] = mm<MADE>(u, rt.kc(ln, 32 * tb, k0), pr[n]);
-                    else pr[n] = mm<MADE>(u, dot.kc(ln, 32 * tb, k0), pr[n]);
-                }
+                    for (int k0 = 0; k0 < COLS; k0 += 16) pr[n] = mm<MADE>(wt.kc(ln, 32 * jb, k0), rt.kc(ln, 32 * tb, k0), pr[n]);
+                else
+#pragma unroll
+                    for (int k0 = 0; k0 < COLS; k0 += 16) pr[n] = mm<MADE>(wt.kc(ln, 32 * jb, k0), dot.kc(ln, 32 * tb, k0), pr[n]);
             }
     }
     __syncthreads();
@@ -1069,25 +1103,26 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         if (job(n) < L::JOBS) {
             const int jo = job(n), tb = token_block(jo), jb = key_block(jo), i = 32 * tb + ln.r;
             const bool is_em = jo & 1;
-            const double gi = g.sum[i];
             f32x16 z = {};   // k_j . q_i or k_j . k_i
-            if (dlog_g)
+            if (dlog_g) {
+                const typename L::Data other{is_em ? kt.p : qt.p};
 #pragma unroll
-                for (int k0 = 0; k0 < D; k0 += 16) {
-                    const auto x = kt.kc(ln, 32 * jb, k0);
-                    z = is_em ? mm<MADE>(x, kt.kc(ln, 32 * tb, k0), z) : mm<MADE>(x, qt.kc(ln, 32 * tb, k0), z);
-                }
-            float along = 0.0f;
-            const float bi = is_em ? g.beta[i] : 1.0f;
+                for (int k0 = 0; k0 < D; k0 += 16) z = mm<MADE>(kt.kc(ln, 32 * jb, k0), other.kc(ln, 32 * tb, k0), z);
+            }
+            float along = 0.0f, diagonal = 0.0f;
+            const float bi = is_em ? -g.beta[i] : 1.0f;
+            const f32x16 x = weights_by_row<false>(g.sum + 32 * jb, g.sum[i], ln) * by_row(g.beta + 32 * jb, ln) * bi;
+            const int last = 32 * (tb - jb) + ln.r - is_em;   // rows up to here are keys that the token sees
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int j = 32 * jb + ln.acc_row(e);
-                if (is_em && j == i) red.beta[i] = pr[n][e];   // dbeta_i = w_i . dR_i
-                const float x = j <= i ? g.beta[j] * bi * power(gi - g.sum[j]) : 0.0f;
-                pr[n][e] *= is_em ? (j < i ? -x : 0.0f) : x;
-                z[e] = j < i ? pr[n][e] * z[e] : 0.0f;
+                const int o = ln.acc_row(e);
+                diagonal = o == ln.r ? pr[n][e] : diagonal;
+                const float v = pr[n][e] * x[e];
+                pr[n][e] = o <= last ? v : 0.0f;
+                z[e] = o < 32 * (tb - jb) + ln.r ? v * z[e] : 0.0f;
                 along += z[e];
             }
+            if (is_em && tb == jb && ln.h == (ln.r >> 2 & 1)) red.beta[i] = diagonal;   // dbeta_i = w_i . dR_i
             if (dlog_g) {
                 along += __shfl_xor(along, 32);
                 const float down = sum_lanes(z, ln);
@@ -1098,13 +1133,12 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
             to.st_acc(ln, pr[n]);
         }
     __syncthreads();
-    const int m = 32 * tk + ln.r;
-    {
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+        const int tk = tk0 + n, m = 32 * tk + ln.r;
         const float start = g.start[m], rest = g.rest[m];
         const size_t to = (row + m) * D + d0;   // (shared heads: a partial sum for every state, in float)
-        aq *= start;
-        a1 *= start * g.beta[m];
-        a2 *= rest * g.beta[m];
+        f32x16 x = aq[n] * start, z = a1[n] * (start * g.beta[m]), y = a2[n] * (rest * g.beta[m]);
         if (dlog_g) {
             float up = 0.0f, on = 0.0f;
 #pragma unroll
@@ -1112,8 +1146,8 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
                 const f32x4 q4 = qt.get4(m, d0 + 8 * f + 4 * ln.h), k4 = kt.get4(m, d0 + 8 * f + 4 * ln.h);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    up = __builtin_fmaf(q4[e], aq[4 * f + e], __builtin_fmaf(-k4[e], a1[4 * f + e], up));
-                    on = __builtin_fmaf(k4[e], a2[4 * f + e], on);
+                    up = __builtin_fmaf(q4[e], x[4 * f + e], __builtin_fmaf(-k4[e], z[4 * f + e], up));
+                    on = __builtin_fmaf(k4[e], y[4 * f + e], on);
                 }
             }
             up += __shfl_xor(up, 32);
@@ -1125,23 +1159,23 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         }
         for (int jb = 0; jb <= tk; ++jb)
 #pragma unroll
-            for (int k0 = 0; k0 < 32; k0 += 16) aq = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), ep.at(tk, jb).kc(ln, k0), aq);
-        if (m < there) store_acc(dQ + to, ln, aq);
-        a2 -= a1;
+            for (int k0 = 0; k0 < 32; k0 += 16) x = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), ep.at(tk, jb).kc(ln, k0), x);
+        if (m < there) store_acc(dQ + to, ln, x);
+        y -= z;
         for (int it = tk; it < NB; ++it)
 #pragma unroll
             for (int k0 = 0; k0 < 32; k0 += 16) {
-                a2 = mm<P::ROUNDED>(qt.ks(ln, 32 * it + k0, d0), ep.at(it, tk).ks(ln, k0), a2);
-                a2 = mm<P::ROUNDED>(kt.ks(ln, 32 * it + k0, d0), em.at(it, tk).ks(ln, k0), a2);
+                y = mm<P::ROUNDED>(qt.ks(ln, 32 * it + k0, d0), ep.at(it, tk).ks(ln, k0), y);
+                y = mm<P::ROUNDED>(kt.ks(ln, 32 * it + k0, d0), em.at(it, tk).ks(ln, k0), y);
             }
         for (int jb = 0; jb <= tk; ++jb)
 #pragma unroll
-            for (int k0 = 0; k0 < 32; k0 += 16) a2 = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), em.at(tk, jb).kc(ln, k0), a2);
-        if (m < there) store_acc(dK + to, ln, a2);
+            for (int k0 = 0; k0 < 32; k0 += 16) y = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), em.at(tk, jb).kc(ln, k0), y);
+        if (m < there) store_acc(dK + to, ln, y);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) both += __shfl_xor(both, d);
-    if (ln.id == 0 && tk == 0) red.both[slice] = both;
+    if (ln.id == 0 && tk0 == 0) red.both[slice] = both;
     __syncthreads();
     if (wave != 0) return;
     if (ln.id < there) dbeta[row + ln.id] = red.beta[ln.id];
