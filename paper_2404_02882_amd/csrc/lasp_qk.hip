@@ -20,26 +20,36 @@ constexpr int kThreads = 256, kTable = 512;   // entries of the table: tokens ti
 struct QkCall {
     int B, N, H, Hk, D, rot, half, norm, tokens, group;   // tokens of the call; of a group (one table)
     long long ldq, ldk;                                    // elements between rows of the projections
-    float eps, amplitude;
+    float eps, amplitude, share;   // share: of a row's squares (1 / D or 1)
     const double *freq;
     const int *pos;
 };
 
-struct Row {   // where a row lies
-    bool key;
-    size_t x, y;
-    int table;
+// The rows (heads of tokens) that a thread comes to in a group, one after the other; counted up, as a division takes as long as the row itself.
+struct Walk {
+    int slot, head, b, s;    // token of the group, its head, sequence and place there
+    int left;                // rows left up to the last of the group, less than 1: none
+    DEVI Walk(const QkCall &c, int token0, int count, int heads, int first) {
+        b = token0 / c.N;
+        s = token0 - b * c.N;
+        slot = 0;
+        head = first;
+        left = count * heads - first;
+        settle(c, heads);
+    }
+    DEVI void settle(const QkCall &c, int heads) {
+        while (head >= heads) {
+            head -= heads;
+            ++slot;
+            if (++s == c.N) s = 0, ++b;
+        }
+    }
+    DEVI void next(const QkCall &c, int heads, int rows) {
+        head += rows;
+        left -= rows;
+        settle(c, heads);
+    }
 };
-DEVI Row place(const QkCall &c, int token, int slot, int head) {
-    const int b = token / c.N, s = token - b * c.N;
-    Row r;
-    r.key = head >= c.H;
-    const int h = r.key ? head - c.H : head, heads = r.key ? c.Hk : c.H;
-    r.x = (size_t)token * (r.key ? c.ldk : c.ldq) + h * c.D;
-    r.y = (((size_t)b * heads + h) * c.N + s) * c.D;
-    r.table = slot * (c.rot / 2);
-    return r;
-}
 DEVI void make_table(const QkCall &c, float2 *table, int token0, int count) {
     const int pairs = c.rot / 2;
     for (int e = threadIdx.x; e < count * pairs; e += kThreads) {
@@ -108,15 +118,32 @@ struct Turn {
         }
     }
 };
-DEVI float scale_of(const QkCall &c, float squares) {
-    if (c.norm == 0) return 1.0f;
-    return 1.0f / __builtin_sqrtf((c.norm == 1 ? squares / (float)c.D : squares) + c.eps);
+// x^(-1/2): the instruction is good to one step, but takes numbers below the smallest normal one as 0.
+DEVI float rsqrt_of(float x) {
+    const bool tiny = x < 0x1p-96f;
+    const float y = __builtin_amdgcn_rsqf(tiny ? x * 0x1p64f : x);
+    return tiny ? y * 0x1p32f : y;
 }
+DEVI float scale_of(const QkCall &c, float squares) { return c.norm == 0 ? 1.0f : rsqrt_of(__builtin_fmaf(squares, c.share, c.eps)); }
 template <int W>
 DEVI void weights_of(const float *w, int at, bool has, float (&f)[W]) {
 #pragma unroll
     for (int i = 0; i < W; ++i) f[i] = 1.0f;
     if (w && has) load_floats<W>(w + at, f);
+}
+
+// The weights of a thread's piece and of its partner's.
+template <int W>
+struct Weighted {
+    float own[W], other[W];
+};
+template <typename T, int LANES>
+DEVI Weighted<Piece<T>::W> weighted(const float *w, const Turn<T, LANES> &my, bool has) {
+    constexpr int W = Piece<T>::W;
+    Weighted<W> f;
+    weights_of<W>(w, my.at, has, f.own);
+    weights_of<W>(w, (my.other & (LANES - 1)) * W, has && my.first >= 0, f.other);
+    return f;
 }
 
 template <typename T, int LANES, bool STREAM>
@@ -125,17 +152,11 @@ __global__ __launch_bounds__(kThreads) void k_qk_fwd(const T *__restrict__ xq, c
     using P = Piece<T>;
     constexpr int W = P::W, ROWS = kThreads / LANES;
     __shared__ __attribute__((aligned(16))) float2 table[kTable];
-    const int lane = threadIdx.x % LANES, heads = c.H + c.Hk;
+    const int lane = threadIdx.x % LANES;
     const bool has = lane * W < c.D;
     const Turn<T, LANES> my(c, lane);
     const int at = has ? my.at : 0;
-    // the weights of this piece and of its partner's, for queries and keys
-    float w[2][W], wo[2][W];
-    weights_of<W>(wq, at, has, w[0]);
-    weights_of<W>(wk, at, has, w[1]);
-    const int ato = (my.other & (LANES - 1)) * W;
-    weights_of<W>(wq, ato, has && my.first >= 0, wo[0]);
-    weights_of<W>(wk, ato, has && my.first >= 0, wo[1]);
+    const auto ws_q = weighted<T, LANES>(wq, my, has), ws_k = weighted<T, LANES>(wk, my, has);
     for (int token0 = blockIdx.x * c.group; token0 < c.tokens; token0 += gridDim.x * c.group) {
         const int count = min(c.group, c.tokens - token0);
         if (c.rot) {
@@ -143,26 +164,33 @@ __global__ __launch_bounds__(kThreads) void k_qk_fwd(const T *__restrict__ xq, c
             make_table(c, table, token0, count);
             __syncthreads();
         }
-        for (int r0 = 0; r0 < count * heads; r0 += ROWS) {   // (all threads take part in every turn: the sums want whole waves)
-            const int r = r0 + threadIdx.x / LANES;
-            const bool there = r < count * heads;
-            const int slot = there ? r / heads : 0, head = there ? r - slot * heads : 0;
-            const Row row = place(c, token0 + slot, slot, head);
-            const u32x4 v = gload<u32x4, STREAM>((row.key ? xk : xq) + row.x + at, 0);
-            float f[W], g[W], s = 0.0f;
-            P::unpack(v, f);
+        auto part = [&](const T *x, T *y, const Weighted<W> &w, int heads, long long ld) {
+            Walk r(c, token0, count, heads, threadIdx.x / LANES);
+            const T *rows = x + (size_t)token0 * ld + at;
+            auto load = [&]() { return gload<u32x4, STREAM>(r.left > 0 ? rows + r.slot * ld + r.head * c.D : rows, 0); };
+            u32x4 next = load();
+            for (int turn = count * heads; turn > 0; turn -= ROWS) {   // (all threads take part in every turn: the sums want whole waves)
+                const u32x4 v = next;
+                const Walk now = r;
+                r.next(c, heads, ROWS);
+                if (turn > ROWS) next = load();
+                float f[W], g[W], s = 0.0f;
+                P::unpack(v, f);
 #pragma unroll
-            for (int i = 0; i < W; ++i) s = __builtin_fmaf(f[i], f[i], s);
-            const float k = scale_of(c, row_sum<LANES>(has ? s : 0.0f));
-            P::unpack(my.partner(c, v), g);
+                for (int i = 0; i < W; ++i) s = __builtin_fmaf(f[i], f[i], s);
+                const float k = scale_of(c, c.norm == 0 ? 0.0f : row_sum<LANES>(has ? s : 0.0f));
+                P::unpack(my.partner(c, v), g);
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                f[i] *= k * (row.key ? w[1][i] : w[0][i]);
-                g[i] *= k * (row.key ? wo[1][i] : wo[0][i]);
+                for (int i = 0; i < W; ++i) {
+                    f[i] *= k * w.own[i];
+                    g[i] *= k * w.other[i];
+                }
+                my.template turn<false>(c, table + (now.left > 0 ? now.slot : 0) * (c.rot / 2), f, g);
+                if (now.left > 0 && has) put<STREAM>(y + (((size_t)now.b * heads + now.head) * c.N + now.s) * c.D + at, P::pack(f));
             }
-            my.template turn<false>(c, table + row.table, f, g);
-            if (there && has) put<STREAM>((row.key ? yk : yq) + row.y + at, P::pack(f));
-        }
+        };
+        part(xq, yq, ws_q, c.H, c.ldq);
+        if (c.Hk) part(xk, yk, ws_k, c.Hk, c.ldk);
     }
 }
 
@@ -173,8 +201,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_bwd(const T *__restrict__ xq, c
     using P = Piece<T>;
     constexpr int W = P::W, ROWS = kThreads / LANES;
     __shared__ __attribute__((aligned(16))) float2 table[kTable];
-    __shared__ __attribute__((aligned(16))) float part[kThreads / 64][LANES * W];
-    const int lane = threadIdx.x % LANES, heads = c.H + c.Hk;
+    __shared__ __attribute__((aligned(16))) float part_sums[kThreads / 64][LANES * W];
+    const int lane = threadIdx.x % LANES;
     const bool has = lane * W < c.D, sums = pq || pk, reads = c.norm != 0 || sums;
     const Turn<T, LANES> my(c, lane);
     const int at = has ? my.at : 0;
@@ -188,42 +216,50 @@ __global__ __launch_bounds__(kThreads) void k_qk_bwd(const T *__restrict__ xq, c
             make_table(c, table, token0, count);
             __syncthreads();
         }
-        for (int r0 = 0; r0 < count * heads; r0 += ROWS) {
-            const int r = r0 + threadIdx.x / LANES;
-            const bool there = r < count * heads;
-            const int slot = there ? r / heads : 0, head = there ? r - slot * heads : 0;
-            const Row row = place(c, token0 + slot, slot, head);
-            const u32x4 vy = gload<u32x4, STREAM>((row.key ? dyk : dyq) + row.y + at, 0);
-            u32x4 vx{0, 0, 0, 0};
-            if (reads) vx = gload<u32x4, STREAM>((row.key ? xk : xq) + row.x + at, 0);
-            float f[W], d[W], o[W], s = 0.0f, t = 0.0f;
-            P::unpack(vy, d);
-            P::unpack(my.partner(c, vy), o);
-            P::unpack(vx, f);
-            my.template turn<true>(c, table + row.table, d, o);
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                o[i] = d[i] * (row.key ? w[1][i] : w[0][i]);
-                s = __builtin_fmaf(f[i], f[i], s);
-                t = __builtin_fmaf(o[i], f[i], t);
-            }
-            float k = 1.0f, mean = 0.0f;
-            if (c.norm != 0) {
-                k = scale_of(c, row_sum<LANES>(has ? s : 0.0f));
-                mean = row_sum<LANES>(has ? t : 0.0f) * k * k;
-                if (c.norm == 1) mean /= (float)c.D;
-            }
-            if (there && has) {
+        auto part = [&](const T *x, const T *dy, T *dx, const float (&w)[W], float (&acc)[W], int heads, long long ld) {
+            Walk r(c, token0, count, heads, threadIdx.x / LANES);
+            const T *rows = x + (size_t)token0 * ld + at;
+            T *to = dx + (size_t)token0 * ld + at;
+            u32x4 nx{0, 0, 0, 0}, ny;
+            auto load = [&]() {
+                const bool there = r.left > 0;
+                ny = gload<u32x4, STREAM>(dy + (there ? (((size_t)r.b * heads + r.head) * c.N + r.s) * c.D : 0) + at, 0);
+                if (reads) nx = gload<u32x4, STREAM>(there ? rows + r.slot * ld + r.head * c.D : rows, 0);
+            };
+            load();
+            for (int turn = count * heads; turn > 0; turn -= ROWS) {
+                const u32x4 vx = nx, vy = ny;
+                const Walk now = r;
+                r.next(c, heads, ROWS);
+                if (turn > ROWS) load();
+                float f[W], d[W], o[W], s = 0.0f, t = 0.0f;
+                P::unpack(vy, d);
+                P::unpack(my.partner(c, vy), o);
+                P::unpack(vx, f);
+                my.template turn<true>(c, table + (now.left > 0 ? now.slot : 0) * (c.rot / 2), d, o);
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
-                    const float n = d[i] * (f[i] * k);   // (one of the two sums: a select instead of a branch)
-                    acc[0][i] += row.key ? 0.0f : n;
-                    acc[1][i] += row.key ? n : 0.0f;
-                    o[i] = k * (o[i] - f[i] * mean);
+                    o[i] = d[i] * w[i];
+                    s = __builtin_fmaf(f[i], f[i], s);
+                    t = __builtin_fmaf(o[i], f[i], t);
                 }
-                put<STREAM>((row.key ? dxk : dxq) + row.x + at, P::pack(o));
+                float k = 1.0f, mean = 0.0f;
+                if (c.norm != 0) {
+                    k = scale_of(c, row_sum<LANES>(has ? s : 0.0f));
+                    mean = row_sum<LANES>(has ? t : 0.0f) * c.share * k * k;
+                }
+                if (now.left > 0 && has) {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        acc[i] = __builtin_fmaf(d[i] * k, f[i], acc[i]);
+                        o[i] = k * (o[i] - f[i] * mean);
+                    }
+                    put<STREAM>(to + now.slot * ld + now.head * c.D, P::pack(o));
+                }
             }
-        }
+        };
+        part(xq, dyq, dxq, w[0], acc[0], c.H, c.ldq);
+        if (c.Hk) part(xk, dyk, dxk, w[1], acc[1], c.Hk, c.ldk);
     }
     // a partial row per workgroup: the rows of a wave by shuffles, the waves in LDS, in a fixed order
 #pragma unroll
@@ -235,9 +271,9 @@ __global__ __launch_bounds__(kThreads) void k_qk_bwd(const T *__restrict__ xq, c
 #pragma unroll
             for (int d = LANES; d < 64; d *= 2) acc[n][i] += __shfl_xor(acc[n][i], d);
         __syncthreads();
-        if ((threadIdx.x & 63) < LANES) store_floats<W>(&part[threadIdx.x >> 6][lane * W], acc[n]);
+        if ((threadIdx.x & 63) < LANES) store_floats<W>(&part_sums[threadIdx.x >> 6][lane * W], acc[n]);
         __syncthreads();
-        for (int e = threadIdx.x; e < c.D; e += kThreads) to[(size_t)blockIdx.x * c.D + e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+        for (int e = threadIdx.x; e < c.D; e += kThreads) to[(size_t)blockIdx.x * c.D + e] = (part_sums[0][e] + part_sums[1][e]) + (part_sums[2][e] + part_sums[3][e]);
     }
 }
 
@@ -254,7 +290,7 @@ int workgroups(const QkPlan &p, int a_cu) {
 }
 constexpr int kForwardACu = 8, kBackwardACu = 4;
 QkCall call_of(const QkPlan &p, const QkArgs &a) {
-    return {p.B, p.N, p.H, p.Hk, p.D, p.rot, p.half, p.norm, p.B * p.N, group_of(p), p.ldq, p.ldk, a.eps, a.amplitude, a.freq, a.pos};
+    return {p.B, p.N, p.H, p.Hk, p.D, p.rot, p.half, p.norm, p.B * p.N, group_of(p), p.ldq, p.ldk, a.eps, a.amplitude, p.norm == 1 ? 1.0f / p.D : 1.0f, a.freq, a.pos};
 }
 // f.template operator()<T, LANES, STREAM>()
 template <typename T, bool STREAM, typename F>
