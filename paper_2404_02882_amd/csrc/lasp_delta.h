@@ -16,6 +16,7 @@ struct DeltaPlan {
     int B, H, N, D, Dv, dtype, key_heads;
     int tiles, grad_tiles;    // tiles of a sequence; those that the gradients are computed in
     int segments, seg_tiles;  // segments a sequence is cut into, tiles of one
+    bool split;               // the walks: a state's key features shared by two waves
 };
 DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_heads);
 

@@ -496,8 +496,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
 }
 
 // Waves a SIMD that a walk is compiled for: two, so that one computes while the other waits, where 256 registers are enough.
-template <typename T, int D, int DV>
-constexpr int waves_of() { return D == 128 && (sizeof(T) == 4 || DV == 64) ? 1 : 2; }
+template <typename T, int D, int DV, int SPLIT>
+constexpr int waves_of() { return SPLIT == 1 && D == 128 && (sizeof(T) == 4 || DV == 64) ? 1 : 2; }
+// Two waves that have half a sum each: a square of accumulators through LDS, a lane's values as they lie.
+constexpr int kSplitCols = 64, kSquareBytes = 4096;
+DEVI void put_tile(float *to, const Lane &ln, const f32x16 &x) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *(f32x4 *)(to + 256 * g + 4 * ln.id) = f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
+}
+DEVI f32x16 get_tile(const float *from, const Lane &ln) {
+    f32x16 x;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *(const f32x4 *)(from + 256 * g + 4 * ln.id);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
+    }
+    return x;
+}
 
 // Values of the lane's column in rows of LD elements, in the order of an accumulator tile's rows; `there`: rows that exist. A scalar base every
 // eight rows, so that a row is at most an instruction's own offset away from it.
@@ -541,18 +557,21 @@ DEVI void save_state(const f32x16 (&S)[KB], const Lane &ln, float *dst) {
 // ---------------------------------------------------------------------------
 // k_delta_walk: a wave carries 32 columns of the state in its accumulators and meets no other wave's: what a product leaves in an
 // accumulator tile (a row per token or key feature, a lane per column) is the next one's operand as it lies there, with the contraction in the
-// order of the accumulator's rows; the waves share the tile's keys, queries, N and scores in LDS. LOCAL: no outputs; the state a segment reaches
+// order of the accumulator's rows; the waves share the tile's keys, queries, N and scores in LDS. SPLIT = 2: two waves have half of the key
+// features of 32 columns each, and add up S^T k and S^T q once a tile. LOCAL: no outputs; the state a segment reaches
 // from zero, and (waves behind those of the values) its matrix T, which is the state reached from the identity without values.
 // ---------------------------------------------------------------------------
-template <typename T, int D, int DV, bool LOCAL>
+template <typename T, int D, int DV, bool LOCAL, int SPLIT>
 struct Walk {
     using P = Parts<T>;
-    static constexpr int KB = D / 32, WAVES = (DV + (LOCAL ? D : 0)) / 32, NT = 64 * WAVES;
+    static constexpr int ALL = DV + (LOCAL ? D : 0), COLS = SPLIT == 1 ? ALL : kSplitCols, GROUPS = ALL / COLS;
+    static constexpr int CW = COLS / 32, WAVES = CW * SPLIT, NT = 64 * WAVES, KB = D / 32 / SPLIT;   // (KB: blocks of key features of a wave)
     typedef Tile<P::DATA, kTile, D> Data;
-    typedef Tile<1, kTile, DV> Value;
+    static constexpr int VALUES = COLS < DV ? COLS : DV;
+    typedef Tile<1, kTile, VALUES> Value;
     static constexpr bool STAGED = sizeof(T) == 2;   // two-byte values go through LDS, which hands a lane four tokens of its column at a time
     static constexpr int PREP = 0, K = Prepared<T>::BYTES, V = K + Data::BYTES, Q = V + (STAGED ? Value::BYTES : 0),
-                         STAGE = LOCAL ? Q : Q + Data::BYTES, LDS = 2 * STAGE;
+                         STAGE = LOCAL ? Q : Q + Data::BYTES, XCH = 2 * STAGE, LDS = XCH + (SPLIT == 1 ? 0 : CW * (LOCAL ? 2 : 3) * kSquareBytes);
 };
 struct WalkStates {
     const float *first;   // states that segments start from ([head][segment], or kv_in where there is one segment); null = zeros
@@ -562,11 +581,11 @@ struct WalkStates {
     float *w;             // w of every token; goes with the cache
     int all_trans;        // T is wanted of the last segment too
 };
-template <typename T, int D, int DV, bool LOCAL>
-__global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())) void k_delta_walk(const T *__restrict__ Q, const T *__restrict__ K,
+template <typename T, int D, int DV, bool LOCAL, int SPLIT>
+__global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D, DV, SPLIT>())) void k_delta_walk(const T *__restrict__ Q, const T *__restrict__ K,
                                                                               const T *__restrict__ V, const char *__restrict__ prepared,
                                                                               T *__restrict__ O, WalkStates st, DeltaCall a) {
-    using L = Walk<T, D, DV, LOCAL>;
+    using L = Walk<T, D, DV, LOCAL, SPLIT>;
     using P = typename L::P;
     using Pr = Prepared<T>;
     constexpr int KB = L::KB, MADE = P::MADE;
@@ -574,8 +593,9 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
     const Lane ln(threadIdx.x);
     const int wave = wave_id(), seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
     if (LOCAL && seg == a.segments - 1 && !st.all_trans) return;
-    const bool trans = LOCAL && wave >= DV / 32;
-    const int c0 = 32 * (trans ? wave - DV / 32 : wave);
+    const int part = SPLIT == 1 ? 0 : wave / L::CW, cw = wave - part * L::CW, v0 = L::GROUPS == 1 ? 0 : blockIdx.y * L::COLS;
+    const bool trans = LOCAL && v0 + 32 * cw >= DV;
+    const int c0 = v0 + 32 * cw - (trans ? DV : 0), d0 = 32 * KB * part;
     const int tokens = a.valid(b, 0, a.N), end = min(a.tiles, (seg + 1) * a.seg_tiles);
     const int t0 = seg * a.seg_tiles, t1 = min(end, (tokens + kTile - 1) / kTile);   // (tiles behind a sequence's end leave the state as it is)
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N;
@@ -584,20 +604,20 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[kb][e] = 32 * kb + ln.acc_row(e) == c0 + ln.r ? 1.0f : 0.0f;
+            for (int e = 0; e < 16; ++e) S[kb][e] = d0 + 32 * kb + ln.acc_row(e) == c0 + ln.r ? 1.0f : 0.0f;
     } else {
-        load_state<KB, DV>(S, ln, LOCAL || !st.first ? nullptr : st.first + ((size_t)bh * a.segments + seg) * D * DV + c0);
+        load_state<KB, DV>(S, ln, LOCAL || !st.first ? nullptr : st.first + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
     }
     Fetch<T, kTile, D, L::NT> fk, fq;
     Copy<Pr::BYTES, L::NT> fp;
-    Fetch<T, kTile, DV, L::NT> fv;   // (STAGED)
+    Fetch<T, kTile, L::VALUES, L::NT> fv;   // (STAGED)
     f32x16 v = {};                   // (else)
     auto fetch = [&](int t) {
         const int token0 = t * kTile, valid = min(tokens - token0, kTile);
         fp.load(prepared + ((size_t)bh * a.tiles + t) * Pr::BYTES);
         fk.load(K + (key_row + token0) * D, D, valid);
         if constexpr (!LOCAL) fq.load(Q + (key_row + token0) * D, D, valid);
-        if constexpr (L::STAGED) fv.load(V + (row + token0) * DV, DV, valid);
+        if constexpr (L::STAGED) fv.load(V + (row + token0) * DV + (v0 < DV ? v0 : 0), DV, valid);
         else if (!trans) v = load_rows<DV>(V + (row + token0) * DV + c0, ln, valid);
     };
     if (t0 < t1) fetch(t0);
@@ -616,7 +636,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
         if (t + 1 < t1) fetch(t + 1);
         if constexpr (!LOCAL)
             if (st.cache && t % P::GRAD_TILES == 0)
-                save_state<KB, DV>(S, ln, st.cache + ((size_t)bh * a.grad_tiles + t / P::GRAD_TILES) * D * DV + c0);
+                save_state<KB, DV>(S, ln, st.cache + (((size_t)bh * a.grad_tiles + t / P::GRAD_TILES) * D + d0) * DV + c0);
         f32x16 o = {};   // r: a row per token;  o: a lane per token, a row per column
         {
             f32x16 x = {};
@@ -625,20 +645,31 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     const auto s = split<MADE>(S[kb], m);
-                    x = mm<MADE>(kt.kp(ln, 0, 32 * kb, m), s, x);
-                    if constexpr (!LOCAL) o = mm<P::ROUNDED>(s, qt.kp(ln, 0, 32 * kb, m), o);
+                    x = mm<MADE>(kt.kp(ln, 0, d0 + 32 * kb, m), s, x);
+                    if constexpr (!LOCAL) o = mm<P::ROUNDED>(s, qt.kp(ln, 0, d0 + 32 * kb, m), o);
                 }
+            if constexpr (SPLIT == 2) {
+                float *mine = (float *)(lds + L::XCH + (part * L::CW + cw) * kSquareBytes), *other = (float *)(lds + L::XCH + ((1 - part) * L::CW + cw) * kSquareBytes),
+                      *out = (float *)(lds + L::XCH + (2 * L::CW + cw) * kSquareBytes);
+                put_tile(mine, ln, x);
+                if constexpr (!LOCAL)
+                    if (part == 0) put_tile(out, ln, o);
+                __syncthreads();
+                x += get_tile(other, ln);
+                if constexpr (!LOCAL)
+                    if (part == 1) o += get_tile(out, ln);
+            }
             if constexpr (L::STAGED)
-                if (!trans) r = vt.rows(ln, c0);
+                if (!trans) r = vt.rows(ln, c0 - v0);
             r -= by_row((const float *)(at + Pr::START), ln) * x;
             x = by_row((const float *)(at + Pr::BETA), ln) * r;
 #pragma unroll
             for (int m = 0; m < 2; ++m) r = mm<MADE>(nt.kp(ln, m), split<MADE>(x, m), r);
         }
         if constexpr (!LOCAL)
-            if (st.cache) store_rows<DV>(st.w + (row + token0) * DV + c0, ln, there, r);
+            if (st.cache && part == 0) store_rows<DV>(st.w + (row + token0) * DV + c0, ln, there, r);
         r *= by_row((const float *)(at + Pr::BETA), ln);
-        if constexpr (!LOCAL) {
+        if (!LOCAL && part == SPLIT - 1) {
             o *= ((const float *)(at + Pr::START))[ln.r];
 #pragma unroll
             for (int m = 0; m < 2; ++m) o = mm<P::ROUNDED>(split<P::ROUNDED>(r, m), pt.kp(ln, m), o);
@@ -652,16 +683,17 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL>::NT), (waves_of<T, D, DV>())
         for (int m = 0; m < 2; ++m) {
             const auto f = split<MADE>(r, m);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, 32 * kb, m), f, S[kb]);
+            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, d0 + 32 * kb, m), f, S[kb]);
         }
     }
     if constexpr (LOCAL) {
-        if (trans) save_state<KB, D>(S, ln, st.trans + ((size_t)bh * a.segments + seg) * D * D + c0);
-        else save_state<KB, DV>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0);
+        if (trans) save_state<KB, D>(S, ln, st.trans + (((size_t)bh * a.segments + seg) * D + d0) * D + c0);
+        else save_state<KB, DV>(S, ln, st.local + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
     } else {
-        for (int t = max(t0, t1); t < end; ++t)
-            store_rows<DV>(O + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
-        if (seg == a.segments - 1) save_state<KB, DV>(S, ln, st.last + (size_t)bh * D * DV + c0);
+        if (part == 0)
+            for (int t = max(t0, t1); t < end; ++t)
+                store_rows<DV>(O + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
+        if (seg == a.segments - 1) save_state<KB, DV>(S, ln, st.last + ((size_t)bh * D + d0) * DV + c0);
     }
 }
 
@@ -824,16 +856,17 @@ __global__ __launch_bounds__(kThreads) void k_delta_step(const T *__restrict__ Q
 }
 
 // ---------------------------------------------------------------------------
-// k_delta_back: the walk in reverse. LOCAL: the gradient that reaches a segment's front from its own tokens.
+// k_delta_back: the walk in reverse (SPLIT as there; the sum is dU's). LOCAL: the gradient that reaches a segment's front from its own tokens.
 // ---------------------------------------------------------------------------
-template <typename T, int D, int DV>
+template <typename T, int D, int DV, int SPLIT>
 struct Back {
     using P = Parts<T>;
-    static constexpr int KB = D / 32, WAVES = DV / 32, NT = 64 * WAVES;
+    static constexpr int COLS = SPLIT == 1 ? DV : kSplitCols, GROUPS = DV / COLS, CW = COLS / 32, WAVES = CW * SPLIT, NT = 64 * WAVES, KB = D / 32 / SPLIT;
     typedef Tile<P::DATA, kTile, D> Data;
-    typedef Tile<P::DATA, kTile, DV> Grad;
+    typedef Tile<P::DATA, kTile, COLS> Grad;
     static constexpr int PREP = 0, K = Prepared<T>::BYTES, Q = K + Data::BYTES, DO = Q + Data::BYTES, STAGE = DO + Grad::BYTES,
-                         STAGES = 2 * STAGE <= 163840 ? 2 : 1, LDS = STAGES * STAGE;
+                         XBYTES = SPLIT == 1 ? 0 : 2 * CW * kSquareBytes,
+                         STAGES = 2 * STAGE + XBYTES <= 163840 ? 2 : 1, XCH = STAGES * STAGE, LDS = XCH + XBYTES;
 };
 struct BackStates {
     const float *last;   // gradients of the states segments end with ([head][segment], or dkv_out where there is one segment); null = zeros
@@ -842,35 +875,36 @@ struct BackStates {
     float *grads;        // the gradient of the state behind every tile that k_delta_grad takes
     float *dr;           // [B][H][N][Dv]
 };
-template <typename T, int D, int DV, bool LOCAL>
-__global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void k_delta_back(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ dO,
+template <typename T, int D, int DV, bool LOCAL, int SPLIT>
+__global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SPLIT>())) void k_delta_back(const T *__restrict__ Q, const T *__restrict__ K, const T *__restrict__ dO,
                                                                        const char *__restrict__ prepared, T *__restrict__ dV, BackStates st,
                                                                        DeltaCall a) {
-    using L = Back<T, D, DV>;
+    using L = Back<T, D, DV, SPLIT>;
     using P = typename L::P;
     using Pr = Prepared<T>;
     constexpr int KB = L::KB, MADE = P::MADE, GT = P::GRAD_TILES;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const Lane ln(threadIdx.x);
-    const int wave = wave_id(), c0 = 32 * wave, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
+    const int wave = wave_id(), part = SPLIT == 1 ? 0 : wave / L::CW, cw = wave - part * L::CW, v0 = L::GROUPS == 1 ? 0 : blockIdx.y * L::COLS, c0 = v0 + 32 * cw,
+              d0 = 32 * KB * part, seg = blockIdx.x % a.segments, bh = blockIdx.x / a.segments, b = bh / a.H, h = bh - b * a.H;
     if (LOCAL && seg == 0) return;
     const int tokens = a.valid(b, 0, a.N), end = min(a.tiles, (seg + 1) * a.seg_tiles);
     const int t0 = seg * a.seg_tiles, t1 = min(end, (tokens + kTile - 1) / kTile);
     const size_t key_row = a.key_row(b, h), row = (size_t)bh * a.N;
     f32x16 S[KB];
-    load_state<KB, DV>(S, ln, LOCAL || !st.last ? nullptr : st.last + ((size_t)bh * a.segments + seg) * D * DV + c0);
-    if constexpr (!LOCAL)
+    load_state<KB, DV>(S, ln, LOCAL || !st.last ? nullptr : st.last + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
+    if (!LOCAL && part == 0)
         for (int t = max(t0, t1); t < end; ++t)
             store_rows<DV>(dV + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
     Fetch<T, kTile, D, L::NT> fk, fq;
-    Fetch<T, kTile, DV, L::NT> fo;
+    Fetch<T, kTile, L::COLS, L::NT> fo;
     Copy<Pr::BYTES, L::NT> fp;
     auto fetch = [&](int t) {
         const int token0 = t * kTile, valid = min(tokens - token0, kTile);
         fp.load(prepared + ((size_t)bh * a.tiles + t) * Pr::BYTES);
         fk.load(K + (key_row + token0) * D, D, valid);
         fq.load(Q + (key_row + token0) * D, D, valid);
-        fo.load(dO + (row + token0) * DV, DV, valid);
+        fo.load(dO + (row + token0) * DV + v0, DV, valid);
     };
     if (t0 < t1) fetch(t1 - 1);
     for (int t = t1 - 1; t >= t0; --t) {
@@ -887,20 +921,20 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
         __syncthreads();
         if (t > t0) fetch(t - 1);
         if constexpr (!LOCAL)
-            if (t % GT == GT - 1 || t == t1 - 1) save_state<KB, DV>(S, ln, st.grads + ((size_t)bh * a.grad_tiles + t / GT) * D * DV + c0);
+            if (t % GT == GT - 1 || t == t1 - 1) save_state<KB, DV>(S, ln, st.grads + (((size_t)bh * a.grad_tiles + t / GT) * D + d0) * DV + c0);
         f32x16 du = {};   // a row per token
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) du = mm<MADE>(kt.kp(ln, 0, 32 * kb, m), split<MADE>(S[kb], m), du);
+            for (int m = 0; m < 2; ++m) du = mm<MADE>(kt.kp(ln, 0, d0 + 32 * kb, m), split<MADE>(S[kb], m), du);
         du *= by_row((const float *)(at + Pr::REST), ln);
         const float whole = *(const float *)(at + Pr::WHOLE);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) S[kb] *= whole;
 #pragma unroll
         for (int f = 0; f < kTile / 16; ++f) {
-            const auto go = dot.ks(ln, 16 * f, c0);
-            du = mm<MADE>(pt.ks(ln, 16 * f), go, du);
+            const auto go = dot.ks(ln, 16 * f, c0 - v0);
+            if (SPLIT == 1 || part == f) du = mm<MADE>(pt.ks(ln, 16 * f), go, du);
             f32x8 y = {};   // Q^T (exp(G) dO)
 #pragma unroll
             for (int i = P::DATA - 1; i >= 0; --i) y += __builtin_convertvector(go.p[i], f32x8);
@@ -908,7 +942,12 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
             y *= __builtin_shufflevector(*(const f32x4 *)start, *(const f32x4 *)(start + 4), 0, 1, 2, 3, 4, 5, 6, 7);
             const auto s = split<MADE>(y);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(qt.ks(ln, 16 * f, 32 * kb), s, S[kb]);
+            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(qt.ks(ln, 16 * f, d0 + 32 * kb), s, S[kb]);
+        }
+        if constexpr (SPLIT == 2) {
+            put_tile((float *)(lds + L::XCH + wave * kSquareBytes), ln, du);
+            __syncthreads();
+            du += get_tile((const float *)(lds + L::XCH + ((1 - part) * L::CW + cw) * kSquareBytes), ln);
         }
         const f32x16 beta = by_row((const float *)(at + Pr::BETA), ln);
         {
@@ -919,19 +958,19 @@ __global__ __launch_bounds__((Back<T, D, DV>::NT), (waves_of<T, D, DV>())) void 
         const f32x16 dv = beta * du;
         if constexpr (!LOCAL) {
             const size_t to = (row + token0) * DV + c0;
-            store_rows<DV>(st.dr + to, ln, there, du);
-            store_rows<DV>(dV + to, ln, there, dv);
+            if (part == 0) store_rows<DV>(st.dr + to, ln, there, du);
+            if (part == SPLIT - 1) store_rows<DV>(dV + to, ln, there, dv);
         }
         const f32x16 z = -dv * by_row((const float *)(at + Pr::START), ln);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const auto f = split<MADE>(z, m);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, 32 * kb, m), f, S[kb]);
+            for (int kb = 0; kb < KB; ++kb) S[kb] = mm<MADE>(kt.ksp(ln, 0, d0 + 32 * kb, m), f, S[kb]);
         }
     }
-    if (LOCAL) save_state<KB, DV>(S, ln, st.local + ((size_t)bh * a.segments + seg) * D * DV + c0);
-    else if (seg == 0) save_state<KB, DV>(S, ln, st.first + (size_t)bh * D * DV + c0);
+    if (LOCAL) save_state<KB, DV>(S, ln, st.local + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
+    else if (seg == 0) save_state<KB, DV>(S, ln, st.first + ((size_t)bh * D + d0) * DV + c0);
 }
 
 // ---------------------------------------------------------------------------
@@ -1293,17 +1332,22 @@ struct Forward {
         float *trans = (float *)(ca ? ca + l.trans : sc + l.own_trans), *local = (float *)(sc + l.local), *first = (float *)(sc + l.first);
         k_delta_prep<T, D><<<dim3((p.tiles + kWaves - 1) / kWaves, bh), dim3(kThreads), 0, s>>>(q, k, inv, c);
         WalkStates st{a.kv_in, a.kv_out, local, trans, (float *)ca, (float *)(ca ? ca + l.w : nullptr), ca != nullptr};
-        const dim3 grid(p.segments * bh);
         if (p.segments > 1) {
-            typedef Walk<T, D, DV, true> L;
-            if (hipError_t e = room(k_delta_walk<T, D, DV, true>, L::LDS); e != hipSuccess) return e;
-            k_delta_walk<T, D, DV, true><<<grid, dim3(L::NT), L::LDS, s>>>(nullptr, k, v, inv, nullptr, st, c);
+            if (hipError_t e = walk<T, D, DV, true>(nullptr, k, v, inv, nullptr, st, c); e != hipSuccess) return e;
             k_delta_scan<D, false><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.kv_in, trans, local, first, DV, p.segments);
             st.first = first;
         }
-        typedef Walk<T, D, DV, false> L;
-        if (hipError_t e = room(k_delta_walk<T, D, DV, false>, L::LDS); e != hipSuccess) return e;
-        k_delta_walk<T, D, DV, false><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, v, inv, (T *)a.out, st, c);
+        return walk<T, D, DV, false>(q, k, v, inv, (T *)a.out, st, c);
+    }
+    template <typename T, int D, int DV, bool LOCAL>
+    hipError_t walk(const T *q, const T *k, const T *v, const char *inv, T *out, const WalkStates &st, const DeltaCall &c) const {
+        return p.split ? walk<T, D, DV, LOCAL, 2>(q, k, v, inv, out, st, c) : walk<T, D, DV, LOCAL, 1>(q, k, v, inv, out, st, c);
+    }
+    template <typename T, int D, int DV, bool LOCAL, int SPLIT>
+    hipError_t walk(const T *q, const T *k, const T *v, const char *inv, T *out, const WalkStates &st, const DeltaCall &c) const {
+        typedef Walk<T, D, DV, LOCAL, SPLIT> L;
+        if (hipError_t e = room(k_delta_walk<T, D, DV, LOCAL, SPLIT>, L::LDS); e != hipSuccess) return e;
+        k_delta_walk<T, D, DV, LOCAL, SPLIT><<<dim3(p.segments * p.B * p.H, L::GROUPS), dim3(L::NT), L::LDS, s>>>(q, k, v, inv, out, st, c);
         return hipGetLastError();
     }
 };
@@ -1320,19 +1364,15 @@ struct Backward {
         const Layout l = layout(p);
         char *sc = (char *)a.scratch, *ca = (char *)a.cache;
         const char *inv = ca + l.inv;
-        typedef Back<T, D, DV> L;
         float *last = (float *)(sc + l.last);
         BackStates st{a.dkv_out, a.dkv_in, (float *)(sc + l.back_local), (float *)sc, (float *)(sc + l.dr)};
-        const dim3 grid(p.segments * bh);
         if (p.segments > 1) {
-            if (hipError_t e = room(k_delta_back<T, D, DV, true>, L::LDS); e != hipSuccess) return e;
-            k_delta_back<T, D, DV, true><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, dout, inv, nullptr, st, c);
+            if (hipError_t e = back<T, D, DV, true>(q, k, dout, inv, nullptr, st, c); e != hipSuccess) return e;
             k_delta_scan<D, true><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.dkv_out, (const float *)(ca + l.trans), st.local, last, DV,
                                                                                    p.segments);
             st.last = last;
         }
-        if (hipError_t e = room(k_delta_back<T, D, DV, false>, L::LDS); e != hipSuccess) return e;
-        k_delta_back<T, D, DV, false><<<grid, dim3(L::NT), L::LDS, s>>>(q, k, dout, inv, (T *)a.dv, st, c);
+        if (hipError_t e = back<T, D, DV, false>(q, k, dout, inv, (T *)a.dv, st, c); e != hipSuccess) return e;
         if (p.key_heads == p.H) return grad<T, D>(c, (T *)a.dq, (T *)a.dk, st, l);
         const size_t n = (size_t)bh * p.N * D;
         float *part = (float *)(sc + l.part);
@@ -1340,6 +1380,17 @@ struct Backward {
         const int share = p.H / p.key_heads;
         k_delta_group<T, D><<<dim3((unsigned)((n / share / 4 + kThreads - 1) / kThreads), 2), dim3(kThreads), 0, s>>>(part, (T *)a.dq, (T *)a.dk, n, share,
                                                                                                              p.N);
+        return hipGetLastError();
+    }
+    template <typename T, int D, int DV, bool LOCAL>
+    hipError_t back(const T *q, const T *k, const T *dout, const char *inv, T *dv, const BackStates &st, const DeltaCall &c) const {
+        return p.split ? back<T, D, DV, LOCAL, 2>(q, k, dout, inv, dv, st, c) : back<T, D, DV, LOCAL, 1>(q, k, dout, inv, dv, st, c);
+    }
+    template <typename T, int D, int DV, bool LOCAL, int SPLIT>
+    hipError_t back(const T *q, const T *k, const T *dout, const char *inv, T *dv, const BackStates &st, const DeltaCall &c) const {
+        typedef Back<T, D, DV, SPLIT> L;
+        if (hipError_t e = room(k_delta_back<T, D, DV, LOCAL, SPLIT>, L::LDS); e != hipSuccess) return e;
+        k_delta_back<T, D, DV, LOCAL, SPLIT><<<dim3(p.segments * p.B * p.H, L::GROUPS), dim3(L::NT), L::LDS, s>>>(q, k, dout, inv, dv, st, c);
         return hipGetLastError();
     }
     template <typename T, int D, typename TO>
@@ -1355,10 +1406,13 @@ struct Backward {
 }  // namespace
 
 // Segments: a walk takes the longer the fewer workgroups it has. Cutting a sequence costs a second walk (the local one, over twice the
-// columns) and a chain of one step a segment: two workgroups a CU are looked for, a segment has two tiles or more, the chain is kept in
-// proportion to the walk, and fewer than five segments do not pay. (Forward, bf16, heads of 128, 8 x 1777 tokens x 16 heads: 221 us
-// uncut, 265 in four; with gradients, 8 x 4096 x 8 heads: 705 us in eight, 730 uncut; float, 2 x 1001 x 4 heads: 181 us in 11, 284 in
-// four; 32768 x 16 heads: 2.03 ms in 32 as in 16, 2.2 in 48.)
+// columns) and a chain of one step a segment: two workgroups a CU are looked for, a segment has two tiles or more, the chain is kept to a
+// part of the walk, and fewer than five segments do not pay. (Forward, bf16, heads of 128: 8 x 1777 tokens x 16 heads 217 us uncut, 303 in
+// four; 16384 x 8 heads 250 us in 31 segments, 316 in 52. Forward and backward: 32768 x 16 heads 2.03 ms in 32 as in 16, 2.2 in 48;
+// 8 x 4096 x 8 heads with keys of 64 705 us in eight, 730 uncut; 4096 x 16 heads 372 us in 16, 424 in 26, 396 in 11.)
+// split: a second wave to every 32 columns, which takes half of the key features, as long as every such workgroup has a CU to itself. (The
+// two meet once a tile: 8 x 1777 x 16 heads 217 us with it and 253 without, float, 2 x 1001 x 4 heads, forward and backward 153 and 185;
+// beyond that it costs: 12 x 1777 x 16 heads 405 us with it, 275 without.)
 DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_heads) {
     DeltaPlan p{B, H, N, D, Dv, dtype, key_heads};
     p.tiles = (int)(((long long)N + kTile - 1) / kTile);
@@ -1366,10 +1420,11 @@ DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_head
     p.grad_tiles = (p.tiles + together - 1) / together;
     const long long walks = (long long)B * H;
     int cut = (int)std::min<long long>(2 * kCus / std::min<long long>(walks, 2 * kCus), p.tiles / 2);
-    while (cut > 1 && (long long)cut * cut > 6LL * p.tiles) --cut;
+    while (cut > 1 && (long long)cut * cut > 2LL * p.tiles) --cut;
     if (cut < 5) cut = 1;
     p.seg_tiles = ((p.tiles + cut - 1) / cut + together - 1) / together * together;
     p.segments = (p.tiles + p.seg_tiles - 1) / p.seg_tiles;
+    p.split = walks * p.segments * (Dv / kSplitCols) <= kCus;
     return p;
 }
 size_t delta_cache(const DeltaPlan &p) { return layout(p).cache; }
