@@ -121,6 +121,18 @@ def test_forward_and_backward(L, O, dtype, kw):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,Dv", [(64, 64), (64, 128), (128, 64), (128, 128)])
+def test_many_states(L, O, dtype, D, Dv):
+    """As many states as fill the card (a wave then has all key features of its columns), uncut and in segments; fewer in segments."""
+    x = make(dtype, B=9, H=32, N=67, D=D, Dv=Dv, Hk=16, seed=3)
+    lens = [67, 0, 1, 64, 65, 33, 32, 31, 66]
+    check(O, Call(L, x, dtype, lens).run(), want(O, x, lens), dtype)
+    for H in (52 if Dv == 64 else 28, 3):
+        x = make(dtype, H=H, N=550, D=D, Dv=Dv, seed=4)
+        check(O, Call(L, x, dtype).run(), want(O, x), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kw", [dict(N=1), dict(N=3, D=128), dict(N=16, Dv=128), dict(N=7, B=5, H=4, Hk=2, D=128), dict(N=9, gate=False, states=False),
                                 dict(N=2, B=40, H=8, D=128), dict(N=17), dict(N=600, D=128)], ids=str)
 def test_forward_without_a_cache(L, O, dtype, kw):
