@@ -10,7 +10,6 @@
 namespace lasp {
 
 constexpr int kDeltaTile = 32;         // tokens of a walk's tile
-constexpr int kDeltaStepTokens = 16;   // forward calls up to this length, without a cache, run token by token
 
 struct DeltaPlan {
     int B, H, N, D, Dv, dtype, key_heads;
@@ -18,6 +17,8 @@ struct DeltaPlan {
     int segments, seg_tiles;  // segments a sequence is cut into, tiles of one
     bool split;               // the walks: a state's key features shared by two waves
 };
+// Forward calls without a cache run token by token up to this length.
+inline int delta_step_tokens(const DeltaPlan &p) { return p.dtype == 0 ? 8 : 4; }
 DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_heads);
 
 struct DeltaArgs {

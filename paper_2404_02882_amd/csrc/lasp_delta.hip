@@ -1318,8 +1318,11 @@ struct Forward {
         const DeltaCall c = call_of(p, a);
         const int bh = p.B * p.H;
         const T *q = (const T *)a.q, *k = (const T *)a.k, *v = (const T *)a.v;
-        if (!a.cache && p.N <= kDeltaStepTokens) {
-            // narrower blocks of columns where 32 would not give every CU two workgroups
+        // Token by token (16 heads of 128): bf16, 1 sequence 11 us for 4 tokens, 19 for 16, in a tile 13; 64 sequences 36 for 4, 63 for 8,
+        // 115 for 16, in a tile 42. Float: 11 for 8 and 62 for 8, in a tile 17 and 67.
+        if (!a.cache && p.N <= delta_step_tokens(p)) {
+            // narrower blocks of columns where 32 would not give every CU two workgroups (64 sequences: 23 us with 32, 33 with 16;
+            // one: 13 and 10)
             if (bh * (DV / 32) >= 2 * kCus)
                 k_delta_step<T, D, 32><<<dim3(bh * (DV / 32)), dim3(kThreads), 0, s>>>(q, k, v, a.kv_in, (T *)a.out, a.kv_out, c);
             else

@@ -75,7 +75,7 @@ int lasp_delta_fwd(const lasp_delta_shape *shape, const void *q, const void *k, 
     lasp::DeltaPlan p;
     if (int rc = make(shape, &p); rc != LASP_OK) return rc;
     if (!q || !k || !v || !beta || !out || !kv_out) return LASP_ERR_NULL;
-    const size_t need = !state_cache && p.N <= lasp::kDeltaStepTokens ? 0 : lasp::delta_scratch(p);
+    const size_t need = !state_cache && p.N <= lasp::delta_step_tokens(p) ? 0 : lasp::delta_scratch(p);
     if (need > 0 && (!scratch || scratch_bytes < need)) return LASP_ERR_WORKSPACE;
     if (need == 0) scratch = nullptr;
     const Sizes b(p);
