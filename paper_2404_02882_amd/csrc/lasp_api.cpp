@@ -598,13 +598,13 @@ hipError_t allow_dynamic_lds(const void *kernel, size_t bytes) {
 
 extern "C" {
 
-int lasp_version(void) { return 7; }
+int lasp_version(void) { return 8; }
 
 const char *lasp_status_str(int status) {
     switch (status) {
         case LASP_OK: return "ok";
         case LASP_ERR_NULL: return "a required pointer is NULL";
-        case LASP_ERR_SHAPE: return "unsupported shape (attention: need B,H,N > 0, D and Dv in {64,128} (Dv 0 = D), chunk in {64,128,256}, 0 <= segments <= ceil(N/tile); recurrence and norms: sizes > 0, rows of a multiple of 8 elements, see lasp_rec_shape, lasp_rows, lasp_gate_shape) or eps";
+        case LASP_ERR_SHAPE: return "unsupported shape (attention: need B,H,N > 0, D and Dv in {64,128} (Dv 0 = D), chunk in {64,128,256}, 0 <= segments <= ceil(N/tile); recurrence and norms: sizes > 0, rows of a multiple of 8 elements, see lasp_rec_shape, lasp_rows, lasp_gate_shape; delta rule and queries/keys: see lasp_delta_shape, lasp_qk_shape) or eps";
         case LASP_ERR_DTYPE: return "unsupported dtype (LASP_F32 or LASP_BF16)";
         case LASP_ERR_DECAY: return "decay must be finite and in (0, 1] (log decay: finite and <= 0)";
         case LASP_ERR_WORKSPACE: return "scratch buffer missing or too small (see lasp_scratch_bytes); lasp_fwd_noalloc: the shape needs more scratch than the library holds (see lasp_noalloc_scratch_limit)";
