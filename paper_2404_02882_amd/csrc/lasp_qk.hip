@@ -5,7 +5,7 @@
 // A head of a token is a row: LANES threads with one piece of 16 bytes each. The workgroup first makes the table of cosines and
 // sines of the tokens it takes, each angle once for all heads (an angle costs about as much as ten rows' pieces: position times frequency in 64 bits, whole turns
 // taken off there, so that far positions keep the float's precision), then its threads go over the rows of these tokens, queries and keys.
-// Bound by memory: 32768 tokens x 16 + 16 heads of 128, bfloat16: forward 120 us (4.5 TB/s), backward 155 (5.2 TB/s). A row's next piece is
+// Bound by memory: 32768 tokens x 16 + 16 heads of 128, bfloat16: forward 112 us (4.8 TB/s), backward 155 (5.2 TB/s). A row's next piece is
 // loaded before this one is used. A few tokens (64 x 16 + 4 heads): 5.2 us, launch, table and one row one after the other.
 #include <hip/hip_runtime.h>
 
@@ -139,11 +139,11 @@ struct Weighted {
     float own[W], other[W];
 };
 template <typename T, int LANES>
-DEVI Weighted<Piece<T>::W> weighted(const float *w, const Turn<T, LANES> &my, bool has) {
+DEVI Weighted<Piece<T>::W> weighted(const float *w, const Turn<T, LANES> &my) {
     constexpr int W = Piece<T>::W;
     Weighted<W> f;
-    weights_of<W>(w, my.at, has, f.own);
-    weights_of<W>(w, (my.other & (LANES - 1)) * W, has && my.first >= 0, f.other);
+    load_floats<W>(w + my.at, f.own);
+    load_floats<W>(w + (my.other & (LANES - 1)) * W, f.other);
     return f;
 }
 
@@ -157,7 +157,13 @@ __global__ __launch_bounds__(kThreads) void k_qk_fwd(const T *__restrict__ xq, c
     const bool has = lane * W < c.D;
     const Turn<T, LANES> my(c, lane);
     const int at = has ? my.at : 0;
-    const auto ws_q = weighted<T, LANES>(wq, my, has), ws_k = weighted<T, LANES>(wk, my, has);
+    __shared__ __attribute__((aligned(16))) float weights[2][LANES * W];   // (read once a group: in registers they leave room for four waves a SIMD, not five)
+    for (int e = threadIdx.x; e < 2 * LANES * W; e += kThreads) {
+        const int n = e / (LANES * W), d = e - n * LANES * W;
+        const float *w = n ? wk : wq;
+        weights[n][d] = w && d < c.D ? w[d] : 1.0f;
+    }
+    if (!c.rot) __syncthreads();
     for (int token0 = blockIdx.x * c.group; token0 < c.tokens; token0 += gridDim.x * c.group) {
         const int count = min(c.group, c.tokens - token0);
         if (c.rot) {
@@ -165,7 +171,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_fwd(const T *__restrict__ xq, c
             make_table(c, table, token0, count);
             __syncthreads();
         }
-        auto part = [&](const T *x, T *y, const Weighted<W> &w, int heads, long long ld) {
+        auto part = [&](const T *x, T *y, const float *ws, int heads, long long ld) {
+            const auto w = weighted<T, LANES>(ws, my);
             Walk r(c, token0, count, heads, threadIdx.x / LANES);
             const T *rows = x + (size_t)token0 * ld + at;
             auto load = [&]() { return gload<u32x4, STREAM>(r.left > 0 ? rows + r.slot * ld + r.head * c.D : rows, 0); };
@@ -190,8 +197,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_fwd(const T *__restrict__ xq, c
                 if (now.left > 0 && has) put<STREAM>(y + (((size_t)now.b * heads + now.head) * c.N + now.s) * c.D + at, P::pack(f));
             }
         };
-        part(xq, yq, ws_q, c.H, c.ldq);
-        if (c.Hk) part(xk, yk, ws_k, c.Hk, c.ldk);
+        part(xq, yq, weights[0], c.H, c.ldq);
+        if (c.Hk) part(xk, yk, weights[1], c.Hk, c.ldk);
     }
 }
 
@@ -280,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_bwd(const T *__restrict__ xq, c
 
 constexpr int kCus = 256;
 // Tokens of a group: four, and no more than the table holds or than leave four workgroups a CU something to do (bf16, 32768 tokens x 16 + 16
-// heads of 128: forward 122 us with four, 126 with eight, 128 with 16; backward 155, 162, 163).
+// heads of 128, with eight workgroups a CU: forward 122 us with four, 126 with eight, 128 with 16; backward 155, 162, 163).
 int group_of(const QkPlan &p) {
     const long long tokens = (long long)p.B * p.N;
     const long long room = p.rot ? std::min(4, kTable / (p.rot / 2)) : 4;
@@ -290,9 +297,10 @@ int workgroups(const QkPlan &p, int a_cu) {
     const long long tokens = (long long)p.B * p.N, g = group_of(p);
     return (int)std::min<long long>((tokens + g - 1) / g, (long long)a_cu * kCus);
 }
-// Workgroups a CU. Forward, 4 to 64 are within 3% of each other; backward each leaves a row of partial sums (same sizes: 185 us with two a CU,
-// 162 with four, 161 with eight, 165 with sixteen; float, 7503 tokens x 8 + 2 heads of 64: 20, 15.7, 13.2, 13.2).
-constexpr int kForwardACu = 8, kBackwardACu = 8;
+// Workgroups a CU. Forward 64, which is one a group up to 65536 tokens (same sizes: 112 us, 120 with eight; 20012 tokens x 12 + 12 heads of 96: 45.6,
+// 49.6); backward each leaves a row of partial sums (185 us with two a CU, 162 with four, 161 with eight, 165 with sixteen; float, 7503 tokens x
+// 8 + 2 heads of 64: 20, 15.7, 13.2, 13.2).
+constexpr int kForwardACu = 64, kBackwardACu = 8;
 QkCall call_of(const QkPlan &p, const QkArgs &a) {
     return {p.B, p.N, p.H, p.Hk, p.D, p.rot, p.half, p.norm, p.B * p.N, group_of(p), p.ldq, p.ldk, a.eps, a.amplitude, p.norm == 1 ? 1.0f / p.D : 1.0f, a.freq, a.pos};
 }
