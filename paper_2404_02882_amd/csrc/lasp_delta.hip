@@ -389,12 +389,13 @@ struct DeltaCall {
     DEVI size_t key_row(int b, int h) const { return ((size_t)b * Hk + h / (H / Hk)) * N; }   // first row of a head of q, k
 };
 
-// What k_delta_prep leaves of a tile: N, scores P (a row per query), and by token exp(G_i), exp(G_C - G_i), beta_i, and (every one the same) exp(G_C).
+// What k_delta_prep leaves of a tile: N, by token exp(G_i), exp(G_C - G_i), beta_i and (every one the same) exp(G_C), and (last, as a walk without
+// outputs has no use for them) the scores P, a row per query.
 template <typename T>
 struct Prepared {
     typedef Block<Parts<T>::MADE> Square;
-    static constexpr int N = 0, P = Square::BYTES, START = 2 * Square::BYTES, REST = START + 4 * kTile, BETA = REST + 4 * kTile, WHOLE = BETA + 4 * kTile,
-                         BYTES = WHOLE + 4 * kTile;
+    static constexpr int N = 0, START = Square::BYTES, REST = START + 4 * kTile, BETA = REST + 4 * kTile, WHOLE = BETA + 4 * kTile, P = WHOLE + 4 * kTile,
+                         BYTES = P + Square::BYTES;
 };
 
 // ---------------------------------------------------------------------------
@@ -559,6 +560,25 @@ DEVI void save_state(const f32x16 (&S)[KB], const Lane &ln, float *dst) {
     for (int kb = 0; kb < KB; ++kb) store_rows<LD>(dst + 32 * kb * LD, ln, 32, S[kb]);
 }
 
+// A matrix as k_delta_scan's waves load it, sixteen bytes a lane and a kilobyte an instruction: of rows 16 tile + l16 the columns 16 step + 4 l4 .. + 3.
+// (Row by row, neighbouring lanes are rows apart, and the loads of a step take longer than its products: 109 us for 32 segments x 16 heads.)
+template <int D>
+DEVI unsigned matrix_piece(int tile, int step, int l16, int l4) { return ((tile * (D / 16) + step) * 64 + 16 * l4 + l16) * 4; }
+// A wave's part of T, rows from d0 on of the lane's column c, and of T^T (may be null).
+template <int KB, int D>
+DEVI void save_matrix(const f32x16 (&S)[KB], const Lane &ln, int d0, int c, float *T, float *back, size_t at) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int r = d0 + 32 * kb + 8 * g + 4 * ln.h;
+            const f32x4 v{S[kb][4 * g], S[kb][4 * g + 1], S[kb][4 * g + 2], S[kb][4 * g + 3]};
+            if (back) *(f32x4 *)(back + at + matrix_piece<D>(c / 16, r / 16, c % 16, r % 16 / 4)) = v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) T[at + matrix_piece<D>(r / 16, c / 16, r % 16 + e, c % 16 / 4) + c % 4] = v[e];
+        }
+}
+
 // ---------------------------------------------------------------------------
 // k_delta_walk: a wave carries 32 columns of the state in its accumulators and meets no other wave's: what a product leaves in an
 // accumulator tile (a row per token or key feature, a lane per column) is the next one's operand as it lies there, with the contraction in the
@@ -577,13 +597,14 @@ struct Walk {
     static constexpr int VALUES = COLS < DV ? COLS : DV;
     typedef Tile<1, kTile, VALUES> Value;
     static constexpr bool STAGED = sizeof(T) == 2;   // two-byte values go through LDS, which hands a lane four tokens of its column at a time
-    static constexpr int PREP = 0, K = Prepared<T>::BYTES, V = K + Data::BYTES, Q = V + (STAGED ? Value::BYTES : 0),
+    static constexpr int PREP = LOCAL ? Prepared<T>::P : Prepared<T>::BYTES;   // what is taken of a prepared tile
+    static constexpr int K = PREP, V = K + Data::BYTES, Q = V + (STAGED ? Value::BYTES : 0),
                          STAGE = LOCAL ? Q : Q + Data::BYTES, XCH = 2 * STAGE, LDS = XCH + (SPLIT == 1 ? 0 : CW * (LOCAL ? 2 : 3) * kSquareBytes);
 };
 struct WalkStates {
     const float *first;   // states that segments start from ([head][segment], or kv_in where there is one segment); null = zeros
     float *last;          // kv_out
-    float *local, *trans; // LOCAL
+    float *local, *trans, *back;   // LOCAL: state, T and (goes with the cache) T^T, as k_delta_scan takes them
     float *cache;         // the state in front of every tile that k_delta_grad takes; may be null
     float *w;             // w of every token; goes with the cache
     int all_trans;        // T is wanted of the last segment too
@@ -616,7 +637,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
         load_state<KB, DV>(S, ln, LOCAL || !st.first ? nullptr : st.first + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
     }
     Fetch<T, kTile, D, L::NT> fk, fq;
-    Copy<Pr::BYTES, L::NT> fp;
+    Copy<L::PREP, L::NT> fp;
     Fetch<T, kTile, L::VALUES, L::NT> fv;   // (STAGED)
     f32x16 v = {};                   // (else)
     auto fetch = [&](int t) {
@@ -694,7 +715,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
         }
     }
     if constexpr (LOCAL) {
-        if (trans) save_state<KB, D>(S, ln, st.trans + (((size_t)bh * a.segments + seg) * D + d0) * D + c0);
+        if (trans) save_matrix<KB, D>(S, ln, d0, c0 + ln.r, st.trans, st.back, ((size_t)bh * a.segments + seg) * D * D);
         else save_state<KB, DV>(S, ln, st.local + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
     } else {
         if (part == 0)
@@ -724,22 +745,16 @@ __global__ __launch_bounds__(4 * D) void k_delta_scan(const float *__restrict__ 
     f32x4 x[TILES];
     auto at = [&](size_t segment, int tl, int i) { return (segment * D + 16 * (wave * TILES + tl) + 4 * l4 + i) * Dv + c; };
     auto fetch = [&](Step &to, int step) {
-        if (step + 1 >= segments) return;
+        step = min(step, segments - 2);   // (without a branch, behind which no load could be waited for apart from those that follow it)
         const int p = BACK ? segments - 1 - step : step;
         const float *t = trans + ((size_t)bh * segments + p) * D * D;
 #pragma unroll
         for (int tl = 0; tl < TILES; ++tl) {
-            const int d = 16 * (wave * TILES + tl) + l16;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                if constexpr (BACK) {
+                const f32x4 y = *(const f32x4 *)(t + matrix_piece<D>(wave * TILES + tl, s, l16, l4));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) to.m[tl][4 * s + i] = t[(size_t)(16 * s + 4 * l4 + i) * D + d];
-                } else {
-                    const f32x4 y = *(const f32x4 *)(t + (size_t)d * D + 16 * s + 4 * l4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) to.m[tl][4 * s + i] = y[i];
-                }
+                for (int i = 0; i < 4; ++i) to.m[tl][4 * s + i] = y[i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) to.add[tl][i] = local[at((size_t)bh * segments + p, tl, i)];
@@ -1283,7 +1298,7 @@ constexpr int kCus = 256;
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 struct Layout {   // byte offsets
-    size_t states, inv, trans, w, cache;                      // cache
+    size_t states, inv, trans, back, w, cache;                // cache
     size_t own_inv, own_trans, local, first, scratch;         // forward scratch
     size_t grads, dr, back_local, last, part, back_scratch;   // backward scratch
 };
@@ -1294,7 +1309,8 @@ Layout layout(const DeltaPlan &p) {
     const size_t trans = p.segments > 1 ? bh * p.segments * p.D * p.D * 4 : 0;
     l.inv = up(bh * p.grad_tiles * state);
     l.trans = l.inv + up(inv);
-    l.w = l.trans + up(trans);
+    l.back = l.trans + up(trans);
+    l.w = l.back + up(trans);
     l.cache = l.w + up(rows);
     l.own_trans = up(inv);
     l.local = l.own_trans + up(trans);
@@ -1344,9 +1360,9 @@ struct Forward {
         const Layout l = layout(p);
         char *sc = (char *)a.scratch, *ca = (char *)a.cache;
         char *inv = ca ? ca + l.inv : sc;
-        float *trans = (float *)(ca ? ca + l.trans : sc + l.own_trans), *local = (float *)(sc + l.local), *first = (float *)(sc + l.first);
+        float *trans = (float *)(ca ? ca + l.trans : sc + l.own_trans), *back = (float *)(ca ? ca + l.back : nullptr), *local = (float *)(sc + l.local), *first = (float *)(sc + l.first);
         k_delta_prep<T, D><<<dim3((p.tiles + kWaves - 1) / kWaves, bh), dim3(kThreads), 0, s>>>(q, k, inv, c);
-        WalkStates st{a.kv_in, a.kv_out, local, trans, (float *)ca, (float *)(ca ? ca + l.w : nullptr), ca != nullptr};
+        WalkStates st{a.kv_in, a.kv_out, local, trans, back, (float *)ca, (float *)(ca ? ca + l.w : nullptr), ca != nullptr};
         if (p.segments > 1) {
             if (hipError_t e = walk<T, D, DV, true>(nullptr, k, v, inv, nullptr, st, c); e != hipSuccess) return e;
             k_delta_scan<D, false><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.kv_in, trans, local, first, DV, p.segments);
@@ -1383,7 +1399,7 @@ struct Backward {
         BackStates st{a.dkv_out, a.dkv_in, (float *)(sc + l.back_local), (float *)sc, (float *)(sc + l.dr)};
         if (p.segments > 1) {
             if (hipError_t e = back<T, D, DV, true>(q, k, dout, inv, nullptr, st, c); e != hipSuccess) return e;
-            k_delta_scan<D, true><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.dkv_out, (const float *)(ca + l.trans), st.local, last, DV,
+            k_delta_scan<D, true><<<dim3(bh, DV / kScanCols), dim3(4 * D), 0, s>>>(a.dkv_out, (const float *)(ca + l.back), st.local, last, DV,
                                                                                    p.segments);
             st.last = last;
         }
