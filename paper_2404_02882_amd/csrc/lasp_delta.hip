@@ -22,12 +22,13 @@
 // 24), as states and the gradients of gates and betas come out in float and a state passes every tile: two parts (2^-18)
 // leave them further off than float sums do. Two where all that follows is rounded to bfloat16. Float data is split in three as well;
 // products of parts below the last kept bit are left out.
-// 32768 tokens x 16 heads of 128, bfloat16, forward and backward: 2.02 ms, 12 KB of memory a token and head (6.3 GB, 3.1 TB/s over all):
+// 32768 tokens x 16 heads of 128, bfloat16, forward and backward: 1.98 ms, 12 KB of memory a token and head (6.3 GB, 3.2 TB/s over all):
 // outputs and inputs are 2.8 KB of it, the rest states and their gradients every 64 tokens (4 KB), w and dR in float (2 KB), N, P and gates
 // (1.9 KB), and keys, queries and values read again. k_delta_walk and k_delta_back run at 4.6 TB/s of it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lasp_delta.h"
 #include "lasp_device.h"
@@ -256,17 +257,19 @@ struct Tile {
     }
 };
 
-// Rows of a global tensor on their way to a tile: 16 bytes a thread (of NT) and piece. Rows from `valid` on are zeros.
+// Rows of a global tensor on their way to a tile: 16 bytes a thread (of NT) and piece. Rows from `valid` (at least 1) on are zeros, but the last of the
+// others is read in their place: behind a load that may not have been issued no other one could be waited for by itself.
 template <typename T, int ROWS, int WIDTH, int NT>
 struct Fetch {
     static constexpr int EPC = 16 / sizeof(T), CPR = WIDTH / EPC, PIECES = ROWS * CPR, N = (PIECES + NT - 1) / NT;
     u32x4 v[N];
+    int rows;
     DEVI void load(const T *base, size_t ld, int valid) {
+        rows = valid;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = threadIdx.x + n * NT, row = c / CPR, col = (c % CPR) * EPC;
-            v[n] = u32x4{0, 0, 0, 0};
-            if (row < valid) v[n] = *(const u32x4 *)(base + row * ld + col);   // (valid <= ROWS)
+            v[n] = gload<u32x4>(base, (min(row, valid - 1) * (unsigned)ld + col) * sizeof(T));
         }
     }
     template <typename F>
@@ -274,7 +277,8 @@ struct Fetch {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = threadIdx.x + n * NT;
-            if (PIECES % NT == 0 || c < PIECES) f(n, c / CPR, (c % CPR) * EPC, v[n]);
+            const u32x4 x = c / CPR < rows ? v[n] : u32x4{0, 0, 0, 0};
+            if (PIECES % NT == 0 || c < PIECES) f(n, c / CPR, (c % CPR) * EPC, x);
         }
     }
     template <typename Tl>
@@ -294,7 +298,7 @@ struct Copy {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = threadIdx.x + n * NT;
-            if (PIECES % NT == 0 || c < PIECES) v[n] = ((const u32x4 *)base)[c];
+            v[n] = gload<u32x4>((const u32x4 *)base, min(c, PIECES - 1) * 16u);
         }
     }
     DEVI void store(void *to) const {
@@ -727,8 +731,8 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
 
 // ---------------------------------------------------------------------------
 // k_delta_scan: first[0] = in, first[p + 1] = T_p first[p] + local[p]; BACK: last[P - 1] = in, last[p - 1] = T_p^T last[p] + local[p].
-// 16 columns a workgroup, in float. 32 segments x 16 heads of 128: 108 us forward, 90 backward; 3.3 us a step, which a CU needs to load
-// the 64 KB of T. (Fewer segments cost the walks what they save here.)
+// 16 columns a workgroup, in float. 32 segments x 16 heads of 128: 82 us in either direction, 2.5 us a step, a chain of barrier, LDS and 32 matrix
+// products on top of each other; more matrices on their way change nothing. (Fewer segments cost the walks what they save here.)
 // ---------------------------------------------------------------------------
 // (v_mfma_f32_16x16x4_f32: lane l supplies row or column l & 15 and contraction index l >> 4; accumulator rows 4 (l >> 4) .. + 3, column l & 15.)
 constexpr int kScanCols = 16;
@@ -1001,8 +1005,8 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
 // ---------------------------------------------------------------------------
 // k_delta_grad: a tile's gradients, from the state in front of it, the gradient of the one behind it, w and dR, 64 value features at a time. A wave
 // has 32 key features of dQ and dK; its rows of both states come from memory straight into its registers, as they are read once.
-// 32768 tokens x 16 heads of 128, bfloat16: 630 us, 4.6 KB a token and head (3.8 TB/s): two workgroups of four waves a CU, as LDS has room for, wait
-// for their states once per 64 features.
+// 32768 tokens x 16 heads of 128, bfloat16: 610 us, 4.6 KB a token and head (3.9 TB/s), two workgroups of four waves a CU, as LDS has room for. (With
+// loads that a branch may leave out, every wait was one for all of them: 640; keys of 64, 8 x 4096 x 8 heads, 257 us against 235.)
 // ---------------------------------------------------------------------------
 template <int C>
 struct Gates {
@@ -1126,14 +1130,17 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
     f32x16 pr[MINE] = {};                              // w dO^T or w dR^T, a row per key token
     f32x16 aq[PER] = {}, a1[PER] = {}, a2[PER] = {};   // S dO^T, S dR^T, dS w^T, a row per key feature
     float both = 0.0f;                                 // <dS, S>
-    for (int c0 = 0; c0 < a.Dv; c0 += COLS) {
-        const bool more = c0 + COLS < a.Dv;
+    auto columns = [&](int c0, auto next) {
+        constexpr bool more = next;
+        const Lane ln = fresh_lane();   // (offsets that all rounds share take the registers of what is on its way, and are reloaded from memory behind it)
+        int c1 = c0 + COLS;
+        asm volatile("" : "+s"(c1));   // (not seen through: addresses then stay a scalar base and 32 bits a lane, where pointers that are counted up spill)
         if (c0 > 0) __syncthreads();   // the tiles have been read
         fo.store(dot);
         fw.store(wt);
         fr.store(rt);
         __syncthreads();
-        if (more) fetch_rows(c0 + COLS);
+        if constexpr (more) fetch_rows(c1);
 #pragma unroll
         for (int k = 0; k < COLS / 16; ++k) {
             const auto fs = split<MADE>(__builtin_shufflevector(s4[k][0], s4[k][1], 0, 1, 2, 3, 4, 5, 6, 7));
@@ -1143,7 +1150,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) both = __builtin_fmaf(s4[k][i][e], d4[k][i][e], both);
-            if (more) fetch_states(c0 + COLS, k);
+            if constexpr (more) fetch_states(c1, k);
 #pragma unroll
             for (int n = 0; n < PER; ++n) {
                 aq[n] = mm<MADE>(fs, dot.kc(ln, 32 * (tk0 + n), 16 * k), aq[n]);
@@ -1162,7 +1169,9 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
 #pragma unroll
                     for (int k0 = 0; k0 < COLS; k0 += 16) pr[n] = mm<MADE>(wt.kc(ln, 32 * jb, k0), dot.kc(ln, 32 * tb, k0), pr[n]);
             }
-    }
+    };
+    for (int c0 = 0; c0 < a.Dv - COLS; c0 += COLS) columns(c0, std::true_type{});
+    columns(a.Dv - COLS, std::false_type{});
     __syncthreads();
     // dlog_a_i = exp(G_C) <dS, S> + sum_{t >= i} x_t + sum_{j < i} y_j + sum_{t >= i > j} Z_tj: what goes through gate i and nothing else, with
     // x_t = exp(G_t) (q_t . S dO_t - k_t . S dV_t), y_j = exp(G_C - G_j) k_j . dS u_j and Z = Ep q.k + Em k.k. Row and column sums of Z give the last one.
