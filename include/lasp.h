@@ -528,11 +528,11 @@ int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u
  *   kv_in, kv_out, dkv_out, dkv_in   [B][H][D][Dv] float. kv_in, dkv_out: NULL = zeros. kv_out may be kv_in and dkv_in may be dkv_out (the
  *                     same pointer): updated in place.
  *   state_cache       forward: NULL = no backward pass will follow; else lasp_delta_cache_bytes() bytes, to be handed to lasp_delta_bwd
- *                     with the same shape and inputs (it holds kv_in too). One float state for every 64 tokens (float data: 32), a float for
- *                     every value and two squares of 32 by 32 for every 32 tokens.
- *   scratch           lasp_delta_scratch_bytes() bytes forward, lasp_delta_bwd_scratch_bytes() backward (backward: as many states again and a float
- *                     for every value; both: states and matrices of the segments a long sequence is cut into). Not looked at by forward calls without a cache of at most 4 tokens (float data: 8),
- *                     which run token by token.
+ *                     with the same shape and inputs (it holds kv_in too): a float state for every 64 tokens (float data: 32), a float for every
+ *                     value, two squares of 32 by 32 for every 32 tokens, and two of D by D for every segment that a long sequence is cut into.
+ *   scratch           lasp_delta_scratch_bytes() bytes forward (those squares, and the states between segments), lasp_delta_bwd_scratch_bytes()
+ *                     backward (as many states and floats as the cache has). Not looked at by forward calls without a cache of at most 4
+ *                     tokens (float data: 8), which run token by token.
  * Keys are expected to be of length 1 or shorter (lasp_qk_fwd's norm LASP_NORM_L2), with 0 <= beta <= 2: then no state grows; with
  * longer ones it may, as the formula says. States, gates and sums are held in float, sums of log_g in 64 bits. Factors that a call computes
  * go into products in three bfloat16 parts (off by at most 2^-27 of themselves), in two (2^-18) where all that follows is rounded to
