@@ -552,6 +552,14 @@ DEVI void store_rows(T *p, const Lane &ln, int there, const f32x16 &x) {
         for (int e = 0; e < 16; ++e)
             if (ln.acc_row(e) < there) Elem<T>::gst1(p + (8 * (e >> 2)) * LD, at + (e & 3) * LD * sizeof(T), x[e]);
 }
+// Zeros in the rows behind a sequence's end, from row `first` on: what the products leave there is 0 times the state, which need not be a number.
+template <int LD, typename T>
+DEVI void zero_rows(T *p, const Lane &ln, int first, int there) {
+    const unsigned at = (4 * ln.h * LD + ln.r) * sizeof(T);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (ln.acc_row(e) >= first && ln.acc_row(e) < there) Elem<T>::gst1(p + (8 * (e >> 2)) * LD, at + (e & 3) * LD * sizeof(T), 0.0f);
+}
 // A wave's part of a state: KB blocks of 32 key features (rows) by its 32 columns (a lane each).
 template <int KB, int LD>
 DEVI void load_state(f32x16 (&S)[KB], const Lane &ln, const float *src) {
@@ -654,7 +662,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
     };
     if (t0 < t1) fetch(t0);
     for (int t = t0; t < t1; ++t) {
-        const int token0 = t * kTile, there = min(a.N - token0, kTile);
+        const int token0 = t * kTile, valid = min(tokens - token0, kTile);
         unsigned char *at = lds + (t & 1) * L::STAGE;   // (the waves that still read the tile before have the other half)
         const typename L::Data kt{(bf16_t *)(at + L::K)}, qt{(bf16_t *)(at + L::Q)};
         const typename Pr::Square nt{(bf16_t *)(at + Pr::N)}, pt{(bf16_t *)(at + Pr::P)};
@@ -699,13 +707,13 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
             for (int m = 0; m < 2; ++m) r = mm<MADE>(nt.kp(ln, m), split<MADE>(x, m), r);
         }
         if constexpr (!LOCAL)
-            if (st.cache && part == 0) store_rows<DV>(st.w + (row + token0) * DV + c0, ln, there, r);
+            if (st.cache && part == 0) store_rows<DV>(st.w + (row + token0) * DV + c0, ln, valid, r);
         r *= by_row((const float *)(at + Pr::BETA), ln);
         if (!LOCAL && part == SPLIT - 1) {
             o *= ((const float *)(at + Pr::START))[ln.r];
 #pragma unroll
             for (int m = 0; m < 2; ++m) o = mm<P::ROUNDED>(split<P::ROUNDED>(r, m), pt.kp(ln, m), o);
-            if (ln.r < there) store_acc(O + (row + token0 + ln.r) * DV + c0, ln, o);
+            if (ln.r < valid) store_acc(O + (row + token0 + ln.r) * DV + c0, ln, o);
         }
         r *= by_row((const float *)(at + Pr::REST), ln);
         const float whole = *(const float *)(at + Pr::WHOLE);
@@ -723,8 +731,8 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
         else save_state<KB, DV>(S, ln, st.local + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
     } else {
         if (part == 0)
-            for (int t = max(t0, t1); t < end; ++t)
-                store_rows<DV>(O + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
+            for (int t = max(t0, tokens / kTile); t < end; ++t)
+                zero_rows<DV>(O + (row + t * kTile) * DV + c0, ln, tokens - t * kTile, min(a.N - t * kTile, kTile));
         if (seg == a.segments - 1) save_state<KB, DV>(S, ln, st.last + ((size_t)bh * D + d0) * DV + c0);
     }
 }
@@ -923,8 +931,8 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
     f32x16 S[KB];
     load_state<KB, DV>(S, ln, LOCAL || !st.last ? nullptr : st.last + (((size_t)bh * a.segments + seg) * D + d0) * DV + c0);
     if (!LOCAL && part == 0)
-        for (int t = max(t0, t1); t < end; ++t)
-            store_rows<DV>(dV + (row + t * kTile) * DV + c0, ln, min(a.N - t * kTile, kTile), f32x16{});
+        for (int t = max(t0, tokens / kTile); t < end; ++t)
+            zero_rows<DV>(dV + (row + t * kTile) * DV + c0, ln, tokens - t * kTile, min(a.N - t * kTile, kTile));
     Fetch<T, kTile, D, L::NT> fk, fq;
     Fetch<T, kTile, L::COLS, L::NT> fo;
     Copy<Pr::BYTES, L::NT> fp;
@@ -937,7 +945,7 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
     };
     if (t0 < t1) fetch(t1 - 1);
     for (int t = t1 - 1; t >= t0; --t) {
-        const int token0 = t * kTile, there = min(a.N - token0, kTile);
+        const int token0 = t * kTile, valid = min(tokens - token0, kTile);
         unsigned char *at = lds + t % L::STAGES * L::STAGE;
         const typename L::Data kt{(bf16_t *)(at + L::K)}, qt{(bf16_t *)(at + L::Q)};
         const typename L::Grad dot{(bf16_t *)(at + L::DO)};
@@ -987,8 +995,8 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
         const f32x16 dv = beta * du;
         if constexpr (!LOCAL) {
             const size_t to = (row + token0) * DV + c0;
-            if (part == 0) store_rows<DV>(st.dr + to, ln, there, du);
-            if (part == SPLIT - 1) store_rows<DV>(dV + to, ln, there, dv);
+            if (part == 0) store_rows<DV>(st.dr + to, ln, valid, du);
+            if (part == SPLIT - 1) store_rows<DV>(dV + to, ln, valid, dv);
         }
         const f32x16 z = -dv * by_row((const float *)(at + Pr::START), ln);
 #pragma unroll
@@ -1237,7 +1245,8 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         for (int jb = 0; jb <= tk; ++jb)
 #pragma unroll
             for (int k0 = 0; k0 < 32; k0 += 16) x = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), ep.at(tk, jb).kc(ln, k0), x);
-        if (m < there) store_acc(dQ + to, ln, x);
+        if (m < valid) store_acc(dQ + to, ln, x);
+        else if (m < there) store_acc(dQ + to, ln, f32x16{});
         y -= z;
         for (int it = tk; it < NB; ++it)
 #pragma unroll
@@ -1248,14 +1257,15 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         for (int jb = 0; jb <= tk; ++jb)
 #pragma unroll
             for (int k0 = 0; k0 < 32; k0 += 16) y = mm<P::ROUNDED>(kt.ks(ln, 32 * jb + k0, d0), em.at(tk, jb).kc(ln, k0), y);
-        if (m < there) store_acc(dK + to, ln, y);
+        if (m < valid) store_acc(dK + to, ln, y);
+        else if (m < there) store_acc(dK + to, ln, f32x16{});
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) both += __shfl_xor(both, d);
     if (ln.id == 0 && tk0 == 0) red.both[slice] = both;
     __syncthreads();
     if (wave != 0) return;
-    if (ln.id < there) dbeta[row + ln.id] = red.beta[ln.id];
+    if (ln.id < there) dbeta[row + ln.id] = ln.id < valid ? red.beta[ln.id] : 0.0f;
     if (!dlog_g) return;
     double up = 0.0, on = 0.0, all = 0.0;   // x_t;  y_j + column j - row j of Z
     if (ln.id < C) {
