@@ -1032,7 +1032,7 @@ struct Grad {
     typedef Tile<P::MADE, C, COLS> Rows;
     typedef Tile<P::DATA, C, COLS> Out;
     static constexpr int JOBS = 2 * Square::BLOCKS, MINE = (JOBS + WAVES - 1) / WAVES;   // blocks of Ep and of Em; of a wave
-    struct Sums {   // by token: dbeta, row and column sums of Z (of a block), x and y (of a wave's key features); <dS, S>
+    struct Sums {   // by token: dbeta, sums of Z (of a block), x and y (of a wave's key features); <dS, S>
         float beta[C], row[JOBS][32], col[JOBS][32], up[SLICES][C], on[SLICES][C], both[SLICES];
     };
     static constexpr int PAIR = Rows::BYTES > Square::BYTES ? Rows::BYTES : Square::BYTES;   // (Ep and Em take the places of w and dR)
@@ -1056,6 +1056,22 @@ DEVI float sum_lanes(const f32x16 &z, const Lane &ln) {
         for (int i = 0; i < n; ++i) v[i] = choose(up, v[n + i], v[i]) + __shfl_xor(choose(up, v[i], v[n + i]), 2 * n);
     }
     return v[0] + __shfl_xor(v[0], 1);
+}
+// Row i: the sum of the rows in front of it, of a tile with a row per register.
+DEVI f32x16 rows_before(const f32x16 &z, const Lane &ln) {
+    f32x16 x;
+    float all = 0.0f;   // of both halves' rows in front of the four
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const float two = z[4 * g] + z[4 * g + 1], three = two + z[4 * g + 2], four = three + z[4 * g + 3], other = __shfl_xor(four, 32);
+        const float from = ln.h ? all + other : all;
+        x[4 * g] = from;
+        x[4 * g + 1] = from + z[4 * g];
+        x[4 * g + 2] = from + two;
+        x[4 * g + 3] = from + three;
+        all += four + other;
+    }
+    return x;
 }
 template <typename T, int D, typename TO>
 __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_delta_grad(const T *__restrict__ Q, const T *__restrict__ K,
@@ -1182,7 +1198,8 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
     columns(a.Dv - COLS, std::false_type{});
     __syncthreads();
     // dlog_a_i = exp(G_C) <dS, S> + sum_{t >= i} x_t + sum_{j < i} y_j + sum_{t >= i > j} Z_tj: what goes through gate i and nothing else, with
-    // x_t = exp(G_t) (q_t . S dO_t - k_t . S dV_t), y_j = exp(G_C - G_j) k_j . dS u_j and Z = Ep q.k + Em k.k. Row and column sums of Z give the last one.
+    // x_t = exp(G_t) (q_t . S dO_t - k_t . S dV_t), y_j = exp(G_C - G_j) k_j . dS u_j and Z = Ep q.k + Em k.k. The last one without a difference of sums: of a block on the
+    // diagonal a sum for every gate; of the one below it, its columns in front of the gate for the first 32 tokens, its rows from the gate on for the others.
 #pragma unroll
     for (int n = 0; n < MINE; ++n)
         if (job(n) < L::JOBS) {
@@ -1194,7 +1211,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
 #pragma unroll
                 for (int k0 = 0; k0 < D; k0 += 16) z = mm<MADE>(kt.kc(ln, 32 * jb, k0), other.kc(ln, 32 * tb, k0), z);
             }
-            float along = 0.0f, diagonal = 0.0f;
+            float diagonal = 0.0f;
             const float bi = is_em ? -g.beta[i] : 1.0f;
             const f32x16 x = weights_by_row<false>(g.sum + 32 * jb, g.sum[i], ln) * by_row(g.beta + 32 * jb, ln) * bi;
             const int last = 32 * (tb - jb) + ln.r - is_em;   // rows up to here are keys that the token sees
@@ -1205,13 +1222,21 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
                 const float v = pr[n][e] * x[e];
                 pr[n][e] = o <= last ? v : 0.0f;
                 z[e] = o < 32 * (tb - jb) + ln.r ? v * z[e] : 0.0f;
-                along += z[e];
             }
             if (is_em && tb == jb && ln.h == (ln.r >> 2 & 1)) red.beta[i] = diagonal;   // dbeta_i = w_i . dR_i
             if (dlog_g) {
-                along += __shfl_xor(along, 32);
+                if (tb == jb) {
+                    z = rows_before(z, ln);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) z[e] = ln.r >= ln.acc_row(e) ? z[e] : 0.0f;
+                } else {
+                    float along = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) along += z[e];
+                    along += __shfl_xor(along, 32);
+                    if (ln.h == 0) red.row[jo][ln.r] = along;
+                }
                 const float down = sum_lanes(z, ln);
-                if (ln.h == 0) red.row[jo][ln.r] = along;
                 if ((ln.r & 1) == 0) red.col[jo][ln.acc_row(ln.r >> 1)] = down;
             }
             const auto to = is_em ? em.at(tb, jb) : ep.at(tb, jb);
@@ -1267,22 +1292,28 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
     if (wave != 0) return;
     if (ln.id < there) dbeta[row + ln.id] = ln.id < valid ? red.beta[ln.id] : 0.0f;
     if (!dlog_g) return;
-    double up = 0.0, on = 0.0, all = 0.0;   // x_t;  y_j + column j - row j of Z
-    if (ln.id < C) {
+    const bool in = ln.id < C, first = ln.id < 32;
+    double up = 0.0, on = 0.0, across = 0.0, all = 0.0, z = 0.0;   // x_t; y of the token in front; sums of Z below the diagonal
+    if (in) {
 #pragma unroll
         for (int v = 0; v < L::SLICES; ++v) {
             up += red.up[v][ln.id];
-            on += red.on[v][ln.id];
+            on += ln.id > 0 ? red.on[v][ln.id - 1] : 0.0f;
         }
 #pragma unroll
         for (int v = 0; v < L::JOBS; ++v) {
-            if (key_block(v) == ln.id / 32) on += red.col[v][ln.id & 31];
-            if (token_block(v) == ln.id / 32) on -= red.row[v][ln.id & 31];
+            if (token_block(v) != key_block(v)) across += !first ? red.row[v][31 - ln.r] : ln.r > 0 ? red.col[v][ln.r - 1] : 0.0f;   // (rows from the last one on)
+            else if (key_block(v) == ln.id / 32) z += red.col[v][ln.r];
         }
     }
 #pragma unroll
     for (int v = 0; v < L::SLICES; ++v) all += red.both[v];
-    on = sum_up<C>(on, ln.id) - on;         // over the tokens before this one
+    on = sum_up<C>(on, ln.id);
+    if constexpr (NB == 2) {
+        across = sum_up<32>(across, ln.id);
+        const double back = __shfl_xor(across, 31);
+        z += first ? across : back;
+    }
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
         const double y = __shfl_down(up, d, C);
@@ -1290,7 +1321,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
     }
     if (ln.id < there) {
         const bool none = ln.id >= valid || to_base2(a.log_g[row + ln.id]) <= -150.0;   // (a gate of 0 has no slope)
-        dlog_g[row + ln.id] = none ? 0.0f : (float)(g.whole * all + up + on);
+        dlog_g[row + ln.id] = none ? 0.0f : (float)(g.whole * all + up + on + z);
     }
 }
 

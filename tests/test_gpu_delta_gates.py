@@ -1,0 +1,46 @@
+"""Slopes of the gated delta rule's gates where neighbours differ by orders of magnitude, and float results held to what sums in float come to."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_delta import Call, make, np64, want
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def L():
+    assert torch.cuda.is_available(), "needs a GPU"
+    from paper_2404_02882_amd import lasp
+    return lasp
+
+
+@pytest.fixture(scope="module")
+def O():
+    from oracle import delta_oracle
+    return delta_oracle
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kw", [dict(D=64), dict(D=128, Dv=64), dict(D=64, Dv=128, H=4, Hk=2), dict(D=128, N=64)], ids=str)
+@pytest.mark.parametrize("down", [-20.0, -45.0])
+def test_slopes_of_gates_that_let_little_pass(L, O, dtype, kw, down):
+    """dlog_g_i = <dS_{i-1}, S_{i-1}>, the gradient of the state in front of token i times that state. Both come with a relative error of at most
+    DELTA in the 2-norm, and the product with both: 2 DELTA of the product of their norms, whatever the slopes of the tokens around are."""
+    x = make(dtype, seed=4, **{"N": 150, **kw})
+    N = x["v"].shape[2]
+    places = [p for p in (0, 9, 31, 40, 63, 64, 75, 96, 127, 149) if p < N]
+    x["log_g"][..., places] = down
+    call = Call(L, x, dtype).run()
+    got = np64(call.g["dlog_g"])
+    n = {k: np64(t) for k, t in x.items()}
+    w = want(O, x)["dlog_g"]
+    before = O.delta_fwd(*[n[k] for k in ("q", "k", "v", "log_g", "beta")], n["kv_in"])[2]
+    for p in places:
+        rest = {k: (t if k in ("kv_in", "dkv_out") else t[:, :, p:]) for k, t in n.items()}
+        rest["kv_in"] = before[p]
+        dS = O.delta_bwd(*[rest[k] for k in ("q", "k", "v", "log_g", "beta")], rest["dout"], rest["kv_in"], None, rest["dkv_out"])["dkv_in"]
+        size = np.sqrt((dS ** 2).sum((-1, -2)) * (before[p] ** 2).sum((-1, -2)))
+        off = np.abs(got[:, :, p] - w[:, :, p]) / (2 * O.DELTA * size)
+        print(f"  token {p}: {off.max():.3f} of the bound, slope {np.abs(w[:, :, p]).max():.2e}", flush=True)
+        assert off.max() <= 1.0, (p, off.max())
