@@ -131,6 +131,39 @@ DEVI void store_parts(bf16_t *at, f32x4 v) {
     }
 }
 
+// Infinities and NaN. A tile's squares hold zeros where a token does not reach another, and 0 x infinity is NaN: a broken value would spoil tokens of its tile
+// that it does not reach. Operands go without it then, and what it does reach is set to NaN. Whether there is one shows in a sum (one that overflows
+// only costs the search).
+DEVI bool is_broken(float x) { return !(__builtin_fabsf(x) < __builtin_inff()); }
+template <typename V>
+DEVI bool any_broken(const V &x) {   // in any lane of the wave
+    float s[2] = {x[0], x[1]};
+#pragma unroll
+    for (int e = 2; e < (int)(sizeof(V) / 4); ++e) s[e & 1] += x[e];
+    return __builtin_expect(__builtin_amdgcn_ballot_w64(is_broken(s[0] + s[1])) != 0, 0);
+}
+// The first broken row of the lane's column (32: none).
+DEVI int first_broken(const f32x16 &x, const Lane &ln) {
+    int n = 32;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) n = is_broken(x[e]) ? min(n, ln.acc_row(e)) : n;
+    return min(n, __shfl_xor(n, 32));
+}
+// Zeros in place of broken elements.
+template <int NP>
+DEVI void drop_broken(Frags<NP> &f) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        u32x4 x = __builtin_bit_cast(u32x4, f.p[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = (x[e] & 0x7f80u) == 0x7f80u ? x[e] & 0xffff0000u : x[e];
+            x[e] = (x[e] & 0x7f800000u) == 0x7f800000u ? x[e] & 0xffffu : x[e];
+        }
+        f.p[i] = __builtin_bit_cast(bf16x8, x);
+    }
+}
+
 // What the lanes of a wave wrote to LDS is there for its other lanes.
 DEVI void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -441,8 +474,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
     const size_t key_row = a.key_row(b, h) + token0 + ln.r, gate = (size_t)bh * a.N + token0 + ln.r;
     const bool there = ln.r < valid;
     Frags<P::DATA> fk[D / 16], fq[D / 16];
-    operands<T, D>(fk, K + key_row * D, ln, there);
-    operands<T, D>(fq, Q + key_row * D, ln, there);
+    auto load = [&]() {
+        operands<T, D>(fk, K + key_row * D, ln, there);
+        operands<T, D>(fq, Q + key_row * D, ln, there);
+    };
+    load();
     const float bt = there ? a.beta[gate] : 0.0f;
     const double x = sum_up<kTile>(a.log_g && there ? to_base2(a.log_g[gate]) : 0.0, ln.id), all = __shfl(x, kTile - 1, kTile);
     char *to = prepared + ((size_t)bh * a.tiles + tile) * Pr::BYTES;
@@ -454,11 +490,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
         ((float *)(to + Pr::BETA))[ln.r] = bt;
         ((float *)(to + Pr::WHOLE))[ln.r] = power(all);
     }
-    f32x16 m = {}, p = {};   // k_i . k_j, a row per i;  q_i . k_j, a row per j
+    f32x16 m, p;   // k_i . k_j, a row per i;  q_i . k_j, a row per j
+    auto products = [&]() {
+        m = p = f32x16{};
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-        m = mm<P::MADE>(fk[k], fk[k], m);
-        p = mm<P::MADE>(fk[k], fq[k], p);
+        for (int k = 0; k < D / 16; ++k) {
+            m = mm<P::MADE>(fk[k], fk[k], m);
+            p = mm<P::MADE>(fk[k], fq[k], p);
+        }
+    };
+    products();
+    if (any_broken(m)) {   // (the walks see a broken key themselves, and spoil what it reaches; loaded again, as kept operands would spill)
+        load();
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) drop_broken(fk[k]);
+        products();
     }
     wave_sync();
     const f32x16 below = weights_by_row<true>(sum, x, ln), above = weights_by_row<false>(sum, x, ln);
@@ -677,6 +723,7 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
         if constexpr (!LOCAL)
             if (st.cache && t % P::GRAD_TILES == 0)
                 save_state<KB, DV>(S, ln, st.cache + (((size_t)bh * a.grad_tiles + t / P::GRAD_TILES) * D + d0) * DV + c0);
+        bool spoilt = false;   // (LOCAL: the state that is left is NaN either way)
         f32x16 o = {};   // r: a row per token;  o: a lane per token, a row per column
         {
             f32x16 x = {};
@@ -703,6 +750,16 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
                 if (!trans) r = vt.rows(ln, c0 - v0);
             r -= by_row((const float *)(at + Pr::START), ln) * x;
             x = by_row((const float *)(at + Pr::BETA), ln) * r;
+            if (!LOCAL && any_broken(x)) {
+                spoilt = true;
+                const int first = first_broken(x, ln);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (ln.acc_row(e) >= first) {
+                        x[e] = 0.0f;
+                        r[e] = __builtin_nanf("");
+                    }
+            }
 #pragma unroll
             for (int m = 0; m < 2; ++m) r = mm<MADE>(nt.kp(ln, m), split<MADE>(x, m), r);
         }
@@ -711,6 +768,16 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
         r *= by_row((const float *)(at + Pr::BETA), ln);
         if (!LOCAL && part == SPLIT - 1) {
             o *= ((const float *)(at + Pr::START))[ln.r];
+            if (spoilt) {
+                const int first = first_broken(r, ln);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if (ln.acc_row(e) >= first) r[e] = 0.0f;
+                    if (ln.r >= __shfl(first, ln.acc_row(e))) o[e] = __builtin_nanf("");
+                }
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) S[kb] = first < kTile ? f32x16(__builtin_nanf("")) : S[kb];
+            }
 #pragma unroll
             for (int m = 0; m < 2; ++m) o = mm<P::ROUNDED>(split<P::ROUNDED>(r, m), pt.kp(ln, m), o);
             if (ln.r < valid) store_acc(O + (row + token0 + ln.r) * DV + c0, ln, o);

@@ -1,4 +1,6 @@
-"""The gated delta rule with values that are no numbers, on the GPU: what lies behind a sequence's end is 0 whatever its state holds."""
+"""The gated delta rule with values that are no numbers, on the GPU: what lies behind a sequence's end is 0 whatever its state holds, and
+an infinite or NaN value reaches exactly what the definition makes of it: everything else is, bit for bit, as without it. N, P and the weights of a tile hold zeros where
+a token does not reach another, and 0 x infinity is NaN, so that rows of the same tile are where this can go wrong."""
 import pytest
 import torch
 
@@ -40,3 +42,74 @@ def test_zeros_behind_a_length(L, dtype, kw, bad):
             if name not in ("kv_out", "dkv_in"):
                 for b, n in enumerate(lens):
                     assert (t[b, :, n:] == 0).all(), (name, b, n)
+
+
+def same(name, got, want, where=""):
+    assert torch.equal(got, want), (name, where, int((got != want).sum()), got.numel())
+
+
+def broken(name, got, where=""):
+    assert not torch.isfinite(got.float()).any(), (name, where)
+
+
+def spoil(x, what, j, bad):
+    """One value of one token of the second sequence; the states that it enters and its column."""
+    share = x["v"].shape[1] // x["q"].shape[1]
+    states, head, c = ([1], 1, 11) if what in ("v", "dout") else (list(range(share)), 0, 5)
+    x[what][1, head, j, c] = bad
+    return states, c
+
+
+CASES = [pytest.mark.parametrize("dtype", ["f32", "bf16"]), pytest.mark.parametrize("kw", SIZES + [dict(D=128, N=700), MANY], ids=ids),
+         pytest.mark.parametrize("j,bad", [(0, NAN), (45, INF), (77, NAN), (90, -INF)])]   # (tokens of the same tile in front of and behind it)
+
+
+def cases(fn):
+    for mark in CASES:
+        fn = mark(fn)
+    return fn
+
+
+@cases
+@pytest.mark.parametrize("what", ["v", "q", "k"])
+def test_a_broken_token(L, dtype, kw, j, bad, what):
+    x = make(dtype, seed=2, **{"B": 2, "N": 100, **kw})
+    B, H, N, Dv = x["v"].shape
+    good = Call(L, x, dtype, train=False).run().got()
+    states, c = spoil(x, what, j, bad)
+    for train in (False, True):
+        got = Call(L, x, dtype, train=train).run().got()
+        for b in range(B):
+            for h in range(H):
+                if b != 1 or h not in states:
+                    for name in ("out", "kv_out"):
+                        same(name, got[name][b, h], good[name][b, h], (b, h))
+        (out, was), (state, state_was) = ((got[n][1, states], good[n][1, states]) for n in ("out", "kv_out"))
+        same("out", out[:, :j], was[:, :j], "in front")
+        if what == "v":        # its column of the state, from it on
+            other = [e for e in range(Dv) if e != c]
+            same("out", out[..., other], was[..., other], "other columns")
+            same("kv_out", state[..., other], state_was[..., other], "other columns")
+            broken("out", out[:, j:, c])
+            broken("kv_out", state[..., c])
+        elif what == "q":      # its own output
+            same("out", out[:, j + 1:], was[:, j + 1:], "behind")
+            same("kv_out", state, state_was)
+            broken("out", out[:, j])
+        else:                  # the state from it on
+            broken("out", out[:, j:])
+            broken("kv_out", state)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+def test_tokens_in_front_do_not_depend_on_the_length_of_the_call(L, dtype, what):
+    """A few tokens go one by one, more in tiles: in front of the broken one both give what they gave."""
+    for N in (3, 30):
+        x = make(dtype, N=N, D=128, seed=3)
+        good = Call(L, x, dtype, train=False).run().got()
+        x[what][0, 1, 2, 4] = NAN
+        got = Call(L, x, dtype, train=False).run().got()
+        same("out", got["out"][0, 1, :2], good["out"][0, 1, :2], N)
+        same("out", got["out"][0, 0], good["out"][0, 0], N)
+        assert torch.isnan(got["out"][0, 1, 2].float()).any()
