@@ -536,8 +536,9 @@ int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u
  * Keys are expected to be of length 1 or shorter (lasp_qk_fwd's norm LASP_NORM_L2), with 0 <= beta <= 2: then no state grows; with
  * longer ones it may, as the formula says. States, gates and sums are held in float, sums of log_g in 64 bits. Factors that a call computes
  * go into products in three bfloat16 parts (off by at most 2^-27 of themselves), in two (2^-18) where all that follows is rounded to
- * bfloat16; float data is split in three as for lasp_fwd. An infinity, a NaN or a float that rounds to infinity as bfloat16 in q, k, v or a state
- * makes NaN (or infinity) of what the formulas carry it to, and changes nothing else: no token in front of it, whatever the length of the call.
+ * bfloat16; float data is split in three as for lasp_fwd. An infinity, a NaN or a float that rounds to infinity as bfloat16 in q, k, v, dout, a state or its
+ * gradient makes NaN (or infinity) of what the formulas carry it to, and changes nothing else: no output in front of its token, no gradient that only tokens
+ * away from it enter, whatever the length of the call.
  * Results are bit-reproducible. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, H, N < 1; more than 65535 in B H; D or
  * Dv (0 = D) not 64 or 128; key_heads (0 = H) no divisor of H: H / key_heads consecutive states share a head of q and k, whose gradients are summed.
  */

@@ -132,14 +132,13 @@ DEVI void store_parts(bf16_t *at, f32x4 v) {
 }
 
 // Infinities and NaN. A tile's squares hold zeros where a token does not reach another, and 0 x infinity is NaN: a broken value would spoil tokens of its tile
-// that it does not reach. Operands go without it then, and what it does reach is set to NaN. Whether there is one shows in a sum (one that overflows
-// only costs the search).
-DEVI bool is_broken(float x) { return !(__builtin_fabsf(x) < __builtin_inff()); }
-template <typename V>
-DEVI bool any_broken(const V &x) {   // in any lane of the wave
+// that it does not reach. So N and P are made without broken values, the other operands of their products go without them, which leaves every product as it is for
+// the other tokens, and what a broken value does reach is set to NaN. A state that is broken spoils its whole column, as it should.
+DEVI bool is_broken(float x) { return !(__builtin_fabsf(x) < 0x1.ffp127f); }   // (floats from there on are infinite as bfloat16)
+DEVI bool any_broken(const f32x16 &x) {   // in any lane of the wave (or values so large that their sum is)
     float s[2] = {x[0], x[1]};
 #pragma unroll
-    for (int e = 2; e < (int)(sizeof(V) / 4); ++e) s[e & 1] += x[e];
+    for (int e = 2; e < 16; ++e) s[e & 1] += x[e];
     return __builtin_expect(__builtin_amdgcn_ballot_w64(is_broken(s[0] + s[1])) != 0, 0);
 }
 // The first broken row of the lane's column (32: none).
@@ -149,20 +148,35 @@ DEVI int first_broken(const f32x16 &x, const Lane &ln) {
     for (int e = 0; e < 16; ++e) n = is_broken(x[e]) ? min(n, ln.acc_row(e)) : n;
     return min(n, __shfl_xor(n, 32));
 }
-// Zeros in place of broken elements.
+// Zeros in place of broken bfloat16 elements.
+DEVI u32x4 drop_broken(u32x4 x) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = (x[e] & 0x7f80u) == 0x7f80u ? x[e] & 0xffff0000u : x[e];
+        x[e] = (x[e] & 0x7f800000u) == 0x7f800000u ? x[e] & 0xffffu : x[e];
+    }
+    return x;
+}
 template <int NP>
 DEVI void drop_broken(Frags<NP> &f) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        u32x4 x = __builtin_bit_cast(u32x4, f.p[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] = (x[e] & 0x7f80u) == 0x7f80u ? x[e] & 0xffff0000u : x[e];
-            x[e] = (x[e] & 0x7f800000u) == 0x7f800000u ? x[e] & 0xffffu : x[e];
-        }
-        f.p[i] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int i = 0; i < NP; ++i) f.p[i] = __builtin_bit_cast(bf16x8, drop_broken(__builtin_bit_cast(u32x4, f.p[i])));
 }
+// How far what is broken in a tile reaches: of even and odd tiles the greatest of 32 times a number that grows from tile to tile, plus a number of rows: up to 32
+// from the tile's end the walk goes to.
+template <int COLS>
+struct Marks {
+    int any[2], keys[2], cols[2][COLS];   // (any: the tile's number)
+    DEVI void clear() {
+        for (int e = threadIdx.x; e < (int)(sizeof(*this) / 4); e += blockDim.x) ((int *)this)[e] = -1;
+    }
+    DEVI void mark(int &to, int tile, int rows) {
+        any[tile & 1] = tile;
+        atomicMax(&to, 32 * tile + rows - 1);
+    }
+    DEVI bool at(int tile) const { return __builtin_expect(__builtin_amdgcn_readfirstlane(any[tile & 1]) == tile, 0); }
+    DEVI int rows(int tile, int col) const { return max(max(keys[tile & 1], cols[tile & 1][col]) - 32 * tile + 1, 0); }
+};
 
 // What the lanes of a wave wrote to LDS is there for its other lanes.
 DEVI void wave_sync() {
@@ -312,6 +326,44 @@ struct Fetch {
             const int c = threadIdx.x + n * NT;
             const u32x4 x = c / CPR < rows ? v[n] : u32x4{0, 0, 0, 0};
             if (PIECES % NT == 0 || c < PIECES) f(n, c / CPR, (c % CPR) * EPC, x);
+        }
+    }
+    // Whether this thread's pieces hold a broken value; those are handed to f(row, column) and become zeros.
+    DEVI bool looks_broken() const {
+        if constexpr (sizeof(T) == 2) {   // (by their sum, two elements an instruction)
+            typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+            float y = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned two = v[n][e];   // (a cast of the element itself would take the vector's first)
+                    y = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), bf16x2{1, 1}, y, false);
+                }
+            return __builtin_expect(is_broken(y), 0);
+        } else {
+            bool y = false;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y |= is_broken(__uint_as_float(v[n][e]));
+            return __builtin_expect(y, 0);
+        }
+    }
+    template <typename F>
+    DEVI void drop(F f) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = threadIdx.x + n * NT, row = c / CPR, col = c % CPR * EPC;
+            const bool there = (PIECES % NT == 0 || c < PIECES) && row < rows;
+#pragma unroll
+            for (int e = 0; e < EPC; ++e) {
+                const unsigned x = sizeof(T) == 4 ? v[n][e & 3] : e & 1 ? v[n][e / 2] & 0xffff0000u : v[n][e / 2] << 16;
+                if (!is_broken(__uint_as_float(x))) continue;
+                if (there) f(row, col + e);
+                if constexpr (sizeof(T) == 4) v[n][e & 3] = 0;
+                else v[n][e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
+            }
         }
     }
     template <typename Tl>
@@ -500,10 +552,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_delta_prep(const T *__restrict_
         }
     };
     products();
-    if (any_broken(m)) {   // (the walks see a broken key themselves, and spoil what it reaches; loaded again, as kept operands would spill)
+    if (any_broken(p)) {   // (a broken key shows there, too; loaded again, as operands that are kept would spill)
         load();
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) drop_broken(fk[k]);
+        for (int k = 0; k < D / 16; ++k) {
+            drop_broken(fk[k]);
+            drop_broken(fq[k]);
+        }
         products();
     }
     wave_sync();
@@ -970,7 +1025,8 @@ struct Back {
     typedef Tile<P::DATA, kTile, COLS> Grad;
     static constexpr int PREP = 0, K = Prepared<T>::BYTES, Q = K + Data::BYTES, DO = Q + Data::BYTES, STAGE = DO + Grad::BYTES,
                          XBYTES = SPLIT == 1 ? 0 : 2 * CW * kSquareBytes,
-                         STAGES = 2 * STAGE + XBYTES <= 163840 ? 2 : 1, XCH = STAGES * STAGE, LDS = XCH + XBYTES;
+                         MBYTES = (int)sizeof(Marks<COLS>), STAGES = 2 * STAGE + XBYTES + MBYTES <= 163840 ? 2 : 1, XCH = STAGES * STAGE, MARKS = XCH + XBYTES,
+                         LDS = MARKS + MBYTES;
 };
 struct BackStates {
     const float *last;   // gradients of the states segments end with ([head][segment], or dkv_out where there is one segment); null = zeros
@@ -1011,6 +1067,11 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
         fo.load(dO + (row + token0) * DV + v0, DV, valid);
     };
     if (t0 < t1) fetch(t1 - 1);
+    Marks<L::COLS> &marks = *(Marks<L::COLS> *)(lds + L::MARKS);   // (LOCAL needs none)
+    if constexpr (!LOCAL) {
+        marks.clear();
+        __syncthreads();
+    }
     for (int t = t1 - 1; t >= t0; --t) {
         const int token0 = t * kTile, valid = min(tokens - token0, kTile);
         unsigned char *at = lds + t % L::STAGES * L::STAGE;
@@ -1018,6 +1079,13 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
         const typename L::Grad dot{(bf16_t *)(at + L::DO)};
         const typename Pr::Square nt{(bf16_t *)(at + Pr::N)}, pt{(bf16_t *)(at + Pr::P)};
         if (L::STAGES == 1) __syncthreads();
+        const int number = a.tiles - t;
+        if constexpr (!LOCAL) {   // what is broken reaches the tokens up to it
+            auto token = [&](int row, int) { marks.mark(marks.keys[number & 1], number, row + 1); };
+            if (fk.looks_broken()) fk.drop(token);
+            if (fq.looks_broken()) fq.drop(token);
+            if (fo.looks_broken()) fo.drop([&](int row, int col) { marks.mark(marks.cols[number & 1][col], number, row + 1); });
+        }
         fp.store(at);
         fk.store(kt);
         fq.store(qt);
@@ -1059,6 +1127,11 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
 #pragma unroll
             for (int m = 0; m < 2; ++m) du = mm<MADE>(nt.ksp(ln, m), split<MADE>(x, m), du);
         }
+        if (!LOCAL && marks.at(number)) {
+            const int rows = marks.rows(number, c0 - v0 + ln.r);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) du[e] = ln.acc_row(e) < rows ? __builtin_nanf("") : du[e];
+        }
         const f32x16 dv = beta * du;
         if constexpr (!LOCAL) {
             const size_t to = (row + token0) * DV + c0;
@@ -1088,6 +1161,7 @@ struct Gates {
     double sum[C];
     float start[C], rest[C], beta[C];   // exp(G_i), exp(G_C - G_i)
     float whole;
+    int spoilt;   // something in the tile is broken
 };
 template <typename T, int D>
 struct Grad {
@@ -1213,7 +1287,10 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
                 g.rest[ln.id] = power(all - x);
                 g.beta[ln.id] = bt;
             }
-            if (ln.id == 0) g.whole = power(all);
+            if (ln.id == 0) {
+                g.whole = power(all);
+                g.spoilt = 0;
+            }
         }
         fk.store(kt);
         fq.store(qt);
@@ -1272,6 +1349,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         if (job(n) < L::JOBS) {
             const int jo = job(n), tb = token_block(jo), jb = key_block(jo), i = 32 * tb + ln.r;
             const bool is_em = jo & 1;
+            if (any_broken(pr[n])) g.spoilt = 1;   // (a broken key has spoilt its w, a broken query its dR)
             f32x16 z = {};   // k_j . q_i or k_j . k_i
             if (dlog_g) {
                 const typename L::Data other{is_em ? kt.p : qt.p};
@@ -1310,6 +1388,10 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
             to.st_acc(ln, pr[n]);
         }
     __syncthreads();
+    if (__builtin_expect(g.spoilt, 0)) {   // Ep and Em hold zeros for tokens that a broken one does not reach, NaN for those that it does
+        for (int e = threadIdx.x; e < 2 * L::Data::BYTES / 16; e += NT) ((u32x4 *)(lds + L::K))[e] = drop_broken(((const u32x4 *)(lds + L::K))[e]);
+        __syncthreads();
+    }
 #pragma unroll
     for (int n = 0; n < PER; ++n) {
         const int tk = tk0 + n, m = 32 * tk + ln.r;

@@ -101,6 +101,61 @@ def test_a_broken_token(L, dtype, kw, j, bad, what):
             broken("kv_out", state)
 
 
+@cases
+@pytest.mark.parametrize("what", ["v", "q", "k", "dout"])
+def test_gradients_around_a_broken_token(L, dtype, kw, j, bad, what):
+    x = make(dtype, seed=2, **{"B": 2, "N": 100, **kw})
+    B, H, N, Dv = x["v"].shape
+    share = H // x["q"].shape[1]
+    good = Call(L, x, dtype).run().got()
+    states, c = spoil(x, what, j, bad)
+    got = Call(L, x, dtype).run().got()
+    grads = [n for n in got if n not in ("out", "kv_out")]
+    heads = {n: sorted({s // share for s in states}) if n in ("dq", "dk") else states for n in grads}
+    for n in grads:      # other sequences and heads
+        for b in range(B):
+            for h in range(got[n].shape[1]):
+                if b != 1 or h not in heads[n]:
+                    same(n, got[n][b, h], good[n][b, h], (b, h))
+    of, was = ({n: t[n][1, heads[n]] for n in grads} for t in (got, good))
+    other = [e for e in range(Dv) if e != c]
+
+    def unchanged(names, a, b):
+        for n in names:
+            same(n, of[n][:, a:b], was[n][:, a:b], (a, b))
+
+    def spoilt(names, a, b):
+        for n in names:
+            broken(n, of[n][:, a:b], (a, b))
+
+    if what == "v":        # the state's column from it on; gradients of v and of the state do not depend on it, nor does its own gate's (which stands in front of it)
+        unchanged(["dv", "dkv_in"], 0, None)
+        unchanged(["dq", "dk", "dbeta"], 0, j)
+        unchanged(["dlog_g"], 0, j + 1)
+        spoilt(["dq", "dk", "dbeta"], j, N)
+        spoilt(["dlog_g"], j + 1, N)
+    elif what == "q":      # the state's gradient up to it
+        unchanged(["dq"], 0, N)
+        unchanged(["dv", "dk", "dbeta", "dlog_g"], j + 1, N)
+        spoilt(["dv", "dk", "dbeta", "dlog_g"], 0, j + 1)
+        spoilt(["dkv_in"], 0, None)
+    elif what == "k":      # both
+        unchanged(["dq"], 0, j)
+        unchanged(["dv"], j + 1, N)
+        spoilt(["dq"], j, N)
+        spoilt(["dv"], 0, j + 1)
+        spoilt(["dk", "dbeta", "dlog_g", "dkv_in"], 0, None)
+    else:                  # a column of the state's gradient up to it
+        unchanged(["dq"], 0, j)
+        unchanged(["dq", "dv", "dk", "dbeta", "dlog_g"], j + 1, N)
+        for n in ("dv", "dkv_in"):
+            same(n, of[n][..., other], was[n][..., other], "other columns")
+        broken("dv", of["dv"][:, :j + 1, c])
+        broken("dkv_in", of["dkv_in"][..., c])
+        spoilt(["dq"], j, j + 1)
+        spoilt(["dk", "dbeta", "dlog_g"], 0, j + 1)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("what", ["q", "k", "v"])
 def test_tokens_in_front_do_not_depend_on_the_length_of_the_call(L, dtype, what):
