@@ -521,7 +521,7 @@ int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u
  *   q, k, dq, dk      [B][key_heads][N][D] of `dtype`.    v, out, dout, dv  [B][H][N][Dv] of `dtype`.
  *   beta, dbeta       [B][H][N] float, any finite value (0..1, or up to 2).
  *   log_g, dlog_g     [B][H][N] float, <= 0; -inf: a = 0, the state starts anew at that token (documents packed into one sequence),
- *                     and the gradient there is 0. Both NULL = no decay (a = 1). From 2^-150 down a counts as 0. Values
+ *                     and the gradient there is 0. Both NULL = no decay (a = 1). Below 2^-126 a counts as 0. Values
  *                     > 0 or NaN give undefined numbers (never a fault).
  *   len               NULL, or DEVICE int32 [B]: tokens of every sequence, 0 <= len <= N (other values count as the nearest of these). What the
  *                     inputs hold past it is not looked at; out and all gradients are 0 there.

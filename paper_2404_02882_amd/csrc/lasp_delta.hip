@@ -427,6 +427,7 @@ DEVI double to_base2(float log_g) {
     const double x = (double)log_g * 1.4426950408889634;
     return x < -300.0 ? -300.0 : x;   // (NaN stays)
 }
+constexpr double kLeastGate = -126.0;   // (the power of less is 0)
 DEVI float power(double d) { return __builtin_amdgcn_exp2f((float)d); }
 // Sums over the lanes of C up to this one.
 template <int C>
@@ -1469,7 +1470,7 @@ __global__ __launch_bounds__((Grad<T, D>::NT), (Grad<T, D>::PER_SIMD)) void k_de
         if ((ln.id & (C - 1)) + d < C) up += y;
     }
     if (ln.id < there) {
-        const bool none = ln.id >= valid || to_base2(a.log_g[row + ln.id]) <= -150.0;   // (a gate of 0 has no slope)
+        const bool none = ln.id >= valid || to_base2(a.log_g[row + ln.id]) < kLeastGate;   // (a gate of 0 has no slope)
         dlog_g[row + ln.id] = none ? 0.0f : (float)(g.whole * all + up + on + z);
     }
 }

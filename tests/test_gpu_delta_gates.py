@@ -44,3 +44,19 @@ def test_slopes_of_gates_that_let_little_pass(L, O, dtype, kw, down):
         off = np.abs(got[:, :, p] - w[:, :, p]) / (2 * O.DELTA * size)
         print(f"  token {p}: {off.max():.3f} of the bound, slope {np.abs(w[:, :, p]).max():.2e}", flush=True)
         assert off.max() <= 1.0, (p, off.max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("train,N", [(True, 130), (False, 70), (False, 3)])
+def test_gates_below_the_least_are_none(L, dtype, train, N):
+    """A gate below 2^-126 counts as 0: all results are those of -infinity, bit for bit."""
+    results = []
+    for down in (-np.log(2.0) * 126.5, -100.0, -float("inf")):
+        x = make(dtype, N=N, seed=5)
+        x["log_g"][..., [p for p in (0, 2, 31, 32, 50, 64) if p < N]] = down
+        results.append(Call(L, x, dtype, train=train).run().got())
+    for got in results[:2]:
+        for name, t in got.items():
+            assert torch.equal(t, results[2][name]), name
+    if train:
+        assert (results[0]["dlog_g"][..., [0, 2, 31, 32, 50, 64]] == 0).all()
