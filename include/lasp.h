@@ -530,15 +530,17 @@ int lasp_gatenorm_bwd(const lasp_gate_shape *shape, const void *o, const void *u
  *   state_cache       forward: NULL = no backward pass will follow; else lasp_delta_cache_bytes() bytes, to be handed to lasp_delta_bwd
  *                     with the same shape and inputs (it holds kv_in too): a float state for every 64 tokens (float data: 32), a float for every
  *                     value, two squares of 32 by 32 for every 32 tokens, and two of D by D for every segment that a long sequence is cut into.
- *   scratch           lasp_delta_scratch_bytes() bytes forward (those squares, and the states between segments), lasp_delta_bwd_scratch_bytes()
- *                     backward (as many states and floats as the cache has). Not looked at by forward calls without a cache of at most 4
- *                     tokens (float data: 8), which run token by token.
+ *   scratch           forward: lasp_delta_scratch_bytes() bytes, those squares of 32 by 32, and one of D by D and two states for every segment (with a
+ *                     cache the squares lie there, but as much is asked for); not looked at by calls without a cache of at most 4 tokens (float
+ *                     data: 8), which run token by token. backward: lasp_delta_bwd_scratch_bytes() bytes, as many states and floats as the cache
+ *                     has, two states for every segment, and with key_heads < H two float tensors [B][H][N][D].
  * Keys are expected to be of length 1 or shorter (lasp_qk_fwd's norm LASP_NORM_L2), with 0 <= beta <= 2: then no state grows; with
  * longer ones it may, as the formula says. States, gates and sums are held in float, sums of log_g in 64 bits. Factors that a call computes
- * go into products in three bfloat16 parts (off by at most 2^-27 of themselves), in two (2^-18) where all that follows is rounded to
- * bfloat16; float data is split in three as for lasp_fwd. An infinity, a NaN or a float that rounds to infinity as bfloat16 in q, k, v, dout, a state or its
+ * go into products in three bfloat16 parts, which hold all of a float's bits (where two such meet, less than 2^-23 of their product is left out), and in two, off
+ * by at most 2^-17 (where two such meet, at most another 2^-16 of their product), where all that follows is rounded to bfloat16; float data is split in three as
+ * for lasp_fwd. An infinity, a NaN or a float that rounds to infinity as bfloat16 in q, k, v, dout, a state or its
  * gradient makes NaN (or infinity) of what the formulas carry it to, and changes nothing else: no output in front of its token, no gradient that only tokens
- * away from it enter, whatever the length of the call.
+ * away from it enter, whatever the length of the call. (a = 0 times a broken state is NaN.)
  * Results are bit-reproducible. Statuses and asynchrony as for lasp_fwd. Refused (LASP_ERR_SHAPE): B, H, N < 1; more than 65535 in B H; D or
  * Dv (0 = D) not 64 or 128; key_heads (0 = H) no divisor of H: H / key_heads consecutive states share a head of q and k, whose gradients are summed.
  */
