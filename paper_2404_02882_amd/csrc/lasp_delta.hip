@@ -396,21 +396,7 @@ struct Copy {
     }
 };
 
-// 16 features of the lane's token in the order of an accumulator tile (p: the token's row at the tile's first feature).
-template <typename T>
-DEVI f32x16 load_acc(const T *p, const Lane &ln, bool there) {
-    f32x16 x = {};
-    if (there)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            f32x4 v;
-            if constexpr (sizeof(T) == 2) v = __builtin_convertvector(*(const bf16x4 *)(p + 8 * g + 4 * ln.h), f32x4);
-            else v = *(const f32x4 *)(p + 8 * g + 4 * ln.h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
-        }
-    return x;
-}
+// 16 features of the lane's token, as an accumulator tile has them (p: the token's row at the tile's first feature).
 template <typename T>
 DEVI void store_acc(T *p, const Lane &ln, const f32x16 &x) {
 #pragma unroll
@@ -863,8 +849,8 @@ __global__ __launch_bounds__((Walk<T, D, DV, LOCAL, SPLIT>::NT), (waves_of<T, D,
 
 // ---------------------------------------------------------------------------
 // k_delta_scan: first[0] = in, first[p + 1] = T_p first[p] + local[p]; BACK: last[P - 1] = in, last[p - 1] = T_p^T last[p] + local[p].
-// 16 columns a workgroup, in float. 32 segments x 16 heads of 128: 82 us in either direction, 2.5 us a step, a chain of barrier, LDS and 32 matrix
-// products on top of each other; more matrices on their way change nothing. (Fewer segments cost the walks what they save here.)
+// 16 columns a workgroup, 16 rows a wave, in float. 32 segments x 16 heads of 128: 82 us in either direction, 2.5 us a step, a chain of barrier, LDS and 32
+// matrix products on top of each other; more matrices on their way change nothing. (Fewer segments cost the walks what they save here.)
 // ---------------------------------------------------------------------------
 // (v_mfma_f32_16x16x4_f32: lane l supplies row or column l & 15 and contraction index l >> 4; accumulator rows 4 (l >> 4) .. + 3, column l & 15.)
 constexpr int kScanCols = 16;
@@ -872,64 +858,51 @@ template <int D, bool BACK>
 __global__ __launch_bounds__(4 * D) void k_delta_scan(const float *__restrict__ in, const float *__restrict__ trans, const float *__restrict__ local,
                                                          float *__restrict__ states, int Dv, int segments) {
     __shared__ __attribute__((aligned(16))) float S[2][kScanCols][D + 4];   // a row per column
-    constexpr int TILES = 1;   // 16 rows a wave
     const int bh = blockIdx.x, c = blockIdx.y * kScanCols + (threadIdx.x & 15), wave = threadIdx.x >> 6, l16 = threadIdx.x & 15, l4 = threadIdx.x >> 4 & 3;
     struct Step {
-        f32x4 add[TILES];
-        float m[TILES][D / 4];   // contraction 16 s + 4 l4 + i at 4 s + i
+        f32x4 add;
+        float m[D / 4];   // contraction 16 s + 4 l4 + i at 4 s + i
     };
-    f32x4 x[TILES];
-    auto at = [&](size_t segment, int tl, int i) { return (segment * D + 16 * (wave * TILES + tl) + 4 * l4 + i) * Dv + c; };
+    f32x4 x;
+    auto at = [&](size_t segment, int i) { return (segment * D + 16 * wave + 4 * l4 + i) * Dv + c; };
     auto fetch = [&](Step &to, int step) {
         step = min(step, segments - 2);   // (without a branch, behind which no load could be waited for apart from those that follow it)
         const int p = BACK ? segments - 1 - step : step;
         const float *t = trans + ((size_t)bh * segments + p) * D * D;
 #pragma unroll
-        for (int tl = 0; tl < TILES; ++tl) {
+        for (int s = 0; s < D / 16; ++s) {
+            const f32x4 y = *(const f32x4 *)(t + matrix_piece<D>(wave, s, l16, l4));
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                const f32x4 y = *(const f32x4 *)(t + matrix_piece<D>(wave * TILES + tl, s, l16, l4));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) to.m[tl][4 * s + i] = y[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) to.add[tl][i] = local[at((size_t)bh * segments + p, tl, i)];
+            for (int i = 0; i < 4; ++i) to.m[4 * s + i] = y[i];
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to.add[i] = local[at((size_t)bh * segments + p, i)];
     };
     auto go = [&](const Step &now, int step) {   // the state in front of this step's segment is written, and taken through it
         const int p = BACK ? segments - 1 - step : step;
         auto &lds = S[step & 1];   // (read by the other waves until the barrier of the next step)
+        *(f32x4 *)(&lds[l16][16 * wave + 4 * l4]) = x;
 #pragma unroll
-        for (int tl = 0; tl < TILES; ++tl) {
-            *(f32x4 *)(&lds[l16][16 * (wave * TILES + tl) + 4 * l4]) = x[tl];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) states[at((size_t)bh * segments + p, tl, i)] = x[tl][i];
-        }
+        for (int i = 0; i < 4; ++i) states[at((size_t)bh * segments + p, i)] = x[i];
         if (step + 1 == segments) return;
         __syncthreads();
-        f32x4 y[D / 16], z[TILES] = {};
+        f32x4 y[D / 16], z = {};
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) y[s] = *(const f32x4 *)(&lds[l16][16 * s + 4 * l4]);
-#pragma unroll
-        for (int tl = 0; tl < TILES; ++tl) x[tl] = now.add[tl];
+        x = now.add;
         __builtin_amdgcn_sched_barrier(0);   // (all reads are on their way before the first product waits for one)
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int tl = 0; tl < TILES; ++tl) {   // (two chains a tile)
-                    auto &sum = i & 1 ? z[tl] : x[tl];
-                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(now.m[tl][4 * s + i], y[s][i], sum, 0, 0, 0);
-                }
-#pragma unroll
-        for (int tl = 0; tl < TILES; ++tl) x[tl] += z[tl];
+            for (int i = 0; i < 4; ++i) {   // (two chains)
+                auto &sum = i & 1 ? z : x;
+                sum = __builtin_amdgcn_mfma_f32_16x16x4f32(now.m[4 * s + i], y[s][i], sum, 0, 0, 0);
+            }
+        x += z;
     };
 #pragma unroll
-    for (int tl = 0; tl < TILES; ++tl)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[tl][i] = in ? in[at(bh, tl, i)] : 0.0f;
-    constexpr int AHEAD = 2;   // (a matrix is on its way while the one before is used: what a CU can load, 20 bytes a ns, bounds a step)
+    for (int i = 0; i < 4; ++i) x[i] = in ? in[at(bh, i)] : 0.0f;
+    constexpr int AHEAD = 2;   // (a matrix is on its way while the one before is used)
     Step ring[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD - 1; ++i) fetch(ring[i], i);
