@@ -10,6 +10,11 @@ HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
 # makes an error grow (keys of length 1, 0 <= beta <= 2: I - beta k k^T has no value beyond 1). Eight of them, four times that for
 # terms that partly cancel: 4 * 8 * sqrt(192) * 2^-24 = 2.6e-5 of the result's 2-norm.
 DELTA = 4 * 8 * 192 ** 0.5 * 2.0 ** -24
+# What float sums come to, as roundings of random sign spread evenly over half a step do: 2^-24 / sqrt(3) of a partial sum each, and partial sums of n terms grow to the
+# whole one like sqrt(n), so that n roundings have sqrt(n / 2) of the last one's: sqrt(n / 6) 2^-24 of the sum, n at most D + 32 = 160 (a tile has 32 tokens). Eight of
+# them independent of one another, twice that for terms that partly cancel: 2 sqrt(8 * 160 / 6) 2^-24 = 1.7e-6 of the 2-norm of a result of thousands of elements.
+# Products whose computed factors are cut to two bfloat16 parts (2^-17) are off by more.
+FLOAT = 2 * (8 * 160 / 6) ** 0.5 * 2.0 ** -24
 
 
 def delta_fwd(q, k, v, log_g, beta, kv_in=None, lens=None):
@@ -79,6 +84,12 @@ def off(got, want, dtype, float_part=DELTA, floor=0.0):
     by_norm = np.linalg.norm(err) / ((half + float_part) * norm)
     rms = norm / want.size ** 0.5
     return max(by_norm, (err / (half * np.abs(want) + 16 * float_part * np.maximum(rms, np.abs(want)))).max())
+
+
+def off_in_norm(got, want, floor=0.0):
+    """The 2-norm of the difference in units of FLOAT times that of `want` (or of the size `floor` of its elements)."""
+    want = np.asarray(want, dtype=np.float64)
+    return np.linalg.norm(np.asarray(got, dtype=np.float64) - want) / (FLOAT * max(np.linalg.norm(want), floor * want.size ** 0.5))
 
 
 # ---------------------------------------------------------------------------

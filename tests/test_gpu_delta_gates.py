@@ -60,3 +60,16 @@ def test_gates_below_the_least_are_none(L, dtype, train, N):
             assert torch.equal(t, results[2][name]), name
     if train:
         assert (results[0]["dlog_g"][..., [0, 2, 31, 32, 50, 64]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kw", [dict(N=200, D=64), dict(N=200, D=128), dict(N=200, D=64, Dv=128, H=4, Hk=2), dict(N=1100, D=128, Dv=64), dict(N=1100, D=64),
+                                dict(N=67, D=64, B=9, H=32, Hk=16), dict(N=67, D=128, B=9, H=32)], ids=lambda kw: "-".join(f"{k}{v}" for k, v in kw.items()))
+def test_float_results_are_as_good_as_float_sums(L, O, dtype, kw):
+    """States and the slopes of gates and betas, of either data type, in the 2-norm over all of them. (A slope is a sum of terms of either sign: held to 0.05 a token at least.)"""
+    x = make(dtype, seed=6, **kw)
+    call, w = Call(L, x, dtype).run(), want(O, x)
+    for name, floor in (("kv_out", 0.0), ("dkv_in", 0.0), ("dlog_g", 0.05), ("dbeta", 0.05)):
+        off = O.off_in_norm(np64(call.got()[name]), w[name], floor)
+        print(f"  {name}: {off:.3f}", flush=True)
+        assert off <= 1.0, (name, off)
