@@ -11,6 +11,7 @@ pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
 SIZES = [dict(D=64), dict(D=128), dict(D=64, Dv=128, H=4, Hk=2), dict(D=128, Dv=64)]
 MANY = dict(B=9, H=32, D=64)      # (a wave then has all key features of its columns)
+WIDE = [dict(MANY, D=128), dict(MANY, D=128, Dv=64), dict(MANY, Dv=128)]
 
 
 @pytest.fixture(scope="module")
@@ -60,7 +61,7 @@ def spoil(x, what, j, bad):
     return states, c
 
 
-CASES = [pytest.mark.parametrize("dtype", ["f32", "bf16"]), pytest.mark.parametrize("kw", SIZES + [dict(D=128, N=700), MANY], ids=ids),
+CASES = [pytest.mark.parametrize("dtype", ["f32", "bf16"]), pytest.mark.parametrize("kw", SIZES + [dict(D=128, N=700), MANY] + WIDE, ids=ids),
          pytest.mark.parametrize("j,bad", [(0, NAN), (45, INF), (77, NAN), (90, -INF)])]   # (tokens of the same tile in front of and behind it)
 
 
@@ -154,6 +155,34 @@ def test_gradients_around_a_broken_token(L, dtype, kw, j, bad, what):
         broken("dkv_in", of["dkv_in"][..., c])
         spoilt(["dq"], j, j + 1)
         spoilt(["dk", "dbeta", "dlog_g"], 0, j + 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kw", SIZES + [dict(D=128, N=700), MANY], ids=ids)
+@pytest.mark.parametrize("bad", [NAN, -INF])
+@pytest.mark.parametrize("what", ["kv_in", "dkv_out"])
+def test_a_broken_state(L, dtype, kw, bad, what):
+    """One element of a head's state, or of its gradient: its column, whatever the tokens are."""
+    x = make(dtype, seed=4, **{"B": 2, "N": 100, **kw})
+    Dv, share = x["v"].shape[-1], x["v"].shape[1] // x["q"].shape[1]
+    good = Call(L, x, dtype).run().got()
+    x[what][1, 1, 7, 11] = bad
+    got = Call(L, x, dtype).run().got()
+    other = [e for e in range(Dv) if e != 11]
+    forward, columns = what == "kv_in", ("out", "kv_out") if what == "kv_in" else ("dv", "dkv_in")
+    for n, t in got.items():
+        head = 1 // share if n in ("dq", "dk") else 1
+        for b in range(t.shape[0]):
+            for h in range(t.shape[1]):
+                if (b, h) != (1, head):
+                    same(n, t[b, h], good[n][b, h], (b, h))
+        if n in columns:
+            same(n, t[1, 1][..., other], good[n][1, 1][..., other], "other columns")
+            broken(n, t[1, 1][..., 11])
+        elif n in (("dv", "dkv_in") if forward else ("out", "kv_out", "dq")):
+            same(n, t[1, head], good[n][1, head])
+        else:
+            broken(n, t[1, head])
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
