@@ -23,9 +23,9 @@
 // leave them further off than float sums do. Two where all that follows is rounded to bfloat16, by up to 2^-8: one output in 300 then differs by a step from what float
 // products round to, and the distance from the definition is the same in four digits (three: 8 prompts up to 1777 tokens 206 us instead of 197). Float data is
 // split in three as well. Products of parts i + j >= 3 (of two: 2) are left out, less than 2^-23 (at most 2^-16) of a product of two such factors.
-// 32768 tokens x 16 heads of 128, bfloat16, forward and backward: 1.98 ms, 12 KB of memory a token and head (6.3 GB, 3.2 TB/s over all):
+// 32768 tokens x 16 heads of 128, bfloat16, forward and backward: 1.99 ms, 12 KB of memory a token and head (6.3 GB, 3.2 TB/s over all):
 // outputs and inputs are 2.8 KB of it, the rest states and their gradients every 64 tokens (4 KB), w and dR in float (2 KB), N, P and gates
-// (1.9 KB), and keys, queries and values read again. k_delta_walk and k_delta_back run at 4.6 TB/s of it.
+// (1.9 KB), and keys, queries and values read again. k_delta_walk and k_delta_back run at 4.4 TB/s of it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -478,7 +478,7 @@ struct Prepared {
 // ---------------------------------------------------------------------------
 // k_delta_prep: a wave per tile, keys and queries straight into operands. N in blocks of 16 by substitution, a lane per column; then joined,
 //     N21 = -(I + N22 beta) M21 (I + beta N11).
-// 16384 tiles of 128 features: 98 us, 4.8 TB/s: bound by memory.
+// 16384 tiles of 128 features: 99 us, 4.8 TB/s: bound by memory.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 DEVI void operands(Frags<Parts<T>::DATA> (&f)[D / 16], const T *row, const Lane &ln, bool there) {
@@ -686,7 +686,7 @@ DEVI void save_matrix(const f32x16 (&S)[KB], const Lane &ln, int d0, int c, floa
 // order of the accumulator's rows; the waves share the tile's keys, queries, N and scores in LDS. SPLIT = 2: two waves have half of the key
 // features of 32 columns each, and add up S^T k and S^T q once a tile. LOCAL: no outputs; the state a segment reaches
 // from zero, and (waves behind those of the values) its matrix T, which is the state reached from the identity without values.
-// 32768 tokens x 16 heads of 128, bfloat16, with a cache: 335 us, 4.6 TB/s, memory; LOCAL: 345 us over twice the columns, 1.4 TB/s, bound by what
+// 32768 tokens x 16 heads of 128, bfloat16, with a cache: 349 us, 4.4 TB/s, memory (2 % of it the look for broken values); LOCAL: 350 us over twice the columns, 1.4 TB/s, bound by what
 // a wave issues (a tile takes 3.6 us of matrix products, parts of accumulators and waits for LDS, one after the other).
 // ---------------------------------------------------------------------------
 template <typename T, int D, int DV, bool LOCAL, int SPLIT>
@@ -990,7 +990,8 @@ __global__ __launch_bounds__(kThreads) void k_delta_step(const T *__restrict__ Q
 
 // ---------------------------------------------------------------------------
 // k_delta_back: the walk in reverse (SPLIT as there; the sum is dU's). LOCAL: the gradient that reaches a segment's front from its own tokens.
-// Sizes as above: 335 us, 4.6 TB/s; LOCAL 250 us.
+// What a thread stages is looked at for broken values on its way, which costs no register behind it (a look at dU and dO where they are used: 34 registers spilt, 78 us more).
+// Sizes as above: 355 us, 4.3 TB/s; LOCAL 250 us.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int DV, int SPLIT>
 struct Back {
@@ -1128,7 +1129,7 @@ __global__ __launch_bounds__((Back<T, D, DV, SPLIT>::NT), (waves_of<T, D, DV, SP
 // ---------------------------------------------------------------------------
 // k_delta_grad: a tile's gradients, from the state in front of it, the gradient of the one behind it, w and dR, 64 value features at a time. A wave
 // has 32 key features of dQ and dK; its rows of both states come from memory straight into its registers, as they are read once.
-// 32768 tokens x 16 heads of 128, bfloat16: 610 us, 4.6 KB a token and head (3.9 TB/s), two workgroups of four waves a CU, as LDS has room for. (With
+// 32768 tokens x 16 heads of 128, bfloat16: 608 us, 4.6 KB a token and head (3.9 TB/s), two workgroups of four waves a CU, as LDS has room for. (With
 // loads that a branch may leave out, every wait was one for all of them: 640; keys of 64, 8 x 4096 x 8 heads, 257 us against 235.)
 // ---------------------------------------------------------------------------
 template <int C>
@@ -1612,12 +1613,13 @@ struct Backward {
 
 // Segments: a walk takes the longer the fewer workgroups it has. Cutting a sequence costs a second walk (the local one, over twice the
 // columns) and a chain of one step a segment: two workgroups a CU are looked for, a segment has two tiles or more, the chain is kept to a
-// part of the walk, and fewer than five segments do not pay. (Forward, bf16, heads of 128: 8 x 1777 tokens x 16 heads 217 us uncut, 303 in
-// four; 16384 x 8 heads 250 us in 31 segments, 316 in 52. Forward and backward: 32768 x 16 heads 2.03 ms in 32 as in 16, 2.2 in 48;
-// 8 x 4096 x 8 heads with keys of 64 705 us in eight, 730 uncut; 4096 x 16 heads 372 us in 16, 424 in 26, 396 in 11.)
+// part of the walk, and fewer than five segments do not pay, also where that leaves CUs without a workgroup. (Forward, bf16, heads of 128: 8 x 1777 tokens
+// x 16 heads 234 us uncut, 327 in four; 7 x 4096 x 16 474 and 581, values of 64 477 and 505, 7 x 16384 x 16 1880 and 2170; 16384 x 8 heads 230 us in 32
+// segments, 1570 uncut. Forward and backward: 32768 x 16 heads 2.0 ms in 32 segments, 7.7 uncut; 8 x 4096 x 8 heads with keys of 64 672 us in eight, 921 uncut. The
+// chain's part, on an earlier state of these kernels: 32768 x 16 heads 2.03 ms in 32 as in 16, 2.2 in 48; 4096 x 16 heads 372 us in 16, 424 in 26, 396 in 11.)
 // split: a second wave to every 32 columns, which takes half of the key features, as long as every such workgroup has a CU to itself. (The
-// two meet once a tile: 8 x 1777 x 16 heads 217 us with it and 253 without, float, 2 x 1001 x 4 heads, forward and backward 153 and 185;
-// beyond that it costs: 12 x 1777 x 16 heads 405 us with it, 275 without.)
+// two meet once a tile: 8 x 1777 x 16 heads 234 us with it and 277 without, 7 x 4096 x 16 474 and 606, float, 2 x 1001 x 4 heads, forward and backward 149 and 197;
+// beyond that it costs: 12 x 1777 x 16 heads 407 us with it, 298 without.)
 DeltaPlan delta_plan(int B, int H, int N, int D, int Dv, int dtype, int key_heads) {
     DeltaPlan p{B, H, N, D, Dv, dtype, key_heads};
     p.tiles = (int)(((long long)N + kTile - 1) / kTile);

@@ -6,7 +6,9 @@
 // sines of the tokens it takes, each angle once for all heads (an angle costs about as much as ten rows' pieces: position times frequency in 64 bits, whole turns
 // taken off there, so that far positions keep the float's precision), then its threads go over the rows of these tokens, queries and keys.
 // Bound by memory: 32768 tokens x 16 + 16 heads of 128, bfloat16: forward 112 us (4.8 TB/s), backward 155 (5.2 TB/s). A row's next piece is
-// loaded before this one is used. A few tokens (64 x 16 + 4 heads): 5.2 us, launch, table and one row one after the other.
+// loaded before this one is used. A few tokens (64 x 16 + 4 heads): 5.2 us, launch, table and one row one after the other. Where a group's tokens have fewer heads than the
+// workgroup takes rows at a time, threads are idle and the table and its barriers bound it: 65536 tokens, heads of 128, 8 + 8 of them 4.5 TB/s forward and 5.0 backward,
+// 4 + 4 4.3 and 4.2, 4 + 1 2.4 and 2.9, 1 + 1 0.8 and 1.0.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,7 +28,8 @@ struct QkCall {
     const int *pos;
 };
 
-// The rows (heads of tokens) that a thread comes to in a group, one after the other; counted up, as a division takes as long as the row itself.
+// The rows (heads of tokens) that a thread comes to in a group, one after the other; counted up, as a division takes as long as the row itself (one subtraction a row
+// with 16 heads of 128; with one head sixteen of them).
 struct Walk {
     int slot, head, b, s;    // token of the group, its head, sequence and place there
     int left;                // rows left up to the last of the group, less than 1: none
@@ -287,7 +290,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_bwd(const T *__restrict__ xq, c
 
 constexpr int kCus = 256;
 // Tokens of a group: four, and no more than the table holds or than leave four workgroups a CU something to do (bf16, 32768 tokens x 16 + 16
-// heads of 128, with eight workgroups a CU: forward 122 us with four, 126 with eight, 128 with 16; backward 155, 162, 163).
+// heads of 128, with eight workgroups a CU: forward 122 us with four, 126 with eight, 128 with 16; backward 155, 162, 163). Measured with many heads; with few
+// of them four tokens are too few rows for a workgroup (rates at the top).
 int group_of(const QkPlan &p) {
     const long long tokens = (long long)p.B * p.N;
     const long long room = p.rot ? std::min(4, kTable / (p.rot / 2)) : 4;
