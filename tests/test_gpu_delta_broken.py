@@ -197,3 +197,12 @@ def test_tokens_in_front_do_not_depend_on_the_length_of_the_call(L, dtype, what)
         same("out", got["out"][0, 1, :2], good["out"][0, 1, :2], N)
         same("out", got["out"][0, 0], good["out"][0, 0], N)
         assert torch.isnan(got["out"][0, 1, 2].float()).any()
+
+
+@pytest.mark.parametrize("what", ["q", "k", "dout"])
+@pytest.mark.parametrize("kw", [dict(D=64), dict(D=128)], ids=ids)
+def test_floats_that_round_to_infinity(L, what, kw):
+    """Finite, but infinite as bfloat16: as an infinity."""
+    if what != "dout":
+        test_a_broken_token(L, "f32", kw, 45, 3.4e38, what)
+    test_gradients_around_a_broken_token(L, "f32", kw, 45, 3.4e38, what)
